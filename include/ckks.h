@@ -324,6 +324,77 @@ int he_poly_act_deg7(const ckks_ctx* ctx, const uint64_t* const* h_d_x, uint32_t
                      const int64_t* h_k, const ckks_key* rlk, int merged_division, uint64_t* const* h_d_out,
                      void* d_ws, size_t ws_bytes, void* stream);
 
+/* ---- A transformer block's operators on channel-by-channel packed ciphertexts (not from the paper, whose networks are convolutional;
+ * the packing is its own: ciphertext c of a vector holds channel c, the slots are the tokens, image or video positions of a batch).
+ * Operators that mix channels are sums over ciphertexts, operators on a token's channels act in every slot at once, and no rotation is
+ * needed.  All three take ciphertexts at equal distances in memory instead of pointer lists, as a vector has any number of them. */
+typedef struct he_ct_array {
+    const uint64_t* d;    /* device; limb e of component k of ciphertext i is the N words at d + i*ct_stride + k*comp_stride + e*N */
+    uint64_t ct_stride;   /* words between ciphertexts */
+    uint64_t comp_stride; /* words between components: (L+1)*N where the ciphertexts were made at a level L above the operation's */
+} he_ct_array;            /* d aligned to 16 bytes, strides multiples of two words; comp_stride >= (limbs read)*N, ct_stride >= comp_stride + (limbs read)*N,
+                             or 0: one ciphertext in the place of all (checked where there is more than one ciphertext or component) */
+
+/* Matrix products grouped by expert with ragged sizes: row t of group g (a token block's c_in channel ciphertexts, tokens in the
+ * slots) times that group's weights,
+ *   out[t][o] = Rescale( multiplier * sum_{c < c_in} W_g[o][c] * in[t][c] + (bias_g[o], 0) ),
+ * one level lower.  Rows are numbered through the groups: h_group_rows[g] >= 0 rows of group g follow each other, row t's ciphertexts
+ * are in[t*c_in .. t*c_in + c_in - 1], its outputs out[t*c_out ..] (compact, uint64[2][level][N]).  The sums run over ciphertexts, so a
+ * 1x1 convolution, a shortcut's projection and a transformer's linear layers are this operator with one group.
+ * d_w: signed integers of weight_type, [n_groups][c_out][c_in], or with transposed != 0 [n_groups][c_in][c_out], the product then being with
+ * the transpose of what the forward pass of a layer c_out -> c_in takes: the gradient with respect to that layer's input.
+ * multiplier: a positive integer; a real weight v is W = round(v / step) with multiplier = round(step * q_level) to return to the scale of
+ * the input.  d_bias (or NULL): uint64[n_groups][c_out][level+1], residues of the bias times the scale before the division (the input's
+ * scale times multiplier / step); the same value joins every slot.  c_in, c_out <= 65536. */
+enum he_weight_type { HE_WEIGHT_INT8 = 1, HE_WEIGHT_INT16 = 2, HE_WEIGHT_INT32 = 4 };
+typedef struct he_linear_desc {
+    uint32_t c_in, c_out, n_groups, level;
+    uint32_t weight_type; /* he_weight_type */
+    uint32_t transposed;
+    uint64_t multiplier;
+} he_linear_desc;
+size_t he_linear_workspace_bytes(const ckks_ctx* ctx, const he_linear_desc* desc, const uint32_t* h_group_rows);
+int he_linear_grouped(const ckks_ctx* ctx, const he_linear_desc* desc, const uint32_t* h_group_rows, const he_ct_array* in, const void* d_w,
+                      const uint64_t* d_bias, uint64_t* d_out, void* d_ws, size_t ws_bytes, void* stream);
+
+/* Rotary positions with several axes (time, height, width: the slots are the positions): in every head, channel pair j of n_pairs turns by
+ * its angle, which differs from slot to slot,
+ *   out_a = Rescale(in_a (.) C_j - in_b (.) S_j),  out_b = Rescale(in_a (.) S_j + in_b (.) C_j),
+ * (a, b) = (j, j + n_pairs), interleaved: (2j, 2j + 1).  C_j, S_j: cosine and sine of pair j's frequency times the slot's position on the
+ * pair's axis, encoded at the scale of q_level (d_cos, d_sin uint64[n_pairs][level+1][N], NTT form; all heads share them), so that the
+ * scale stays.  inverse != 0 turns back (-S_j): the gradient.  Channels from 2*n_pairs on are not turned: their first `level` limbs
+ * are copied.  in: n_heads*head_dim ciphertexts; d_out uint64[n_heads*head_dim][2][level][N]. */
+typedef struct he_rope_desc {
+    uint32_t n_heads, head_dim, n_pairs, level;
+    uint32_t interleaved, inverse;
+} he_rope_desc;
+size_t he_rope_workspace_bytes(const ckks_ctx* ctx, const he_rope_desc* desc);
+int he_rope_axes(const ckks_ctx* ctx, const he_rope_desc* desc, const he_ct_array* in, const uint64_t* d_cos, const uint64_t* d_sin,
+                 uint64_t* d_out, void* d_ws, size_t ws_bytes, void* stream);
+
+/* Root-mean-square norm over the channels of every slot, with gate and residual, the inverse square root by Newton's method:
+ *   s = Rescale(Relin(sum_c x_c * x_c)) + k_eps                                 level-1, one relinearisation for all channels
+ *   r = Rescale(k_slope * s) + k_start                                          level-2, the first guess, linear in s
+ *   h_k_newton[i], i < iterations:  u = Rescale(Relin(r*r)), w = Rescale(Relin(s*r)), r = Rescale(Relin(u*w) + h_k_newton[i]*r)    two levels each
+ *   t_c = x_c,  or Rescale(G_c (.) x_c) (HE_GATE_PLAIN),  or Rescale(Relin(g_c * x_c)) (HE_GATE_CIPHER)        at the side of the chain: no depth
+ *   out_c = Rescale(Relin(t_c * r) + k_residual * res_c)                        level-3-2*iterations
+ * Relin and Rescale are one division by P*q each (as merged_division in he_poly_act_deg7).  The signed integers fold constants and scale
+ * ratios; the caller tracks scales.  A Newton step for 1/sqrt(v) is r(3 - v r^2)/2: with u*w = v r^3 taken as twice its scale and a k_newton that
+ * stands for -3/2, each iteration gives minus the step, so the guess's sign is chosen by the number of iterations.
+ * x: `channels` ciphertexts at `level` >= 3 + 2*iterations; gate: uint64[level+1][N] plaintexts ct_stride words apart (comp_stride unused) or
+ * ciphertexts; residual (d = NULL or the pointer NULL: none): ciphertexts of which limbs 0 .. level-2-2*iterations are read; both `channels` of
+ * them.  d_out uint64[channels][2][level-2-2*iterations][N]. */
+enum he_norm_gate_kind { HE_GATE_NONE = 0, HE_GATE_PLAIN = 1, HE_GATE_CIPHER = 2 };
+#define HE_NORM_MAX_ITERATIONS 16
+typedef struct he_norm_desc {
+    uint32_t channels, level, iterations;
+    uint32_t gate; /* he_norm_gate_kind */
+    int64_t k_eps, k_slope, k_start, k_residual;
+} he_norm_desc;
+size_t he_norm_workspace_bytes(const ckks_ctx* ctx, const he_norm_desc* desc);
+int he_norm_gate(const ckks_ctx* ctx, const he_norm_desc* desc, const int64_t* h_k_newton, const he_ct_array* x, const he_ct_array* gate,
+                 const he_ct_array* residual, const ckks_key* rlk, uint64_t* d_out, void* d_ws, size_t ws_bytes, void* stream);
+
 /* Self-test hook (not part of the paper's method): evaluates on the GPU the routines of the double-precision modular
  * arithmetic that the transforms, basis conversions and fused inner products are made of, for moduli q < 2^50, on
  * caller-given operands, so that a test can judge the device's results with wide integers.

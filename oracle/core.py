@@ -802,6 +802,91 @@ class Oracle:
                      self.scalar_mul(self.drop_to_level(x3, l3), self.scalar_residues(k3, l3), l3), l3)
         return self.ctct_mul_relin_rescale(self.drop_to_level(x4, l3), B, rlk, l3, addend=A)     # level-4
 
+    # -------------------------------------------------------- a transformer block's operators
+    def linear_grouped(self, x, level: int, group_rows: Sequence[int], weights, multiplier: int, bias=None) -> List[List[np.ndarray]]:
+        """Rows x[t] (lists of c_in ciphertexts [2][level+1][N]) of the groups in turn; weights[g] [c_out][c_in] integers; bias[g] [c_out][level+1] residues.
+        out[t][o] = Rescale( multiplier * sum_c weights[g][o][c] * x[t][c] + bias )."""
+        out, t = [], 0
+        for g, rows in enumerate(group_rows):
+            for _ in range(rows):
+                row = []
+                for o in range(len(weights[g])):
+                    acc = np.zeros((2, level + 1, self.N), dtype=np.uint64)
+                    for c, ct in enumerate(x[t]):
+                        acc = self.add(acc, self.scalar_mul(ct, self.scalar_residues(int(weights[g][o][c]) * int(multiplier), level), level), level)
+                    if bias is not None:
+                        for i in range(level + 1):
+                            acc[0, i] = (acc[0, i] + np.uint64(bias[g][o][i])) % np.uint64(self.moduli[i])
+                    row.append(self.rescale(acc, level))
+                out.append(row)
+                t += 1
+        return out
+
+    def negate(self, a, level: int) -> np.ndarray:
+        return self.scalar_mul(a, self.scalar_residues(-1, level), level)
+
+    def rope_axes(self, x, level: int, cos, sin, interleaved: bool = False, inverse: bool = False) -> List[np.ndarray]:
+        """One head's channel ciphertexts x[c]; cos, sin [pairs][level+1][N] in NTT form."""
+        idx, n_pairs = list(range(level + 1)), len(cos)
+        out = [self.drop_to_level(ct, level - 1) for ct in x]
+        for j in range(n_pairs):
+            a, b = (2 * j, 2 * j + 1) if interleaved else (j, j + n_pairs)
+            C_, S_ = _u64(cos[j]), _u64(sin[j])
+            if inverse:
+                S_ = self.negate(S_, level)
+            times = lambda ct, pt: np.stack([self.mul(ct[k], pt, idx) for k in range(2)])  # noqa: E731
+            out[a] = self.rescale(self.add(times(x[a], C_), self.negate(times(x[b], S_), level), level), level)
+            out[b] = self.rescale(self.add(times(x[a], S_), times(x[b], C_), level), level)
+        return out
+
+    def add_constant(self, ct, k: int, level: int) -> np.ndarray:
+        """The integer k in every slot: the constant polynomial, whose value is k at every evaluation point."""
+        out = _u64(ct).copy()
+        for i in range(level + 1):
+            out[0, i] = (out[0, i] + np.uint64(int(k) % self.moduli[i])) % np.uint64(self.moduli[i])
+        return out
+
+    def relin_rescale(self, d0, d1, d2, rlk, level: int) -> np.ndarray:
+        """((d0, d1) + KeySwitch(d2)) / q_level, one division by P q_level."""
+        L1 = level + 1
+        v = self.key_inner(self.modup(d2, level), rlk, level)
+        Pres = self.special_product_residues(level)[:L1]
+        out = []
+        for comp, dpart in enumerate((d0, d1)):
+            vc = v[comp].copy()
+            vc[:L1] = self.add(vc[:L1], self.scalar_mul(dpart, Pres, level), level)
+            out.append(self.moddown_rescale(vc, level))
+        return np.stack(out)
+
+    def norm_gate(self, x, level: int, k_eps: int, k_slope: int, k_start: int, k_newton: Sequence[int], rlk, gate=None, residual=None,
+                  k_residual: int = 0) -> List[np.ndarray]:
+        """x: channel ciphertexts [2][level+1][N]; gate: plaintexts [level+1][N] or ciphertexts; residual: ciphertexts of as many limbs or more."""
+        idx = list(range(level + 1))
+        d = [np.zeros((level + 1, self.N), dtype=np.uint64) for _ in range(3)]
+        for ct in x:
+            cross = self.mul(ct[0], ct[1], idx)
+            for i, term in enumerate((self.mul(ct[0], ct[0], idx), self.add(cross, cross, level), self.mul(ct[1], ct[1], idx))):
+                d[i] = self.add(d[i], term, level)
+        s = self.add_constant(self.relin_rescale(*d, rlk, level), k_eps, level - 1)
+        scaled = lambda ct, k, lv: self.scalar_mul(self.drop_to_level(ct, lv), self.scalar_residues(k, lv), lv)  # noqa: E731
+        r = self.add_constant(self.rescale(scaled(s, k_slope, level - 1), level - 1), k_start, level - 2)
+        m = level - 2
+        for k in k_newton:
+            u = self.ctct_mul_relin_rescale(r, r, rlk, m)
+            w = self.ctct_mul_relin_rescale(self.drop_to_level(s, m), r, rlk, m)
+            r = self.ctct_mul_relin_rescale(u, w, rlk, m - 1, addend=scaled(r, k, m - 1))
+            m -= 2
+        out = []
+        for c, ct in enumerate(x):
+            t = _u64(ct)
+            if gate is not None and np.ndim(gate[c]) == 2:
+                t = self.rescale(np.stack([self.mul(t[i], gate[c], idx) for i in range(2)]), level)
+            elif gate is not None:
+                t = self.ctct_mul_relin_rescale(t, gate[c], rlk, level)
+            add = scaled(residual[c], k_residual, m) if residual is not None else None
+            out.append(self.ctct_mul_relin_rescale(self.drop_to_level(t, m), r, rlk, m, addend=add))
+        return out
+
     # ------------------------------------------------------------------ fully connected layer
     @staticmethod
     def fc_shifts(d_in: int, d_out: int, batch: int, base: int):

@@ -9,6 +9,7 @@ the compiled library is missing the import of this module fails.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from typing import List, Optional, Sequence
 
@@ -38,6 +39,13 @@ HE_CONV_DEFERRED_MODDOWN = 2
 HE_CONV_DEFERRED_MERGED = 3
 HE_RELAYOUT_DIRECT = 0
 HE_RELAYOUT_DEFERRED = 1
+HE_WEIGHT_INT8 = 1
+HE_WEIGHT_INT16 = 2
+HE_WEIGHT_INT32 = 4
+HE_GATE_NONE = 0
+HE_GATE_PLAIN = 1
+HE_GATE_CIPHER = 2
+HE_NORM_MAX_ITERATIONS = 16
 
 EXPORTS = (
     "ckks_ctx_create", "ckks_ctx_destroy", "ckks_last_error_string", "ckks_workspace_bytes",
@@ -46,6 +54,7 @@ EXPORTS = (
     "he_conv_workspace_bytes", "he_conv_batched", "he_conv_check_weights", "he_poly_act_deg7", "ckks_f64mod_probe",
     "he_accumulator_workspace_bytes", "he_accumulator_merge", "he_fc_workspace_bytes", "he_fc_batched",
     "he_relayout_workspace_bytes", "he_relayout_two_rotations", "ckks_key_expand_a", "ckks_keyset_stage", "ckks_ctx_set_overlap",
+    "he_linear_workspace_bytes", "he_linear_grouped", "he_rope_workspace_bytes", "he_rope_axes", "he_norm_workspace_bytes", "he_norm_gate",
     "ckks_prof_kernel_count", "ckks_prof_kernel_name", "ckks_prof_begin", "ckks_prof_end",
 )
 
@@ -70,6 +79,25 @@ class _ConvDesc(C.Structure):
 
 class _FcDesc(C.Structure):
     _fields_ = [("d_in", C.c_uint32), ("d_out", C.c_uint32), ("batch", C.c_uint32), ("level", C.c_uint32), ("base", C.c_uint32)]
+
+
+class _CtArray(C.Structure):
+    _fields_ = [("d", C.c_void_p), ("ct_stride", C.c_uint64), ("comp_stride", C.c_uint64)]
+
+
+class _LinearDesc(C.Structure):
+    _fields_ = [("c_in", C.c_uint32), ("c_out", C.c_uint32), ("n_groups", C.c_uint32), ("level", C.c_uint32), ("weight_type", C.c_uint32),
+                ("transposed", C.c_uint32), ("multiplier", C.c_uint64)]
+
+
+class _RopeDesc(C.Structure):
+    _fields_ = [("n_heads", C.c_uint32), ("head_dim", C.c_uint32), ("n_pairs", C.c_uint32), ("level", C.c_uint32),
+                ("interleaved", C.c_uint32), ("inverse", C.c_uint32)]
+
+
+class _NormDesc(C.Structure):
+    _fields_ = [("channels", C.c_uint32), ("level", C.c_uint32), ("iterations", C.c_uint32), ("gate", C.c_uint32), ("k_eps", C.c_int64),
+                ("k_slope", C.c_int64), ("k_start", C.c_int64), ("k_residual", C.c_int64)]
 
 
 def _bind(path: str):
@@ -117,6 +145,16 @@ def _bind(path: str):
     lib.ckks_ctx_set_overlap.argtypes = [vp, i32]
     lib.ckks_key_expand_a.argtypes = [vp, C.c_uint64, vp, vp]
     lib.ckks_keyset_stage.argtypes = [vp, C.POINTER(vp), C.POINTER(C.c_uint64), C.POINTER(vp), u32, vp]
+    arr = C.POINTER(_CtArray)
+    lib.he_linear_workspace_bytes.argtypes = [vp, C.POINTER(_LinearDesc), C.POINTER(u32)]
+    lib.he_linear_workspace_bytes.restype = sz
+    lib.he_linear_grouped.argtypes = [vp, C.POINTER(_LinearDesc), C.POINTER(u32), arr, vp, vp, vp, vp, sz, vp]
+    lib.he_rope_workspace_bytes.argtypes = [vp, C.POINTER(_RopeDesc)]
+    lib.he_rope_workspace_bytes.restype = sz
+    lib.he_rope_axes.argtypes = [vp, C.POINTER(_RopeDesc), arr, vp, vp, vp, vp, sz, vp]
+    lib.he_norm_workspace_bytes.argtypes = [vp, C.POINTER(_NormDesc)]
+    lib.he_norm_workspace_bytes.restype = sz
+    lib.he_norm_gate.argtypes = [vp, C.POINTER(_NormDesc), C.POINTER(C.c_int64), arr, arr, arr, vp, vp, vp, sz, vp]
     lib.ckks_prof_kernel_count.restype = u32
     lib.ckks_prof_kernel_name.argtypes = [u32]
     lib.ckks_prof_kernel_name.restype = C.c_char_p
@@ -572,6 +610,128 @@ def he_fc_batched(ctx: Context, ct: torch.Tensor, level: int, d_in: int, d_out: 
     ctx._check(_lib.he_fc_batched(ctx.handle, C.byref(_FcDesc(d_in, d_out, batch, level, base)), _ptr(ct), _ptr(w_enc), arr(sum_keys),
                                   arr(merge_keys), _ptr(merge_mask), _ptr(place_masks), arr(lo_keys), arr(hi_keys), _ptr(bias),
                                   _ptr(out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+    return out
+
+
+# ------------------------------------------------------------------ a transformer block's operators
+_WEIGHT_TYPES = {torch.int8: HE_WEIGHT_INT8, torch.int16: HE_WEIGHT_INT16, torch.int32: HE_WEIGHT_INT32}
+
+
+def _ct_array(ctx: Context, t: torch.Tensor, n: int, limbs: int, what: str, plain: bool = False) -> _CtArray:
+    """A tensor [..., 2, limbs or more, N] (plain: [..., limbs or more, N]) of n ciphertexts as the library takes it: limbs N apart, the ciphertexts at
+    equal distances; it may be a view into a larger tensor."""
+    tail = 2 if plain else 3
+    if t.device.type != _expect_device or t.dtype not in (torch.int64, torch.uint64):
+        raise ValueError(f"{what}: need an int64 tensor on {_expect_device}")
+    if t.dim() < tail or t.shape[-1] != ctx.N or t.shape[-2] < limbs or (not plain and t.shape[-3] != 2) or math.prod(t.shape[:-tail]) != n:
+        raise ValueError(f"{what}: need {n} {'plaintexts [limbs][N]' if plain else 'ciphertexts [2][limbs][N]'} of at least {limbs} limbs, got {tuple(t.shape)}")
+    if t.stride(-1) != 1 or (t.shape[-2] > 1 and t.stride(-2) != ctx.N):
+        raise ValueError(f"{what}: the limbs have to be N = {ctx.N} words apart")
+    step = 0
+    for size, stride in zip(reversed(t.shape[:-tail]), reversed(t.stride()[:-tail])):  # the leading dimensions have to be one
+        if size > 1:
+            if step and stride != step[0] * step[1]:
+                raise ValueError(f"{what}: the ciphertexts have to be at equal distances")
+            step = (step[0], step[1] * size) if step else (stride, size)
+    return _CtArray(t.data_ptr(), step[0] if step else 0, 0 if plain else t.stride(-3))
+
+
+def _out(ctx: Context, out: Optional[torch.Tensor], *shape) -> torch.Tensor:
+    if out is None:
+        return empty(*[max(n, 1) if i >= len(shape) - 3 else n for i, n in enumerate(shape)])
+    if out.numel() != math.prod(shape):
+        raise ValueError(f"out must be {list(shape)}")
+    return out
+
+
+def _linear_desc(ctx, level, group_rows, c_in, c_out, dtype, transposed, multiplier):
+    if dtype not in _WEIGHT_TYPES:
+        raise ValueError("weights must be int8, int16 or int32")
+    rows = [int(r) for r in group_rows]
+    if any(r < 0 for r in rows):
+        raise ValueError("negative row count")
+    if not 0 < int(multiplier) < 1 << 64:
+        raise ValueError("multiplier must be a positive integer below 2^64")
+    return _LinearDesc(c_in, c_out, len(rows), level, _WEIGHT_TYPES[dtype], int(bool(transposed)), int(multiplier)), (C.c_uint32 * len(rows))(*rows)
+
+
+def he_linear_workspace_bytes(ctx: Context, level: int, group_rows: Sequence[int], c_in: int, c_out: int, dtype: torch.dtype = torch.int32) -> int:
+    d, rows = _linear_desc(ctx, level, group_rows, c_in, c_out, dtype, False, 1)
+    return int(_lib.he_linear_workspace_bytes(ctx.handle, C.byref(d), rows))
+
+
+def he_linear_grouped(ctx: Context, level: int, group_rows: Sequence[int], x: torch.Tensor, w: torch.Tensor, multiplier: int,
+                      bias: Optional[torch.Tensor] = None, transposed: bool = False, out: Optional[torch.Tensor] = None,
+                      ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """x: [rows][c_in][2][level+1 or more][N], the rows of group 0, then of group 1, ...; w: [groups][c_out][c_in] (transposed:
+    [groups][c_in][c_out]) int8, int16 or int32; bias: [groups][c_out][level+1] residues or None.  Returns [rows][c_out][2][level][N]."""
+    if w.dim() != 3 or w.shape[0] != len(group_rows) or x.dim() != 5:
+        raise ValueError("need w [groups][c_out][c_in] and x [rows][c_in][2][limbs][N]")
+    if w.device.type != _expect_device or not w.is_contiguous():
+        raise ValueError(f"w must be contiguous, on {_expect_device}")
+    c_in, c_out = (w.shape[1], w.shape[2]) if transposed else (w.shape[2], w.shape[1])
+    d, rows = _linear_desc(ctx, level, group_rows, c_in, c_out, w.dtype, transposed, multiplier)
+    total = sum(rows)
+    if x.shape[0] != total or x.shape[1] != c_in:
+        raise ValueError(f"x must be [{total}][{c_in}][2][limbs][N]")
+    if bias is not None and bias.numel() != len(rows) * c_out * (level + 1):
+        raise ValueError("bias must be [groups][c_out][level+1]")
+    out = _out(ctx, out, total, c_out, 2, level, ctx.N)
+    arr = _ct_array(ctx, x, total * c_in, level + 1, "x")
+    ws = _ws(ctx, ws, he_linear_workspace_bytes(ctx, level, group_rows, c_in, c_out, w.dtype))
+    ctx._check(_lib.he_linear_grouped(ctx.handle, C.byref(d), rows, C.byref(arr), w.data_ptr(), _ptr(bias), _ptr(out), _ptr(ws),
+                                      ws.numel() * ws.element_size(), _stream(stream)))
+    return out
+
+
+def he_rope_workspace_bytes(ctx: Context, level: int, n_heads: int, head_dim: int, n_pairs: int) -> int:
+    d = _RopeDesc(n_heads, head_dim, n_pairs, level, 0, 0)
+    return int(_lib.he_rope_workspace_bytes(ctx.handle, C.byref(d)))
+
+
+def he_rope_axes(ctx: Context, level: int, x: torch.Tensor, cos: torch.Tensor, sin: torch.Tensor, interleaved: bool = False,
+                 inverse: bool = False, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """x: [heads][head_dim][2][level+1 or more][N]; cos, sin: [pairs][level+1][N], encoded at the scale of q_level (``rope_angles`` in
+    ``block.py`` gives the angles of every slot).  Returns [heads][head_dim][2][level][N]."""
+    if x.dim() != 5 or cos.dim() != 3 or cos.shape != sin.shape or (cos.numel() and tuple(cos.shape[1:]) != (level + 1, ctx.N)):
+        raise ValueError("need x [heads][head_dim][2][limbs][N] and cos, sin [pairs][level+1][N]")
+    heads, head_dim, n_pairs = x.shape[0], x.shape[1], cos.shape[0]
+    d = _RopeDesc(heads, head_dim, n_pairs, level, int(bool(interleaved)), int(bool(inverse)))
+    out = _out(ctx, out, heads, head_dim, 2, level, ctx.N)
+    arr = _ct_array(ctx, x, heads * head_dim, level + 1, "x")
+    ws = _ws(ctx, ws, he_rope_workspace_bytes(ctx, level, heads, head_dim, n_pairs))
+    ctx._check(_lib.he_rope_axes(ctx.handle, C.byref(d), C.byref(arr), _ptr(cos), _ptr(sin), _ptr(out), _ptr(ws), ws.numel() * ws.element_size(),
+                                 _stream(stream)))
+    return out
+
+
+def he_norm_workspace_bytes(ctx: Context, level: int, channels: int, iterations: int, gate: int = HE_GATE_NONE) -> int:
+    d = _NormDesc(channels, level, iterations, gate, 0, 0, 0, 0)
+    return int(_lib.he_norm_workspace_bytes(ctx.handle, C.byref(d)))
+
+
+def he_norm_gate(ctx: Context, level: int, x: torch.Tensor, k_eps: int, k_slope: int, k_start: int, k_newton: Sequence[int], rlk: Key,
+                 gate: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, k_residual: int = 0,
+                 out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """x: [channels][2][level+1 or more][N]; gate: None, plaintexts [channels][level+1 or more][N] or ciphertexts [channels][2][level+1 or
+    more][N]; residual: None or [channels][2][level-1-2*iterations or more][N]; the integers as ``norm_constants`` in ``block.py`` gives
+    them.  Returns [channels][2][level-2-2*iterations][N]."""
+    if x.dim() != 4:
+        raise ValueError("need x [channels][2][limbs][N]")
+    channels, its, limbs = x.shape[0], len(k_newton), level + 1
+    if any(not -(1 << 63) <= int(k) < 1 << 63 for k in (k_eps, k_slope, k_start, k_residual, *k_newton)):
+        raise ValueError("the constants must be 64-bit signed integers")
+    kind = HE_GATE_NONE if gate is None else (HE_GATE_CIPHER if gate.dim() == 4 else HE_GATE_PLAIN)
+    last = level - 2 - 2 * its
+    d = _NormDesc(channels, level, its, kind, int(k_eps), int(k_slope), int(k_start), int(k_residual))
+    kn = (C.c_int64 * max(its, 1))(*[int(k) for k in k_newton])
+    out = _out(ctx, out, channels, 2, last, ctx.N) if last > 0 or out is None else out
+    xa = _ct_array(ctx, x, channels, limbs, "x")
+    ga = _ct_array(ctx, gate, channels, limbs, "gate", plain=kind == HE_GATE_PLAIN) if kind else None
+    ra = _ct_array(ctx, residual, channels, max(last, 0) + 1, "residual") if residual is not None else None
+    ws = _ws(ctx, ws, he_norm_workspace_bytes(ctx, level, channels, its, kind))
+    ctx._check(_lib.he_norm_gate(ctx.handle, C.byref(d), kn, C.byref(xa), C.byref(ga) if ga else None, C.byref(ra) if ra else None,
+                                 rlk.handle if rlk else None, _ptr(out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
     return out
 
 

@@ -2033,6 +2033,317 @@ int he_poly_act_deg7(const ckks_ctx* c, const uint64_t* const* h_d_x, uint32_t n
     return join(CKKS_OK);
 }
 
+// ---- a transformer block's operators ---------------------------------------------------------------------
+// Checks of a vector of n ciphertexts of which `limbs` limbs of n_comp components are read: what the kernels' 16-byte loads and indexes assume.
+static int check_array(const ckks_ctx* c, const he_ct_array* a, size_t n, u32 limbs, u32 n_comp) {
+    if (!a || !a->d) return set_err(c, CKKS_ERR_INVALID_ARG, "null ciphertext array");
+    const u64 one = (u64)limbs * c->N, most = (u64)1 << 40;  // 2^40 words: no product of a stride and a count overflows
+    if (((uintptr_t)a->d & 15) || (a->ct_stride & 1) || (n_comp > 1 && (a->comp_stride & 1)))
+        return set_err(c, CKKS_ERR_INVALID_ARG, "ciphertext array: not aligned to 16 bytes, or an odd stride");
+    if (a->ct_stride > most || (n_comp > 1 && a->comp_stride > most)) return set_err(c, CKKS_ERR_INVALID_ARG, "ciphertext array: stride out of range");
+    if (n_comp > 1 && a->comp_stride < one) return set_err(c, CKKS_ERR_INVALID_ARG, "ciphertext array: components overlap");
+    if (n > 1 && a->ct_stride != 0 && a->ct_stride < (n_comp > 1 ? a->comp_stride : 0) + one) return set_err(c, CKKS_ERR_INVALID_ARG, "ciphertext array: ciphertexts overlap");
+    return CKKS_OK;
+}
+
+static LimbScalars limb_scalars(const ckks_ctx* c, u32 level, int64_t k) {
+    LimbScalars s;
+    for (u32 i = 0; i < CKKS_MAX_MODULI; i++) {
+        const u64 q = i <= level ? c->mod[i] : 1, mag = k >= 0 ? (u64)k : 0 - (u64)k;
+        s.v[i] = k >= 0 ? mag % q : (q - mag % q) % q;
+    }
+    return s;
+}
+
+// Ciphertexts whose sums are in the workspace at a time: of a row's c_out outputs as many as 2 GiB hold, then further rows
+#define LINEAR_SUMS_BYTES ((size_t)2 << 30)
+struct LinearPlan {
+    u64 rows;      // in all
+    u32 outs;      // outputs of a row at a time
+    u32 row_step;  // rows at a time
+};
+static int linear_plan(const ckks_ctx* c, const he_linear_desc* d, const u32* h_rows, LinearPlan* p) {
+    if (!d || !h_rows) return set_err(c, CKKS_ERR_INVALID_ARG, "null descriptor or row counts");
+    if (d->c_in == 0 || d->c_out == 0 || d->n_groups == 0 || d->c_in > 65536 || d->c_out > 65536)
+        return set_err(c, CKKS_ERR_INVALID_ARG, "channels out of range (1 to 65536), or no groups");
+    if (d->weight_type != HE_WEIGHT_INT8 && d->weight_type != HE_WEIGHT_INT16 && d->weight_type != HE_WEIGHT_INT32)
+        return set_err(c, CKKS_ERR_INVALID_ARG, "unknown weight type");
+    if (d->multiplier == 0) return set_err(c, CKKS_ERR_INVALID_ARG, "multiplier is zero");
+    if (!level_ok(c, d->level) || d->level < 1) return set_err(c, CKKS_ERR_LEVEL_MISMATCH, "grouped product needs 1 <= level < num_q");
+    p->rows = 0;
+    u32 most = 0;
+    for (u32 g = 0; g < d->n_groups; g++) {
+        p->rows += h_rows[g];
+        if (h_rows[g] > most) most = h_rows[g];
+    }
+    if (p->rows > (u64)1 << 24) return set_err(c, CKKS_ERR_INVALID_ARG, "too many rows");
+    const size_t fit = LINEAR_SUMS_BYTES / ((size_t)(d->level + 1) * c->N * 16);
+    const u32 cap = fit < CT_BATCH ? CT_BATCH : (fit > 65536 ? 65536 : (u32)fit);
+    p->outs = d->c_out < cap ? d->c_out : cap;
+    p->row_step = cap / p->outs;
+    if (p->row_step > most) p->row_step = most;
+    if (p->row_step == 0) p->row_step = 1;
+    return CKKS_OK;
+}
+static size_t ws_linear(const ckks_ctx* c, const he_linear_desc* d, const LinearPlan& p) {
+    return blk((size_t)p.row_step * p.outs * 2 * (d->level + 1) * c->N) + ws_rescale(c, d->level, CT_BATCH);
+}
+
+size_t he_linear_workspace_bytes(const ckks_ctx* c, const he_linear_desc* d, const uint32_t* h_group_rows) {
+    LinearPlan p;
+    if (!c || linear_plan(c, d, h_group_rows, &p)) return 0;
+    return ws_linear(c, d, p);
+}
+
+int he_linear_grouped(const ckks_ctx* c, const he_linear_desc* d, const uint32_t* h_group_rows, const he_ct_array* in, const void* d_w,
+                      const uint64_t* d_bias, uint64_t* d_out, void* d_ws, size_t ws_bytes, void* stream) {
+    if (!c) return CKKS_ERR_INVALID_ARG;
+    LinearPlan p;
+    if (int rc = linear_plan(c, d, h_group_rows, &p)) return rc;
+    if (p.rows == 0) return CKKS_OK;
+    if (!d_w || !d_out) return set_err(c, CKKS_ERR_INVALID_ARG, "null pointer");
+    if (((uintptr_t)d_out & 15) || ((uintptr_t)d_w & (d->weight_type - 1))) return set_err(c, CKKS_ERR_INVALID_ARG, "weights or output not aligned");
+    const u32 level = d->level, L1 = level + 1;
+    if (int rc = check_array(c, in, p.rows * d->c_in, L1, 2)) return rc;
+    if (!d_ws || ws_bytes < ws_linear(c, d, p)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the grouped product");
+    hipStream_t st = (hipStream_t)stream;
+    const size_t N = c->N, ct = (size_t)2 * L1 * N, out_ct = (size_t)2 * level * N;
+    Arena ar(d_ws, ws_bytes);
+    u64* sums = ar.take((size_t)p.row_step * p.outs * ct);
+    LimbScalars mult;
+    for (u32 i = 0; i < CKKS_MAX_MODULI; i++) mult.v[i] = i <= level ? d->multiplier % c->mod[i] : 0;
+    const size_t w_group = (size_t)d->c_in * d->c_out, w_out = d->transposed ? 1 : d->c_in, w_in = d->transposed ? d->c_out : 1;
+    u64 t0 = 0;
+    for (u32 g = 0; g < d->n_groups; t0 += h_group_rows[g], g++) {
+        for (u32 o0 = 0; o0 < d->c_out; o0 += p.outs) {
+            const u32 no = d->c_out - o0 < p.outs ? d->c_out - o0 : p.outs;
+            const char* w = (const char*)d_w + (g * w_group + o0 * w_out) * d->weight_type;
+            const u64* bias = d_bias ? (const u64*)d_bias + ((size_t)g * d->c_out + o0) * L1 : nullptr;
+            for (u32 r0 = 0; r0 < h_group_rows[g]; r0 += p.row_step) {
+                const u32 nr = h_group_rows[g] - r0 < p.row_step ? h_group_rows[g] - r0 : p.row_step;
+                HIP_TRY(launch_linear_sum(c, level, nr, (const u64*)in->d + (t0 + r0) * d->c_in * in->ct_stride, in->ct_stride, in->comp_stride, d->c_in, no,
+                                          w, d->weight_type, w_out, w_in, bias, mult, sums, st));
+                for (u32 i0 = 0; i0 < nr * no; i0 += CT_BATCH) {
+                    const u32 n = nr * no - i0 < CT_BATCH ? nr * no - i0 : CT_BATCH;
+                    const u64* src[CT_BATCH];
+                    u64* dst[CT_BATCH];
+                    for (u32 b = 0; b < n; b++) {
+                        const u32 i = i0 + b;
+                        src[b] = sums + i * ct;
+                        dst[b] = (u64*)d_out + ((t0 + r0 + i / no) * d->c_out + o0 + i % no) * out_ct;
+                    }
+                    if (int rc = run_rescale(c, level, src, (size_t)L1 * N, dst, n, ar.rest(), st)) return rc;
+                }
+            }
+        }
+    }
+    return CKKS_OK;
+}
+
+static int rope_check(const ckks_ctx* c, const he_rope_desc* d) {
+    if (!d) return set_err(c, CKKS_ERR_INVALID_ARG, "null descriptor");
+    if (d->n_heads == 0 || d->head_dim == 0 || d->n_heads > 65536 || d->head_dim > 65536 || d->n_pairs > d->head_dim / 2)
+        return set_err(c, CKKS_ERR_INVALID_ARG, "heads, channels or pairs out of range");
+    if (!level_ok(c, d->level) || d->level < 1) return set_err(c, CKKS_ERR_LEVEL_MISMATCH, "rotary positions need 1 <= level < num_q");
+    return CKKS_OK;
+}
+#define ROPE_BATCH (CT_BATCH / 2)  // pairs whose sums are rescaled together
+size_t he_rope_workspace_bytes(const ckks_ctx* c, const he_rope_desc* d) {
+    if (!c || rope_check(c, d)) return 0;
+    return blk((size_t)2 * ROPE_BATCH * 2 * (d->level + 1) * c->N) + ws_rescale(c, d->level, 2 * ROPE_BATCH);
+}
+
+int he_rope_axes(const ckks_ctx* c, const he_rope_desc* d, const he_ct_array* in, const uint64_t* d_cos, const uint64_t* d_sin,
+                 uint64_t* d_out, void* d_ws, size_t ws_bytes, void* stream) {
+    if (!c) return CKKS_ERR_INVALID_ARG;
+    if (int rc = rope_check(c, d)) return rc;
+    if (!d_out || (d->n_pairs && (!d_cos || !d_sin))) return set_err(c, CKKS_ERR_INVALID_ARG, "null pointer");
+    if (((uintptr_t)d_out | (uintptr_t)d_cos | (uintptr_t)d_sin) & 15) return set_err(c, CKKS_ERR_INVALID_ARG, "tables or output not aligned to 16 bytes");
+    const u32 level = d->level, L1 = level + 1;
+    if (int rc = check_array(c, in, (size_t)d->n_heads * d->head_dim, L1, 2)) return rc;
+    if (!d_ws || ws_bytes < he_rope_workspace_bytes(c, d)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the rotary positions");
+    hipStream_t st = (hipStream_t)stream;
+    const size_t N = c->N, ct = (size_t)2 * L1 * N, out_ct = (size_t)2 * level * N;
+    Arena ar(d_ws, ws_bytes);
+    u64* y = ar.take((size_t)2 * ROPE_BATCH * ct);
+    RopePairs P = {d->head_dim, d->n_pairs, d->interleaved ? 1u : 0u, d->inverse ? 1u : 0u, 0};
+    const u64 pairs = (u64)d->n_heads * d->n_pairs, rest = (u64)d->n_heads * (d->head_dim - 2 * d->n_pairs);
+    if (pairs >> 32 || rest >> 32) return set_err(c, CKKS_ERR_INVALID_ARG, "too many channels");
+    for (u64 z0 = 0; z0 < pairs; z0 += ROPE_BATCH) {
+        const u32 n = pairs - z0 < ROPE_BATCH ? (u32)(pairs - z0) : ROPE_BATCH;
+        P.z0 = (u32)z0;
+        HIP_TRY(launch_rope_turn(c, level, n, (const u64*)in->d, in->ct_stride, in->comp_stride, P, (const u64*)d_cos, (const u64*)d_sin, y, st));
+        const u64* src[2 * ROPE_BATCH];
+        u64* dst[2 * ROPE_BATCH];
+        for (u32 b = 0; b < n; b++) {
+            const u64 head = (z0 + b) / d->n_pairs * d->head_dim;
+            const u32 j = (u32)((z0 + b) % d->n_pairs);
+            src[2 * b] = y + 2 * b * ct;
+            src[2 * b + 1] = y + (2 * b + 1) * ct;
+            dst[2 * b] = (u64*)d_out + (head + P.first(j)) * out_ct;
+            dst[2 * b + 1] = (u64*)d_out + (head + P.second(j)) * out_ct;
+        }
+        if (int rc = run_rescale(c, level, src, (size_t)L1 * N, dst, 2 * n, ar.rest(), st)) return rc;
+    }
+    for (u64 z0 = 0; z0 < rest; z0 += 65535) {  // the launch's third dimension holds 65535 workgroups
+        P.z0 = (u32)z0;
+        HIP_TRY(launch_rope_pass(c, level, rest - z0 < 65535 ? (u32)(rest - z0) : 65535, (const u64*)in->d, in->ct_stride, in->comp_stride, P, (u64*)d_out, st));
+    }
+    return CKKS_OK;
+}
+
+static int norm_check(const ckks_ctx* c, const he_norm_desc* d) {
+    if (!d) return set_err(c, CKKS_ERR_INVALID_ARG, "null descriptor");
+    if (d->channels == 0 || d->channels > 65536) return set_err(c, CKKS_ERR_INVALID_ARG, "channels out of range (1 to 65536)");
+    if (d->iterations > HE_NORM_MAX_ITERATIONS) return set_err(c, CKKS_ERR_INVALID_ARG, "too many iterations");
+    if (d->gate > HE_GATE_CIPHER) return set_err(c, CKKS_ERR_INVALID_ARG, "unknown gate kind");
+    if (!c->dnum) return set_err(c, CKKS_ERR_UNSUPPORTED_PARAMS, "context has no key-switching digits");
+    if (!level_ok(c, d->level) || d->level < 3 + 2 * d->iterations) return set_err(c, CKKS_ERR_LEVEL_MISMATCH, "norm needs 3 + 2 iterations <= level < num_q");
+    return CKKS_OK;
+}
+// channels of a batch of products with the norm's factor
+static u32 norm_batch(const ckks_ctx* c, const he_norm_desc* d) {
+    const u32 most = ks_batch(c);
+    return d->channels < most ? d->channels : most;
+}
+static size_t ws_norm(const ckks_ctx* c, const he_norm_desc* d) {
+    const size_t N = c->N, L1 = d->level + 1, nb = norm_batch(c, d), last = d->level - 2 - 2 * d->iterations;
+    size_t sub = ws_ks(c, d->level, 1, 1), t;
+    if ((t = ws_rescale(c, d->level, CT_BATCH)) > sub) sub = t;
+    if (d->iterations && (t = ws_ctct(c, d->level - 2, 2)) > sub) sub = t;
+    if ((t = ws_ctct(c, (u32)last, (u32)nb)) > sub) sub = t;
+    if (d->gate == HE_GATE_CIPHER && (t = ws_ctct(c, d->level, (u32)nb)) > sub) sub = t;
+    return blk(3 * L1 * N) + 2 * blk(2 * L1 * N) + blk(2 * N * d->level) + 2 * blk(2 * N * d->level) +
+           (d->gate ? blk(nb * 2 * d->level * N) : 0) + (d->gate == HE_GATE_PLAIN || !ntt_has_modup(c) ? blk(nb * 2 * L1 * N) : 0) + sub;
+}
+size_t he_norm_workspace_bytes(const ckks_ctx* c, const he_norm_desc* d) {
+    if (!c || norm_check(c, d)) return 0;
+    return ws_norm(c, d);
+}
+
+int he_norm_gate(const ckks_ctx* c, const he_norm_desc* d, const int64_t* h_k_newton, const he_ct_array* x, const he_ct_array* gate,
+                 const he_ct_array* residual, const ckks_key* rlk, uint64_t* d_out, void* d_ws, size_t ws_bytes, void* stream) {
+    if (!c) return CKKS_ERR_INVALID_ARG;
+    if (int rc = norm_check(c, d)) return rc;
+    if (!d_out || (d->iterations && !h_k_newton)) return set_err(c, CKKS_ERR_INVALID_ARG, "null pointer");
+    if ((uintptr_t)d_out & 15) return set_err(c, CKKS_ERR_INVALID_ARG, "output not aligned to 16 bytes");
+    if (!rlk) return set_err(c, CKKS_ERR_NO_KEY, "no relinearisation key");
+    if (rlk->galois_elt != 0) return set_err(c, CKKS_ERR_NO_KEY, "key is a rotation key, not the relinearisation key");
+    const u32 level = d->level, last = level - 2 - 2 * d->iterations;
+    if (int rc = check_array(c, x, d->channels, level + 1, 2)) return rc;
+    if (d->gate)
+        if (int rc = check_array(c, gate, d->channels, level + 1, d->gate == HE_GATE_CIPHER ? 2 : 1)) return rc;
+    const bool add = residual && residual->d;
+    if (add)
+        if (int rc = check_array(c, residual, d->channels, last + 1, 2)) return rc;
+    if (!d_ws || ws_bytes < ws_norm(c, d)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
+    hipStream_t st = (hipStream_t)stream;
+    const bool mac = ntt_has_modup(c);
+    const size_t N = c->N, L1 = level + 1;
+    const u32 nb = norm_batch(c, d);
+    Arena ar(d_ws, ws_bytes);
+    u64* sq3 = ar.take(3 * L1 * N);             // the three polynomials of the sum of squares
+    u64* ra = ar.take(2 * L1 * N);              // the guess before and after its iterations, in turn
+    u64* rb = ar.take(2 * L1 * N);
+    u64* s = ar.take(2 * N * level);            // level - 1
+    u64* u = ar.take(2 * N * level);
+    u64* w = ar.take(2 * N * level);
+    u64* t = d->gate ? ar.take(nb * 2 * level * N) : nullptr;
+    u64* tmp = d->gate == HE_GATE_PLAIN || !mac ? ar.take(nb * 2 * L1 * N) : nullptr;
+    if (!ar.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
+    int rc;
+
+    // s: a constant k joins a quotient by B exactly as B k joins the dividend (it vanishes modulo every dropped limb), and the addends of the
+    // inner product are multiplied by P already
+    auto times_limb = [&](int64_t k, u32 lv) {
+        LimbScalars v = limb_scalars(c, lv, k);
+        for (u32 i = 0; i <= lv; i++) v.v[i] = (u64)((unsigned __int128)v.v[i] * (c->mod[lv] % c->mod[i]) % c->mod[i]);
+        return v;
+    };
+    HIP_TRY(launch_square_sum(c, level, (const u64*)x->d, x->ct_stride, x->comp_stride, d->channels, times_limb(d->k_eps, level), sq3, st));
+    {
+        KsWs ws;
+        Arena sub = ar.rest();
+        if (!carve_ks(c, level, 1, 1, sub, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
+        const u64 *d0 = sq3, *d1 = sq3 + L1 * N, *d2 = sq3 + 2 * L1 * N;
+        u64* v = ws.v;
+        if ((rc = run_modup(c, level, &d2, 1, ws, st))) return rc;
+        HIP_TRY(launch_key_inner_ext(c, level, dsrc(c, ws, 0), rlk->d_key, 1, &d0, &d1, nullptr, &v, 1, st));
+        const FinalItem item = {nullptr, nullptr, nullptr, s, 1, 0, nullptr};
+        if ((rc = run_moddown(c, level, ws, 1, &item, st, true))) return rc;
+    }
+    // the first guess
+    const size_t ss = (size_t)level * N;  // component stride of s
+    HIP_TRY(launch_affine(c, level - 1, s, ss, limb_scalars(c, level - 1, d->k_slope), times_limb(d->k_start, level - 1), rb, st));
+    const u64* prb = rb;
+    if ((rc = run_rescale(c, level - 1, &prb, ss, &ra, 1, ar.rest(), st))) return rc;
+    // Newton's iterations, r at level m
+    u32 m = level - 2;
+    for (u32 it = 0; it < d->iterations; it++, m -= 2) {
+        const size_t rs = (size_t)(m + 1) * N, us = (size_t)m * N;
+        const u64 *pr = ra, *ps = s, *pu = u, *pw = w;
+        if (mac) {  // r r and r s side by side
+            const u64 *pa[2] = {ra, ra}, *pb0[2] = {ra, s}, *pb1[2] = {ra + rs, s + ss};
+            u64* po[2] = {u, w};
+            KsWs ws;
+            Arena sub = ar.rest();
+            if (!carve_ks(c, m, 2, 2, sub, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
+            if ((rc = run_product(c, m, pa, rs, pb0, pb1, rlk->d_key, po, 2, ws, st, true))) return rc;
+            const LimbScalars kn = limb_scalars(c, m - 1, h_k_newton[it]), zero = limb_scalars(c, m - 1, 0);
+            const LinAddend lin = {&pr, rs, kn.v, &pr, rs, zero.v};
+            if ((rc = run_ctct_merged(c, m - 1, &pu, us, &pw, us, nullptr, 0, rlk->d_key, &rb, 1, ar.rest(), st, &lin))) return rc;
+        } else {
+            if ((rc = run_ctct_merged(c, m, &pr, rs, &pr, rs, nullptr, 0, rlk->d_key, &u, 1, ar.rest(), st))) return rc;
+            if ((rc = run_ctct_merged(c, m, &pr, rs, &ps, ss, nullptr, 0, rlk->d_key, &w, 1, ar.rest(), st))) return rc;
+            HIP_TRY(launch_affine(c, m - 1, ra, rs, limb_scalars(c, m - 1, h_k_newton[it]), limb_scalars(c, m - 1, 0), tmp, st));
+            if ((rc = run_ctct_merged(c, m - 1, &pu, us, &pw, us, tmp, 0, rlk->d_key, &rb, 1, ar.rest(), st))) return rc;
+        }
+        u64* other = ra;
+        ra = rb;
+        rb = other;
+    }
+    // the channels, in batches
+    const size_t rs = (size_t)(last + 1) * N, out_ct = (size_t)2 * last * N;
+    const LimbScalars kr = limb_scalars(c, last, d->k_residual), zero = limb_scalars(c, last, 0);
+    for (u32 i0 = 0; i0 < d->channels; i0 += nb) {
+        const u32 n = d->channels - i0 < nb ? d->channels - i0 : nb;
+        const u64 *px[KS_MAX_BATCH], *pt[KS_MAX_BATCH], *pr[KS_MAX_BATCH], *pg[KS_MAX_BATCH], *pres[KS_MAX_BATCH], *ptmp[KS_MAX_BATCH];
+        u64 *ot[KS_MAX_BATCH], *out[KS_MAX_BATCH];
+        for (u32 b = 0; b < n; b++) {
+            px[b] = (const u64*)x->d + (size_t)(i0 + b) * x->ct_stride;
+            pt[b] = ot[b] = t + (size_t)b * 2 * level * N;
+            pr[b] = ra;
+            pg[b] = d->gate ? (const u64*)gate->d + (size_t)(i0 + b) * gate->ct_stride : nullptr;
+            pres[b] = add ? (const u64*)residual->d + (size_t)(i0 + b) * residual->ct_stride : nullptr;
+            ptmp[b] = tmp + (size_t)b * 2 * L1 * N;
+            out[b] = (u64*)d_out + (size_t)(i0 + b) * out_ct;
+        }
+        size_t ts = x->comp_stride;
+        if (d->gate == HE_GATE_NONE) {
+            for (u32 b = 0; b < n; b++) pt[b] = px[b];
+        } else {
+            ts = (size_t)level * N;
+            if (d->gate == HE_GATE_PLAIN) {
+                HIP_TRY(launch_gate_mul(c, level, n, px[0], x->ct_stride, x->comp_stride, pg[0], gate->ct_stride, tmp, st));
+                for (u32 b0 = 0; b0 < n; b0 += CT_BATCH)
+                    if ((rc = run_rescale(c, level, ptmp + b0, L1 * N, ot + b0, n - b0 < CT_BATCH ? n - b0 : CT_BATCH, ar.rest(), st))) return rc;
+            } else if ((rc = run_ctct_merged(c, level, px, x->comp_stride, pg, gate->comp_stride, nullptr, 0, rlk->d_key, ot, n, ar.rest(), st))) {
+                return rc;
+            }
+        }
+        if (!add) {
+            if ((rc = run_ctct_merged(c, last, pt, ts, pr, rs, nullptr, 0, rlk->d_key, out, n, ar.rest(), st))) return rc;
+        } else if (mac) {
+            const LinAddend lin = {pres, residual->comp_stride, kr.v, pres, residual->comp_stride, zero.v};
+            if ((rc = run_ctct_merged(c, last, pt, ts, pr, rs, nullptr, 0, rlk->d_key, out, n, ar.rest(), st, &lin))) return rc;
+        } else {  // the scaled residuals, compact
+            for (u32 b = 0; b < n; b++) HIP_TRY(launch_affine(c, last, pres[b], residual->comp_stride, kr, zero, tmp + (size_t)b * 2 * rs, st));
+            if ((rc = run_ctct_merged(c, last, pt, ts, pr, rs, tmp, 2 * rs, rlk->d_key, out, n, ar.rest(), st))) return rc;
+        }
+    }
+    return CKKS_OK;
+}
+
 // ---- optional per-kernel timing -------------------------------------------------------------------
 static const char* const kKernelNames[K_COUNT] = {
     "ntt_fwd_hi", "ntt_fwd_lo", "ntt_inv_lo", "ntt_inv_hi", "modup_conv", "key_inner", "moddown_conv", "moddown_final",

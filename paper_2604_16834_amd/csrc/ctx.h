@@ -368,3 +368,28 @@ hipError_t launch_wsum_mfma(const ckks_ctx* c, u32 level, u32 nl, const u64* xs,
 hipError_t launch_lincomb2(const ckks_ctx* c, u32 level, const PtrList8& a, size_t a_cstride, const u64* ka, const PtrList8& b,
                            size_t b_cstride, const u64* kb, const u64* add, size_t add_bstride, u64* out, size_t out_bstride, u32 n,
                            hipStream_t st);
+// block.hip (ciphertexts of a vector at equal distances: ct and component strides in words, limbs N apart)
+// one residue per limb
+struct LimbScalars {
+    u64 v[CKKS_MAX_MODULI];
+};
+// which channels of a head turn together: pair j holds (j, j + n_pairs) or, interleaved, (2j, 2j + 1); pairs are numbered through the heads, z0 is the
+// launch's first
+struct RopePairs {
+    u32 head_dim, n_pairs, interleaved, inverse, z0;
+    __host__ __device__ u32 first(u32 j) const { return interleaved ? 2 * j : j; }
+    __host__ __device__ u32 second(u32 j) const { return interleaved ? 2 * j + 1 : j + n_pairs; }
+};
+hipError_t launch_linear_sum(const ckks_ctx* c, u32 level, u32 rows, const u64* in, size_t in_ct, size_t in_comp, u32 c_in, u32 c_out,
+                             const void* w, u32 weight_bytes, size_t w_out, size_t w_in, const u64* bias, const LimbScalars& mult, u64* acc,
+                             hipStream_t st);
+hipError_t launch_rope_turn(const ckks_ctx* c, u32 level, u32 n, const u64* in, size_t in_ct, size_t in_comp, const RopePairs& P, const u64* cs,
+                            const u64* sn, u64* y, hipStream_t st);
+hipError_t launch_rope_pass(const ckks_ctx* c, u32 level, u32 n, const u64* in, size_t in_ct, size_t in_comp, const RopePairs& P, u64* out,
+                            hipStream_t st);
+hipError_t launch_square_sum(const ckks_ctx* c, u32 level, const u64* in, size_t in_ct, size_t in_comp, u32 channels, const LimbScalars& add, u64* d,
+                             hipStream_t st);
+hipError_t launch_affine(const ckks_ctx* c, u32 level, const u64* ct, size_t ct_comp, const LimbScalars& k, const LimbScalars& add, u64* out,
+                         hipStream_t st);
+hipError_t launch_gate_mul(const ckks_ctx* c, u32 level, u32 n, const u64* ct, size_t ct_stride, size_t ct_comp, const u64* gate, size_t gate_stride,
+                           u64* out, hipStream_t st);
