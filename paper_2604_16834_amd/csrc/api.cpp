@@ -2085,8 +2085,11 @@ static int linear_plan(const ckks_ctx* c, const he_linear_desc* d, const u32* h_
     if (p->row_step == 0) p->row_step = 1;
     return CKKS_OK;
 }
+static size_t linear_digits(const ckks_ctx* c, const he_linear_desc* d, const LinearPlan& p) {
+    return linear_mfma_applies(c) ? linear_mfma_scratch_elems(d->c_in, p.outs, d->weight_type) : 0;
+}
 static size_t ws_linear(const ckks_ctx* c, const he_linear_desc* d, const LinearPlan& p) {
-    return blk((size_t)p.row_step * p.outs * 2 * (d->level + 1) * c->N) + ws_rescale(c, d->level, CT_BATCH);
+    return blk((size_t)p.row_step * p.outs * 2 * (d->level + 1) * c->N) + blk(linear_digits(c, d, p)) + ws_rescale(c, d->level, CT_BATCH);
 }
 
 size_t he_linear_workspace_bytes(const ckks_ctx* c, const he_linear_desc* d, const uint32_t* h_group_rows) {
@@ -2110,8 +2113,7 @@ int he_linear_grouped(const ckks_ctx* c, const he_linear_desc* d, const uint32_t
     const size_t N = c->N, ct = (size_t)2 * L1 * N, out_ct = (size_t)2 * level * N;
     Arena ar(d_ws, ws_bytes);
     u64* sums = ar.take((size_t)p.row_step * p.outs * ct);
-    LimbScalars mult;
-    for (u32 i = 0; i < CKKS_MAX_MODULI; i++) mult.v[i] = i <= level ? d->multiplier % c->mod[i] : 0;
+    u64* digits = ar.take(linear_digits(c, d, p));
     const size_t w_group = (size_t)d->c_in * d->c_out, w_out = d->transposed ? 1 : d->c_in, w_in = d->transposed ? d->c_out : 1;
     u64 t0 = 0;
     for (u32 g = 0; g < d->n_groups; t0 += h_group_rows[g], g++) {
@@ -2122,7 +2124,7 @@ int he_linear_grouped(const ckks_ctx* c, const he_linear_desc* d, const uint32_t
             for (u32 r0 = 0; r0 < h_group_rows[g]; r0 += p.row_step) {
                 const u32 nr = h_group_rows[g] - r0 < p.row_step ? h_group_rows[g] - r0 : p.row_step;
                 HIP_TRY(launch_linear_sum(c, level, nr, (const u64*)in->d + (t0 + r0) * d->c_in * in->ct_stride, in->ct_stride, in->comp_stride, d->c_in, no,
-                                          w, d->weight_type, w_out, w_in, bias, mult, sums, st));
+                                          w, d->weight_type, w_out, w_in, bias, d->multiplier, sums, digits, st));
                 for (u32 i0 = 0; i0 < nr * no; i0 += CT_BATCH) {
                     const u32 n = nr * no - i0 < CT_BATCH ? nr * no - i0 : CT_BATCH;
                     const u64* src[CT_BATCH];

@@ -44,22 +44,76 @@ __global__ __launch_bounds__(BK_THREADS) void linear_sum_kernel(const u64* __res
     }
 }
 
+// The same for moduli below 2^50 and few channels, in double precision (f64m_dot_w: chains of eight exact products of centred residues and
+// weights): a thread reads a column's channels eight at a time and adds a chain to each of OT outputs.
+template <class W, u32 OT>
+__global__ __launch_bounds__(BK_THREADS) void linear_sum_f64_kernel(const u64* __restrict__ in, size_t in_ct, size_t in_comp, const W* __restrict__ w,
+                                                                    size_t w_out, size_t w_in, const u64* __restrict__ bias, LimbScalars mult,
+                                                                    u64* __restrict__ acc, const ModConstF* __restrict__ mcf, u32 N, u32 limbs,
+                                                                    u32 c_in, u32 c_out, u32 o_tiles) {
+    const u32 x = blockIdx.x * BK_THREADS + threadIdx.x;
+    if (x >= N) return;
+    const u32 e = blockIdx.y % limbs, comp = blockIdx.y / limbs, row = blockIdx.z / o_tiles, o0 = blockIdx.z % o_tiles * OT;
+    const ModConstF m = mcf[e];
+    const u64* src = in + (size_t)row * c_in * in_ct + comp * in_comp + (size_t)e * N + x;
+    double sum[OT];
+#pragma unroll
+    for (u32 t = 0; t < OT; t++) sum[t] = 0.0;
+    for (u32 c0 = 0; c0 < c_in; c0 += 8) {
+        double y[8];
+#pragma unroll
+        for (u32 a = 0; a < 8; a++) y[a] = f64m_from_u64(src[(c0 + a < c_in ? c0 + a : c_in - 1) * in_ct]);
+#pragma unroll
+        for (u32 a = 0; a < 8; a++) y[a] = c0 + a < c_in ? f64m_centre(y[a], m.q) : 0.0;
+#pragma unroll
+        for (u32 t = 0; t < OT; t++) {
+            const W* wr = w + (o0 + t < c_out ? o0 + t : c_out - 1) * w_out;
+            double v[8];
+#pragma unroll
+            for (u32 a = 0; a < 8; a++) v[a] = (double)(int)wr[(c0 + a < c_in ? c0 + a : c_in - 1) * w_in];
+            sum[t] = f64m_reduce(sum[t] + f64m_dot_w<8>(y, v, m.q, m.qinv), m.q, m.qinv);
+        }
+    }
+    const double k = f64m_from_u64(mult.v[e]);
+#pragma unroll
+    for (u32 t = 0; t < OT; t++) {
+        if (o0 + t >= c_out) return;
+        double v = f64m_mulmod_any(sum[t], k, m.q, m.qinv);
+        if (bias && comp == 0) v = f64m_reduce(v + f64m_from_u64(bias[(size_t)(o0 + t) * limbs + e]), m.q, m.qinv);
+        acc[(((size_t)row * c_out + o0 + t) * 2 + comp) * limbs * N + (size_t)e * N + x] = f64m_canonical(v, m.q);
+    }
+}
+
+// Up to this many channels on rings that the matrix-core kernel takes.
+#define LINEAR_F64_CHANNELS 8
+
+// scratch: linear_mfma_scratch_elems words where linear_mfma_applies
 hipError_t launch_linear_sum(const ckks_ctx* c, u32 level, u32 rows, const u64* in, size_t in_ct, size_t in_comp, u32 c_in, u32 c_out,
-                             const void* w, u32 weight_bytes, size_t w_out, size_t w_in, const u64* bias, const LimbScalars& mult, u64* acc,
+                             const void* w, u32 weight_bytes, size_t w_out, size_t w_in, const u64* bias, u64 multiplier, u64* acc, u64* scratch,
                              hipStream_t st) {
-    const u32 limbs = level + 1, o_tiles = (c_out + LG_OUT_TILE - 1) / LG_OUT_TILE;
+    if (linear_mfma_applies(c) && c_in > LINEAR_F64_CHANNELS)
+        return launch_linear_mfma(c, level, rows, in, in_ct, in_comp, c_in * in_ct, c_in, c_out, w, weight_bytes, w_out, w_in, bias, multiplier, acc, scratch, st);
+    LimbScalars mult;
+    for (u32 i = 0; i < CKKS_MAX_MODULI; i++) mult.v[i] = i <= level ? multiplier % c->mod[i] : 0;
+    const u32 limbs = level + 1, tile = c->small_q ? (c_out <= 2 ? 2 : 8) : LG_OUT_TILE, o_tiles = (c_out + tile - 1) / tile;
     for (u32 r0 = 0; r0 < rows;) {  // the launch's third dimension holds 65535 workgroups
         const u32 most = 65535 / o_tiles, n = rows - r0 < most ? rows - r0 : most;
         const dim3 grid((c->N + BK_THREADS - 1) / BK_THREADS, 2 * limbs, n * o_tiles);
         const u64* src = in + (size_t)r0 * c_in * in_ct;
         u64* dst = acc + (size_t)r0 * c_out * 2 * limbs * c->N;
         ProfScope ps__(c, K_WEIGHTED_SUM, st, 16.0 * n * c->N * limbs * (c_in + c_out), 2.0 * n * c->N * limbs * c_in * c_out);
-#define LINEAR_SUM(W) hipLaunchKernelGGL(linear_sum_kernel<W>, grid, dim3(BK_THREADS), 0, st, src, in_ct, in_comp, (const W*)w, w_out, w_in, bias, mult, \
-                                         dst, c->d_mc, c->N, limbs, c_in, c_out, o_tiles)
-        if (weight_bytes == 1) LINEAR_SUM(int8_t);
-        else if (weight_bytes == 2) LINEAR_SUM(int16_t);
-        else LINEAR_SUM(int32_t);
+#define LINEAR_ARGS(W, TABLE) grid, dim3(BK_THREADS), 0, st, src, in_ct, in_comp, (const W*)w, w_out, w_in, bias, mult, dst, TABLE, c->N, limbs, c_in, c_out, o_tiles
+#define LINEAR_SUM(W)                                                                               \
+    {                                                                                               \
+        if (!c->small_q) hipLaunchKernelGGL(linear_sum_kernel<W>, LINEAR_ARGS(W, c->d_mc));         \
+        else if (tile == 2) hipLaunchKernelGGL((linear_sum_f64_kernel<W, 2>), LINEAR_ARGS(W, c->d_mcf)); \
+        else hipLaunchKernelGGL((linear_sum_f64_kernel<W, 8>), LINEAR_ARGS(W, c->d_mcf));           \
+    }
+        if (weight_bytes == 1) LINEAR_SUM(int8_t)
+        else if (weight_bytes == 2) LINEAR_SUM(int16_t)
+        else LINEAR_SUM(int32_t)
 #undef LINEAR_SUM
+#undef LINEAR_ARGS
         r0 += n;
     }
     return hipGetLastError();

@@ -368,7 +368,7 @@ hipError_t launch_wsum_mfma(const ckks_ctx* c, u32 level, u32 nl, const u64* xs,
 hipError_t launch_lincomb2(const ckks_ctx* c, u32 level, const PtrList8& a, size_t a_cstride, const u64* ka, const PtrList8& b,
                            size_t b_cstride, const u64* kb, const u64* add, size_t add_bstride, u64* out, size_t out_bstride, u32 n,
                            hipStream_t st);
-// block.hip (ciphertexts of a vector at equal distances: ct and component strides in words, limbs N apart)
+// linear_mfma.hip, block.hip (ciphertexts of a vector at equal distances: ct and component strides in words, limbs N apart)
 // one residue per limb
 struct LimbScalars {
     u64 v[CKKS_MAX_MODULI];
@@ -381,8 +381,15 @@ struct RopePairs {
     __host__ __device__ u32 second(u32 j) const { return interleaved ? 2 * j + 1 : j + n_pairs; }
 };
 hipError_t launch_linear_sum(const ckks_ctx* c, u32 level, u32 rows, const u64* in, size_t in_ct, size_t in_comp, u32 c_in, u32 c_out,
-                             const void* w, u32 weight_bytes, size_t w_out, size_t w_in, const u64* bias, const LimbScalars& mult, u64* acc,
+                             const void* w, u32 weight_bytes, size_t w_out, size_t w_in, const u64* bias, u64 multiplier, u64* acc, u64* scratch,
                              hipStream_t st);
+// linear_mfma.hip
+bool linear_mfma_applies(const ckks_ctx* c);
+size_t linear_mfma_scratch_elems(u32 c_in, u32 c_out, u32 weight_bytes);
+hipError_t launch_linear_mfma(const ckks_ctx* c, u32 level, u32 rows, const u64* in, size_t in_ct, size_t in_comp, size_t in_row, u32 c_in, u32 c_out,
+                              const void* w, u32 weight_bytes, size_t w_out, size_t w_in, const u64* bias, u64 multiplier, u64* acc, u64* scratch,
+                              hipStream_t st);
+// block.hip
 hipError_t launch_rope_turn(const ckks_ctx* c, u32 level, u32 n, const u64* in, size_t in_ct, size_t in_comp, const RopePairs& P, const u64* cs,
                             const u64* sn, u64* y, hipStream_t st);
 hipError_t launch_rope_pass(const ckks_ctx* c, u32 level, u32 n, const u64* in, size_t in_ct, size_t in_comp, const RopePairs& P, u64* out,

@@ -118,6 +118,26 @@ def test_grouped_product_of_nothing():
     assert tuple(out.shape) == (0, 3, 2, 3, orc.N)
 
 
+@pytest.mark.parametrize("dtype", [np.int8, np.int16, np.int32])
+@pytest.mark.parametrize("c_in,c_out,transposed", [(128, 40, True), (256, 33, False), (300, 5, False), (520, 2, True)])
+def test_grouped_product_over_many_channels(dtype, c_in, c_out, transposed):
+    """Sums as long as one launch of the matrix cores takes and longer; residues whose digits are all -128 and weights at the type's ends in
+    half of the products, so that every diagonal is as large as it gets."""
+    p, orc, ctx = world(12, 2, 1, 1)
+    rng = np.random.default_rng(c_in)
+    info = np.iinfo(dtype)
+    x = ciphertexts(rng, p, 1, c_in)
+    x[:, 0, :, 100:200] = 0x0000808080808080 & ~0x0000800000000000 | 0x0000400000000000
+    x[:, :, :, 200:300] = 0x0000008080808080
+    w = rng.integers(info.min, info.max, size=(1, c_out, c_in), endpoint=True).astype(dtype)
+    w[0, 0], w[0, -1] = info.min, info.max
+    w[0, c_out // 2, ::2] = info.min
+    dw = torch.from_numpy(np.ascontiguousarray(w.transpose(0, 2, 1)) if transposed else w).cuda()
+    got = hx.to_host(hx.he_linear_grouped(ctx, 1, (1,), hx.from_host(x)[None], dw, 987654321, transposed=transposed))
+    for o in {0, 1, c_out // 2, c_out - 1}:
+        assert np.array_equal(got[0, o], orc.linear_grouped([x], 1, (1,), w[:, o:o + 1], 987654321)[0][0]), o
+
+
 def test_one_ciphertext_in_the_place_of_all_channels():
     p, orc, ctx = world(12, 4, 2, 2)
     rng = np.random.default_rng(8)
