@@ -2055,10 +2055,19 @@ static LimbScalars limb_scalars(const ckks_ctx* c, u32 level, int64_t k) {
     return s;
 }
 
-// Ciphertexts whose sums are in the workspace at a time: of a row's c_out outputs as many as 2 GiB hold, then further rows
-#define LINEAR_SUMS_BYTES ((size_t)2 << 30)
+// A grouped product's divisions by q_level, in two forms:
+//   sums first: all limbs' sums go to the workspace and are rescaled from there, where the whole call is one launch of the small rings' rescale, and with moduli of
+//     2^50 and more;
+//   share first: the dropped limb's sums alone, its share of the quotients written to the outputs (launch_ntt_rescale_share), and the other limbs' sums, times
+//     multiplier / q_level, added to them as they are formed: no sums in memory, the transforms' plain lo pass instead of the one that reads a second operand, and
+//     any number of outputs per launch.  Sums first / share first in us: 37 -> 29 channels, six rows at N = 2^13, 5 limbs 543 / 287, 64 -> 40, four rows at 2^14, 10
+//     limbs 1446 / 1003, 64 -> 64, three rows at 2^16, 24 limbs 6640 / 6240.  (A few limbs of the outputs at a time, which the last-level cache would hold from one
+//     kernel to the next, is no faster: 6.5 to 7.9 ms for the last of these with 8 down to 1 limbs.)
+// Outputs at a time: as many as the workspace's part below holds, of whole rows if a row fits.
+#define LINEAR_SUMS_BYTES ((size_t)1 << 30)
 struct LinearPlan {
     u64 rows;      // in all
+    bool share;
     u32 outs;      // outputs of a row at a time
     u32 row_step;  // rows at a time
 };
@@ -2077,21 +2086,26 @@ static int linear_plan(const ckks_ctx* c, const he_linear_desc* d, const u32* h_
         if (h_rows[g] > most) most = h_rows[g];
     }
     if (p->rows > (u64)1 << 24) return set_err(c, CKKS_ERR_INVALID_ARG, "too many rows");
-    const size_t fit = LINEAR_SUMS_BYTES / ((size_t)(d->level + 1) * c->N * 16);
-    const u32 cap = fit < CT_BATCH ? CT_BATCH : (fit > 65536 ? 65536 : (u32)fit);
-    p->outs = d->c_out < cap ? d->c_out : cap;
-    p->row_step = cap / p->outs;
+    p->share = ntt_has_modup(c) && !(p->rows * d->c_out <= CT_BATCH && ntt_rescale_one_launch(c, d->level, 2 * (u32)p->rows * d->c_out));
+    const size_t fit = LINEAR_SUMS_BYTES / ((size_t)(p->share ? 1 : d->level + 1) * c->N * 16);
+    const u32 cap = fit < CT_BATCH ? CT_BATCH : (fit > 1024 ? 1024 : (u32)fit);  // (the transforms' launches number the components in 16 bits)
+    p->outs = d->c_out;
+    if (p->outs > cap) {  // even parts of whole tiles of the matrix cores
+        const u32 parts = (d->c_out + cap - 1) / cap, even = ((d->c_out + parts - 1) / parts + 127) / 128 * 128;
+        p->outs = even < cap ? even : cap;
+    }
+    p->row_step = p->outs < d->c_out ? 1 : cap / p->outs;
     if (p->row_step > most) p->row_step = most;
     if (p->row_step == 0) p->row_step = 1;
     return CKKS_OK;
 }
 static size_t linear_digits(const ckks_ctx* c, const he_linear_desc* d, const LinearPlan& p) {
-    return linear_mfma_applies(c) ? linear_mfma_scratch_elems(d->c_in, p.outs, d->weight_type) : 0;
+    return linear_mfma_applies(c, d->c_in) ? linear_mfma_scratch_elems(d->c_in, p.outs, d->weight_type) : 0;
 }
 static size_t ws_linear(const ckks_ctx* c, const he_linear_desc* d, const LinearPlan& p) {
-    return blk((size_t)p.row_step * p.outs * 2 * (d->level + 1) * c->N) + blk(linear_digits(c, d, p)) + ws_rescale(c, d->level, CT_BATCH);
+    const size_t outs = (size_t)p.row_step * p.outs;
+    return blk(outs * 2 * (p.share ? 1 : d->level + 1) * c->N) + blk(linear_digits(c, d, p)) + (p.share ? 0 : ws_rescale(c, d->level, CT_BATCH));
 }
-
 size_t he_linear_workspace_bytes(const ckks_ctx* c, const he_linear_desc* d, const uint32_t* h_group_rows) {
     LinearPlan p;
     if (!c || linear_plan(c, d, h_group_rows, &p)) return 0;
@@ -2110,29 +2124,72 @@ int he_linear_grouped(const ckks_ctx* c, const he_linear_desc* d, const uint32_t
     if (int rc = check_array(c, in, p.rows * d->c_in, L1, 2)) return rc;
     if (!d_ws || ws_bytes < ws_linear(c, d, p)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the grouped product");
     hipStream_t st = (hipStream_t)stream;
-    const size_t N = c->N, ct = (size_t)2 * L1 * N, out_ct = (size_t)2 * level * N;
+    const size_t N = c->N, out_ct = (size_t)2 * level * N;
     Arena ar(d_ws, ws_bytes);
-    u64* sums = ar.take((size_t)p.row_step * p.outs * ct);
+    u64* sums = ar.take((size_t)p.row_step * p.outs * 2 * (p.share ? 1 : L1) * N);
     u64* digits = ar.take(linear_digits(c, d, p));
-    const size_t w_group = (size_t)d->c_in * d->c_out, w_out = d->transposed ? 1 : d->c_in, w_in = d->transposed ? d->c_out : 1;
+    LinearSum S;
+    S.in_ct = in->ct_stride;
+    S.in_comp = in->comp_stride;
+    S.in_row = d->c_in * in->ct_stride;
+    S.c_in = d->c_in;
+    S.weight_bytes = d->weight_type;
+    S.w_out = d->transposed ? 1 : d->c_in;
+    S.w_in = d->transposed ? d->c_out : 1;
+    S.bias_limbs = L1;
+    LimbScalars mult, one, mult_q, inv_q;  // (.. q_level^-1)
+    for (u32 i = 0; i < CKKS_MAX_MODULI; i++) {
+        const u64 q = i < level ? c->mod[i] : 0;
+        mult.v[i] = i <= level ? d->multiplier % c->mod[i] : 0;
+        one.v[i] = i <= level ? 1 : 0;
+        inv_q.v[i] = q && p.share ? c->rescale_inv[(size_t)level * c->num_q + i] : 0;
+        mult_q.v[i] = q ? (u64)((unsigned __int128)mult.v[i] * inv_q.v[i] % q) : 0;
+    }
     u64 t0 = 0;
     for (u32 g = 0; g < d->n_groups; t0 += h_group_rows[g], g++) {
         for (u32 o0 = 0; o0 < d->c_out; o0 += p.outs) {
             const u32 no = d->c_out - o0 < p.outs ? d->c_out - o0 : p.outs;
-            const char* w = (const char*)d_w + (g * w_group + o0 * w_out) * d->weight_type;
-            const u64* bias = d_bias ? (const u64*)d_bias + ((size_t)g * d->c_out + o0) * L1 : nullptr;
+            S.c_out = no;
+            S.w = (const char*)d_w + ((size_t)g * d->c_in * d->c_out + o0 * S.w_out) * d->weight_type;
+            S.bias = d_bias ? (const u64*)d_bias + ((size_t)g * d->c_out + o0) * L1 : nullptr;
             for (u32 r0 = 0; r0 < h_group_rows[g]; r0 += p.row_step) {
                 const u32 nr = h_group_rows[g] - r0 < p.row_step ? h_group_rows[g] - r0 : p.row_step;
-                HIP_TRY(launch_linear_sum(c, level, nr, (const u64*)in->d + (t0 + r0) * d->c_in * in->ct_stride, in->ct_stride, in->comp_stride, d->c_in, no,
-                                          w, d->weight_type, w_out, w_in, bias, d->multiplier, sums, digits, st));
+                u64* out = (u64*)d_out + ((t0 + r0) * d->c_out + o0) * out_ct;
+                S.rows = nr;
+                S.in = (const u64*)in->d + (t0 + r0) * S.in_row;
+                S.add = 0;
+                S.mult = mult;
+                S.bias_mult = one;
+                S.acc = sums;
+                S.limb0 = p.share ? level : 0;
+                S.limbs = p.share ? 1 : L1;
+                S.acc_comp = S.limbs * N;
+                S.acc_ct = 2 * S.acc_comp;
+                S.acc_row = no * S.acc_ct;
+                HIP_TRY(launch_linear_sum(c, S, digits, r0 > 0, st));
+                if (p.share) {  // (nr > 1 only for whole rows: the outputs follow each other)
+                    HIP_TRY(launch_ntt(c, true, sums, 1, sums, 1, range_list(0, 1, level), 2 * nr * no, st, nullptr, nullptr, c->d_rescale_prep_f, nullptr, nullptr, NTT_LO));
+                    HIP_TRY(launch_ntt_rescale_share(c, level, (const double*)sums, out, 2 * nr * no, st));
+                    S.add = 1;
+                    S.mult = mult_q;
+                    S.bias_mult = inv_q;
+                    S.limb0 = 0;
+                    S.limbs = level;
+                    S.acc = out;
+                    S.acc_comp = (size_t)level * N;
+                    S.acc_ct = out_ct;
+                    S.acc_row = no * out_ct;
+                    HIP_TRY(launch_linear_sum(c, S, digits, true, st));
+                    continue;
+                }
                 for (u32 i0 = 0; i0 < nr * no; i0 += CT_BATCH) {
                     const u32 n = nr * no - i0 < CT_BATCH ? nr * no - i0 : CT_BATCH;
                     const u64* src[CT_BATCH];
                     u64* dst[CT_BATCH];
                     for (u32 b = 0; b < n; b++) {
                         const u32 i = i0 + b;
-                        src[b] = sums + i * ct;
-                        dst[b] = (u64*)d_out + ((t0 + r0 + i / no) * d->c_out + o0 + i % no) * out_ct;
+                        src[b] = sums + i * S.acc_ct;
+                        dst[b] = out + ((size_t)(i / no) * d->c_out + i % no) * out_ct;
                     }
                     if (int rc = run_rescale(c, level, src, (size_t)L1 * N, dst, n, ar.rest(), st)) return rc;
                 }

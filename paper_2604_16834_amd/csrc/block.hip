@@ -6,114 +6,133 @@
 #define BK_THREADS 256
 
 // ---- sums over channels with the weights of one expert ------------------------------------------------------
-// acc[r][o][comp][e][x] = (sum_c W[o][c] * in[r][c][comp][e][x]) * mult[e] + (comp == 0 ? bias[o][e] : 0)   mod q_e
-// The products are summed as signed 128-bit integers: a term is below 2^31 q in magnitude, 2^16 of them below 2^47 q, so with 2^48 q
+struct LinearArgs {
+    const u64* in;
+    size_t in_ct, in_comp, in_row;
+    const void* w;
+    size_t w_out, w_in;
+    const u64* bias;
+    u64* acc;
+    size_t acc_ct, acc_comp, acc_row;
+    u32 N, limb0, limbs, bias_limbs, c_in, c_out, o_tiles, add;
+    LimbScalars mult, bias_mult;
+};
+// Any modulus.  The products are summed as signed 128-bit integers: a term is below 2^31 q in magnitude, 2^16 of them below 2^47 q, so with 2^48 q
 // added the sum is positive and below 2^49 q, which barrett_reduce takes.
 #define LG_OUT_TILE 4
 template <class W>
-__global__ __launch_bounds__(BK_THREADS) void linear_sum_kernel(const u64* __restrict__ in, size_t in_ct, size_t in_comp, const W* __restrict__ w,
-                                                                size_t w_out, size_t w_in, const u64* __restrict__ bias, LimbScalars mult,
-                                                                u64* __restrict__ acc, const ModConst* __restrict__ mc, u32 N, u32 limbs,
-                                                                u32 c_in, u32 c_out, u32 o_tiles) {
+__global__ __launch_bounds__(BK_THREADS) void linear_sum_kernel(LinearArgs A, const ModConst* __restrict__ mc) {
     const u32 x = blockIdx.x * BK_THREADS + threadIdx.x;
-    if (x >= N) return;
-    const u32 e = blockIdx.y % limbs, comp = blockIdx.y / limbs, row = blockIdx.z / o_tiles, o0 = blockIdx.z % o_tiles * LG_OUT_TILE;
+    if (x >= A.N) return;
+    const u32 er = blockIdx.y % A.limbs, e = A.limb0 + er, comp = blockIdx.y / A.limbs, row = blockIdx.z / A.o_tiles, o0 = blockIdx.z % A.o_tiles * LG_OUT_TILE;
     const ModConst m = mc[e];
-    const u64* src = in + (size_t)row * c_in * in_ct + comp * in_comp + (size_t)e * N + x;
+    const u64* src = A.in + row * A.in_row + comp * A.in_comp + (size_t)e * A.N + x;
+    const W* w = (const W*)A.w;
     __int128 sum[LG_OUT_TILE];
 #pragma unroll
     for (u32 t = 0; t < LG_OUT_TILE; t++) sum[t] = 0;
-    for (u32 ch = 0; ch < c_in; ch++) {
-        const long long v = (long long)src[ch * in_ct];
+    for (u32 ch = 0; ch < A.c_in; ch++) {
+        const long long v = (long long)src[ch * A.in_ct];
 #pragma unroll
         for (u32 t = 0; t < LG_OUT_TILE; t++) {
-            const u32 o = o0 + t < c_out ? o0 + t : c_out - 1;
-            sum[t] += (__int128)v * (long long)w[o * w_out + ch * w_in];
+            const u32 o = o0 + t < A.c_out ? o0 + t : A.c_out - 1;
+            sum[t] += (__int128)v * (long long)w[o * A.w_out + ch * A.w_in];
         }
     }
 #pragma unroll
     for (u32 t = 0; t < LG_OUT_TILE; t++) {
-        if (o0 + t >= c_out) return;
+        const u32 o = o0 + t;
+        if (o >= A.c_out) return;
         const unsigned __int128 s = (unsigned __int128)(sum[t] + ((__int128)m.q << 48));
         U128 r;
         r.lo = (u64)s;
         r.hi = (u64)(s >> 64);
-        u64 v = mulmod_barrett(barrett_reduce(r, m), mult.v[e], m);
-        if (bias && comp == 0) v = add_mod(v, bias[(size_t)(o0 + t) * limbs + e], m.q);
-        acc[(((size_t)row * c_out + o0 + t) * 2 + comp) * limbs * N + (size_t)e * N + x] = v;
+        u64 v = mulmod_barrett(barrett_reduce(r, m), A.mult.v[e], m);
+        if (A.bias && comp == 0) v = add_mod(v, mulmod_barrett(A.bias[(size_t)o * A.bias_limbs + e], A.bias_mult.v[e], m), m.q);
+        u64* acc = A.acc + row * A.acc_row + o * A.acc_ct + comp * A.acc_comp + (size_t)er * A.N + x;
+        *acc = A.add ? add_mod(v, *acc, m.q) : v;
     }
 }
 
-// The same for moduli below 2^50 and few channels, in double precision (f64m_dot_w: chains of eight exact products of centred residues and
-// weights): a thread reads a column's channels eight at a time and adds a chain to each of OT outputs.
+// Moduli below 2^50 and few channels, in double precision (f64m_dot_w: chains of eight exact products of centred residues and weights): a thread reads a
+// column's channels eight at a time and adds a chain to each of OT outputs, whose weights are in LDS.
 template <class W, u32 OT>
-__global__ __launch_bounds__(BK_THREADS) void linear_sum_f64_kernel(const u64* __restrict__ in, size_t in_ct, size_t in_comp, const W* __restrict__ w,
-                                                                    size_t w_out, size_t w_in, const u64* __restrict__ bias, LimbScalars mult,
-                                                                    u64* __restrict__ acc, const ModConstF* __restrict__ mcf, u32 N, u32 limbs,
-                                                                    u32 c_in, u32 c_out, u32 o_tiles) {
-    const u32 x = blockIdx.x * BK_THREADS + threadIdx.x;
-    if (x >= N) return;
-    const u32 e = blockIdx.y % limbs, comp = blockIdx.y / limbs, row = blockIdx.z / o_tiles, o0 = blockIdx.z % o_tiles * OT;
+__global__ __launch_bounds__(BK_THREADS) void linear_sum_f64_kernel(LinearArgs A, const ModConstF* __restrict__ mcf) {
+    __shared__ double lw[8 * OT];
+    const u32 tid = threadIdx.x, x = blockIdx.x * BK_THREADS + tid, xc = x < A.N ? x : A.N - 1;
+    const u32 er = blockIdx.y % A.limbs, e = A.limb0 + er, comp = blockIdx.y / A.limbs, row = blockIdx.z / A.o_tiles, o0 = blockIdx.z % A.o_tiles * OT;
     const ModConstF m = mcf[e];
-    const u64* src = in + (size_t)row * c_in * in_ct + comp * in_comp + (size_t)e * N + x;
+    const u64* src = A.in + row * A.in_row + comp * A.in_comp + (size_t)e * A.N + xc;
+    u64* acc = A.acc + row * A.acc_row + o0 * A.acc_ct + comp * A.acc_comp + (size_t)er * A.N + xc;
+    const u32 n_out = A.c_out - o0 < OT ? A.c_out - o0 : OT;
+    u64 old[OT];
+    if (A.add) {
+#pragma unroll
+        for (u32 t = 0; t < OT; t++) old[t] = acc[(t < n_out ? t : 0) * A.acc_ct];
+    }
     double sum[OT];
 #pragma unroll
     for (u32 t = 0; t < OT; t++) sum[t] = 0.0;
-    for (u32 c0 = 0; c0 < c_in; c0 += 8) {
-        double y[8];
+    for (u32 c0 = 0; c0 < A.c_in; c0 += 8) {
+        const u32 n = A.c_in - c0 < 8 ? A.c_in - c0 : 8;
+        u64 raw[8];
 #pragma unroll
-        for (u32 a = 0; a < 8; a++) y[a] = f64m_from_u64(src[(c0 + a < c_in ? c0 + a : c_in - 1) * in_ct]);
-#pragma unroll
-        for (u32 a = 0; a < 8; a++) y[a] = c0 + a < c_in ? f64m_centre(y[a], m.q) : 0.0;
-#pragma unroll
-        for (u32 t = 0; t < OT; t++) {
-            const W* wr = w + (o0 + t < c_out ? o0 + t : c_out - 1) * w_out;
-            double v[8];
-#pragma unroll
-            for (u32 a = 0; a < 8; a++) v[a] = (double)(int)wr[(c0 + a < c_in ? c0 + a : c_in - 1) * w_in];
-            sum[t] = f64m_reduce(sum[t] + f64m_dot_w<8>(y, v, m.q, m.qinv), m.q, m.qinv);
+        for (u32 a = 0; a < 8; a++)
+            if (a < n) raw[a] = src[(c0 + a) * A.in_ct];  // (uniform)
+        if (c0) __syncthreads();
+        if (tid < 8 * OT) {
+            const u32 a = tid / OT, t = tid % OT;
+            lw[tid] = a < n && t < n_out ? (double)(int)((const W*)A.w)[(o0 + t) * A.w_out + (c0 + a) * A.w_in] : 0.0;
         }
+        __syncthreads();
+        double tt[OT], lo[OT];
+#pragma unroll
+        for (u32 t = 0; t < OT; t++) tt[t] = F64M_DOT_BASE, lo[t] = 0.0;
+#pragma unroll
+        for (u32 a = 0; a < 8; a++)
+            if (a < n) {
+                const double y = f64m_centre(f64m_from_u64(raw[a]), m.q);
+#pragma unroll
+                for (u32 t = 0; t < OT; t++) f64m_chain_add(tt[t], lo[t], y, lw[a * OT + t]);
+            }
+#pragma unroll
+        for (u32 t = 0; t < OT; t++) sum[t] = f64m_reduce(sum[t] + f64m_chain_join(tt[t], lo[t], m.q, m.qinv), m.q, m.qinv);
     }
-    const double k = f64m_from_u64(mult.v[e]);
+    if (x >= A.N) return;
+    const double k = f64m_from_u64(A.mult.v[e]), kb = f64m_from_u64(A.bias_mult.v[e]);
 #pragma unroll
     for (u32 t = 0; t < OT; t++) {
-        if (o0 + t >= c_out) return;
+        if (t >= n_out) return;
         double v = f64m_mulmod_any(sum[t], k, m.q, m.qinv);
-        if (bias && comp == 0) v = f64m_reduce(v + f64m_from_u64(bias[(size_t)(o0 + t) * limbs + e]), m.q, m.qinv);
-        acc[(((size_t)row * c_out + o0 + t) * 2 + comp) * limbs * N + (size_t)e * N + x] = f64m_canonical(v, m.q);
+        if (A.bias && comp == 0)
+            v = f64m_reduce(v + f64m_mulmod_any(f64m_from_u64(A.bias[(size_t)(o0 + t) * A.bias_limbs + e]), kb, m.q, m.qinv), m.q, m.qinv);
+        if (A.add) v = f64m_reduce(v + f64m_from_u64(old[t]), m.q, m.qinv);
+        acc[t * A.acc_ct] = f64m_canonical(v, m.q);
     }
 }
 
-// Up to this many channels on rings that the matrix-core kernel takes.
-#define LINEAR_F64_CHANNELS 8
-
-// scratch: linear_mfma_scratch_elems words where linear_mfma_applies
-hipError_t launch_linear_sum(const ckks_ctx* c, u32 level, u32 rows, const u64* in, size_t in_ct, size_t in_comp, u32 c_in, u32 c_out,
-                             const void* w, u32 weight_bytes, size_t w_out, size_t w_in, const u64* bias, u64 multiplier, u64* acc, u64* scratch,
-                             hipStream_t st) {
-    if (linear_mfma_applies(c) && c_in > LINEAR_F64_CHANNELS)
-        return launch_linear_mfma(c, level, rows, in, in_ct, in_comp, c_in * in_ct, c_in, c_out, w, weight_bytes, w_out, w_in, bias, multiplier, acc, scratch, st);
-    LimbScalars mult;
-    for (u32 i = 0; i < CKKS_MAX_MODULI; i++) mult.v[i] = i <= level ? multiplier % c->mod[i] : 0;
-    const u32 limbs = level + 1, tile = c->small_q ? (c_out <= 2 ? 2 : 8) : LG_OUT_TILE, o_tiles = (c_out + tile - 1) / tile;
-    for (u32 r0 = 0; r0 < rows;) {  // the launch's third dimension holds 65535 workgroups
-        const u32 most = 65535 / o_tiles, n = rows - r0 < most ? rows - r0 : most;
-        const dim3 grid((c->N + BK_THREADS - 1) / BK_THREADS, 2 * limbs, n * o_tiles);
-        const u64* src = in + (size_t)r0 * c_in * in_ct;
-        u64* dst = acc + (size_t)r0 * c_out * 2 * limbs * c->N;
-        ProfScope ps__(c, K_WEIGHTED_SUM, st, 16.0 * n * c->N * limbs * (c_in + c_out), 2.0 * n * c->N * limbs * c_in * c_out);
-#define LINEAR_ARGS(W, TABLE) grid, dim3(BK_THREADS), 0, st, src, in_ct, in_comp, (const W*)w, w_out, w_in, bias, mult, dst, TABLE, c->N, limbs, c_in, c_out, o_tiles
-#define LINEAR_SUM(W)                                                                               \
-    {                                                                                               \
-        if (!c->small_q) hipLaunchKernelGGL(linear_sum_kernel<W>, LINEAR_ARGS(W, c->d_mc));         \
-        else if (tile == 2) hipLaunchKernelGGL((linear_sum_f64_kernel<W, 2>), LINEAR_ARGS(W, c->d_mcf)); \
-        else hipLaunchKernelGGL((linear_sum_f64_kernel<W, 8>), LINEAR_ARGS(W, c->d_mcf));           \
+hipError_t launch_linear_sum(const ckks_ctx* c, const LinearSum& S, u64* scratch, bool prepared, hipStream_t st) {
+    if (linear_mfma_applies(c, S.c_in)) return launch_linear_mfma(c, S, scratch, prepared, st);
+    const u32 tile = c->small_q ? (S.c_out <= 2 ? S.c_out : 8) : LG_OUT_TILE, o_tiles = (S.c_out + tile - 1) / tile;
+    for (u32 r0 = 0; r0 < S.rows;) {  // the launch's third dimension holds 65535 workgroups
+        const u32 most = 65535 / o_tiles, n = S.rows - r0 < most ? S.rows - r0 : most;
+        const dim3 grid((c->N + BK_THREADS - 1) / BK_THREADS, 2 * S.limbs, n * o_tiles);
+        const LinearArgs A = {S.in + r0 * S.in_row, S.in_ct, S.in_comp, S.in_row, S.w, S.w_out, S.w_in, S.bias, S.acc + r0 * S.acc_row, S.acc_ct, S.acc_comp, S.acc_row,
+                              c->N, S.limb0, S.limbs, S.bias_limbs, S.c_in, S.c_out, o_tiles, S.add, S.mult, S.bias_mult};
+        ProfScope ps__(c, K_WEIGHTED_SUM, st, 16.0 * n * c->N * S.limbs * (S.c_in + (1.0 + S.add) * S.c_out), 2.0 * n * c->N * S.limbs * S.c_in * S.c_out);
+#define LINEAR_F64(W, OT) hipLaunchKernelGGL((linear_sum_f64_kernel<W, OT>), grid, dim3(BK_THREADS), 0, st, A, c->d_mcf)
+#define LINEAR_SUM(W)                                                                                            \
+    {                                                                                                            \
+        if (!c->small_q) hipLaunchKernelGGL(linear_sum_kernel<W>, grid, dim3(BK_THREADS), 0, st, A, c->d_mc);    \
+        else if (tile == 1) LINEAR_F64(W, 1);                                                                    \
+        else if (tile == 2) LINEAR_F64(W, 2);                                                                    \
+        else LINEAR_F64(W, 8);                                                                                   \
     }
-        if (weight_bytes == 1) LINEAR_SUM(int8_t)
-        else if (weight_bytes == 2) LINEAR_SUM(int16_t)
+        if (S.weight_bytes == 1) LINEAR_SUM(int8_t)
+        else if (S.weight_bytes == 2) LINEAR_SUM(int16_t)
         else LINEAR_SUM(int32_t)
 #undef LINEAR_SUM
-#undef LINEAR_ARGS
+#undef LINEAR_F64
         r0 += n;
     }
     return hipGetLastError();

@@ -84,6 +84,7 @@ extern "C" void ckks_ctx_destroy(ckks_ctx* c) {
     (void)hipFree(c->d_moddown_prep_f);
     (void)hipFree(c->d_rescale_prep_f);
     (void)hipFree(c->d_rescale_conv_f);
+    (void)hipFree(c->d_rescale_neg_f);
     (void)hipFree(c->d_rescale_ep);
     (void)hipFree(c->d_moddown_rs_prep_f);
     (void)hipFree(c->d_rescale);
@@ -295,7 +296,7 @@ extern "C" int ckks_ctx_create(const ckks_params* p, ckks_ctx** out) {
         }
     }
     // the conversion constants as doubles for the double-precision conversions
-    std::vector<TwF> modup_f, modup_prep_f, moddown_f, moddown_rs_f, moddown_prep_f, moddown_rs_prep_f, rescale_prep_f, rescale_conv_f;
+    std::vector<TwF> modup_f, modup_prep_f, moddown_f, moddown_rs_f, moddown_prep_f, moddown_rs_prep_f, rescale_prep_f, rescale_conv_f, rescale_neg_f;
     if (c->dnum && c->ntt_f64) {
         const u32 nq = c->num_q;
         modup_f.assign((size_t)nq * c->dnum * M * c->alpha_pad, TwF{0.0, 0.0});
@@ -358,17 +359,26 @@ extern "C" int ckks_ctx_create(const ckks_params* p, ckks_ctx** out) {
 
     // the rescale constants once more, in the layout the transforms' division epilogue reads
     std::vector<u64> resc_ep((size_t)c->num_q * 2 * c->num_q, 0);
+    c->rescale_inv.assign((size_t)c->num_q * c->num_q, 0);
     for (u32 l = 0; l < c->num_q; l++)
         for (u32 i = 0; i < l; i++) {
             resc_ep[((size_t)l * 2 + 0) * c->num_q + i] = resc[((size_t)l * c->num_q + i) * 3 + 0];
+            c->rescale_inv[(size_t)l * c->num_q + i] = resc[((size_t)l * c->num_q + i) * 3 + 0];
             resc_ep[((size_t)l * 2 + 1) * c->num_q + i] = resc[((size_t)l * c->num_q + i) * 3 + 1];
         }
+
+    if (!rescale_conv_f.empty()) {  // -q_level^-1: the conversion constant of the form that has the division's last multiplication in it
+        rescale_neg_f.assign((size_t)c->num_q * c->num_q * 4, TwF{0.0, 0.0});
+        for (u32 l = 1; l < c->num_q; l++)
+            for (u32 i = 0; i < l; i++) rescale_neg_f[((size_t)l * c->num_q + i) * 4] = centred_twf(c->mod[i] - resc[((size_t)l * c->num_q + i) * 3], c->mod[i]);
+    }
 
     hipError_t e = hipSuccess;
     if (e == hipSuccess) e = upload(c->mc, &c->d_mc);
     if (e == hipSuccess) e = upload(resc_ep, &c->d_rescale_ep);
     if (e == hipSuccess) e = upload(rescale_prep_f, &c->d_rescale_prep_f);
     if (e == hipSuccess) e = upload(rescale_conv_f, &c->d_rescale_conv_f);
+    if (e == hipSuccess) e = upload(rescale_neg_f, &c->d_rescale_neg_f);
     if (e == hipSuccess) e = upload(tw, &c->d_tw);
     if (e == hipSuccess) e = upload(itw, &c->d_itw);
     if (e == hipSuccess) e = upload(twf, &c->d_twf);

@@ -130,6 +130,7 @@ struct ckks_ctx {
     bool small_q;        // every modulus is below 2^50: carry-free 25-bit-split accumulation applies
     u32 lazy_terms;      // how many products of two residues may be summed in 128 bits before a reduction
     std::vector<u64> mod, psi;
+    std::vector<u64> rescale_inv;  // [level][num_q]: q_level^-1 mod q_i, i < level
     std::vector<ModConst> mc;
 
     // device tables
@@ -157,6 +158,7 @@ struct ckks_ctx {
     TwF* d_moddown_rs_f = nullptr;    // [level][num_q][k2_pad]
     TwF* d_rescale_prep_f = nullptr;     // [M], by modulus: N^-1 mod q_m (the inverse transform in front of a fused rescale)
     TwF* d_rescale_conv_f = nullptr;     // [num_q][4]: (1, 1 / q_i), 0, 0, 0: the "conversion" of the one dropped limb
+    TwF* d_rescale_neg_f = nullptr;      // [level][num_q][4]: -q_level^-1 mod q_i, centred, 0, 0, 0: the same with the division's last multiplication in it
     u64* d_rescale_ep = nullptr;         // [level][2][num_q]: q_level^-1 mod q_i and its Shoup companion, as FwdEpilogue.cinv
     TwF* d_moddown_prep_f = nullptr;     // [M], by modulus: N^-1 (P/p_a)^-1 mod p_a at the special primes (zero elsewhere)
     TwF* d_moddown_rs_prep_f = nullptr;  // [level][M], by modulus: N^-1 (P q_l / m)^-1 mod m for m in {q_l, p_0..p_{k-1}}
@@ -260,6 +262,9 @@ hipError_t launch_ntt_modup(const ckks_ctx* c, u32 level, const double* y, size_
 u32 ntt_mid_modup(const ckks_ctx* c, u32 level, u32 n);
 u32 ntt_mid_moddown(const ckks_ctx* c, u32 level, bool merged, u32 polys, bool lo_done);
 u32 ntt_mid_rescale(const ckks_ctx* c, u32 level, u32 polys);
+// The rescale's share of the dropped limb, -NTT(y) q_level^-1 on the limbs of dst [batch][level][N] (y as for launch_ntt_rescale, through the inverse
+// transform's first pass): what is left of Rescale(c) is to add c_i q_level^-1, which the caller folds into the constants of what forms c.
+hipError_t launch_ntt_rescale_share(const ckks_ctx* c, u32 level, const double* y, u64* dst, u32 batch, hipStream_t st);
 bool ntt_rescale_one_launch(const ckks_ctx* c, u32 level, u32 polys);
 // contexts with a modulus of 2^50 or more, two-pass transforms: digits [n][beta][E][N], coefficient form (but each digit's own
 // limbs, which are not touched) -> evaluation form
@@ -369,10 +374,6 @@ hipError_t launch_lincomb2(const ckks_ctx* c, u32 level, const PtrList8& a, size
                            size_t b_cstride, const u64* kb, const u64* add, size_t add_bstride, u64* out, size_t out_bstride, u32 n,
                            hipStream_t st);
 // linear_mfma.hip, block.hip (ciphertexts of a vector at equal distances: ct and component strides in words, limbs N apart)
-// one residue per limb
-struct LimbScalars {
-    u64 v[CKKS_MAX_MODULI];
-};
 // which channels of a head turn together: pair j holds (j, j + n_pairs) or, interleaved, (2j, 2j + 1); pairs are numbered through the heads, z0 is the
 // launch's first
 struct RopePairs {
@@ -380,15 +381,30 @@ struct RopePairs {
     __host__ __device__ u32 first(u32 j) const { return interleaved ? 2 * j : j; }
     __host__ __device__ u32 second(u32 j) const { return interleaved ? 2 * j + 1 : j + n_pairs; }
 };
-hipError_t launch_linear_sum(const ckks_ctx* c, u32 level, u32 rows, const u64* in, size_t in_ct, size_t in_comp, u32 c_in, u32 c_out,
-                             const void* w, u32 weight_bytes, size_t w_out, size_t w_in, const u64* bias, u64 multiplier, u64* acc, u64* scratch,
-                             hipStream_t st);
+// one residue per limb
+struct LimbScalars {
+    u64 v[CKKS_MAX_MODULI];
+};
+// Sums over channels for one expert's rows, on limbs limb0 .. limb0 + limbs - 1:  acc = (add ? acc : 0) + mult * sum_c W in + bias_mult * bias (component 0)
+struct LinearSum {
+    const u64* in;                  // limb 0
+    size_t in_ct, in_comp, in_row;  // words
+    u32 rows, c_in, c_out;
+    const void* w;
+    u32 weight_bytes;
+    size_t w_out, w_in;
+    const u64* bias;                // [c_out][bias_limbs], or null
+    u32 bias_limbs, limb0, limbs, add;
+    u64* acc;                       // limb limb0 of the first output
+    size_t acc_ct, acc_comp, acc_row;
+    LimbScalars mult, bias_mult;    // by modulus
+};
+// scratch: linear_mfma_scratch_elems words where linear_mfma_applies; prepared: they hold this expert's weights from the call before
+hipError_t launch_linear_sum(const ckks_ctx* c, const LinearSum& S, u64* scratch, bool prepared, hipStream_t st);
 // linear_mfma.hip
-bool linear_mfma_applies(const ckks_ctx* c);
+bool linear_mfma_applies(const ckks_ctx* c, u32 c_in);
 size_t linear_mfma_scratch_elems(u32 c_in, u32 c_out, u32 weight_bytes);
-hipError_t launch_linear_mfma(const ckks_ctx* c, u32 level, u32 rows, const u64* in, size_t in_ct, size_t in_comp, size_t in_row, u32 c_in, u32 c_out,
-                              const void* w, u32 weight_bytes, size_t w_out, size_t w_in, const u64* bias, u64 multiplier, u64* acc, u64* scratch,
-                              hipStream_t st);
+hipError_t launch_linear_mfma(const ckks_ctx* c, const LinearSum& S, u64* scratch, bool prepared, hipStream_t st);
 // block.hip
 hipError_t launch_rope_turn(const ckks_ctx* c, u32 level, u32 n, const u64* in, size_t in_ct, size_t in_comp, const RopePairs& P, const u64* cs,
                             const u64* sn, u64* y, hipStream_t st);

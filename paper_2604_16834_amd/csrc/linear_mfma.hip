@@ -13,8 +13,13 @@
 //
 // A workgroup owns 64 (CT = 2) or 32 columns of one row, component and limb: it reads them once, for all channels, turns them into digits in LDS, and its
 // four waves take the 32-output tiles in turn, so X streams from HBM exactly once for any number of outputs.  Bound by HBM up to 64 x 64 channels (a column
-// is 8 (c_in + c_out) bytes against c_in c_out 7 DW digit products); two workgroups per CU, so that one's matrix instructions run under
-// the other's loads and folds.  More than 256 channels: launches that add to what the one before them left.
+// is 8 (c_in + 2 c_out) bytes with what is added to, against c_in c_out 7 DW digit products): 64 -> 64, 8-bit weights, two rows of 23 limbs at N = 2^16 2.4 ms,
+// 3.7 TB/s.  With 256 -> 192 channels and 32-bit weights (two rows of 12 limbs, 6.5 ms) the matrix pipe is busy 30 % and the vector units 34 % of the time, the two
+// workgroups of a CU load, multiply and fold in step.  Tried and slower there: one persistent workgroup of eight waves per CU, two of which read and convert the next
+// tile while six multiply (6.9 to 9 ms; 8-bit 64 -> 64 6.1 instead of 3.6 ms: too few loads in flight); four diagonals at a time with 64 accumulator registers and
+// three waves per SIMD (7.2 ms: spills).  More than 256 channels: launches that add to what the one before them left.
+#include <type_traits>
+
 #include "ctx.h"
 
 typedef int v4i __attribute__((ext_vector_type(4)));
@@ -24,6 +29,7 @@ typedef int v16i __attribute__((ext_vector_type(16)));
 #define LM_DX 7                      // digits of a residue
 #define LM_BIAS 0x0080808080808080ull
 #define LM_CHUNK 256                 // channels of a launch
+#define LM_KEEP_ORDER asm volatile("" ::: "memory"); __builtin_amdgcn_sched_barrier(0);
 
 // ---- weights -> digit planes in A-operand layout: wa[((ot*KS + ks)*DW + dw)*64 + lane] = 16 bytes, digit dw of
 //   W[32*ot + lane%32][32*ks + 16*(lane/32) + j], j < 16  (zero beyond c_out and c_in)
@@ -68,44 +74,44 @@ struct LinearMfmaArgs {
     const u64* in;
     size_t in_ct, in_comp, in_row;
     const uint4* wa;
-    const u64* bias;  // [c_out][limbs] or null
-    u64* acc;         // [row][c_out][2][limbs][N]
+    const u64* bias;
+    u64* acc;
+    size_t acc_ct, acc_comp, acc_row;
     const ModConstF* mcf;
-    u32 N, limbs, c_in, c_out, KS, OT, ot_per_wg, add;
+    u32 N, limb0, limbs, bias_limbs, c_in, c_out, KS, OT, ot_per_wg, add;
 };
 // per limb: K 2^(32 g) mod q, centred, g < 3, and the column sum's constant
 struct LinearConsts {
-    double c[4][CKKS_MAX_MODULI];
+    double c[4][CKKS_MAX_MODULI], bias[CKKS_MAX_MODULI];
 };
 
-template <u32 DW, u32 CT>
+template <u32 DW, u32 CT, bool ADD>
 __global__ __launch_bounds__(LM_THREADS, 2) void linear_mfma_kernel(LinearMfmaArgs A, LinearConsts K) {
     constexpr u32 DIAGS = LM_DX + DW - 1, GROUPS = (DIAGS + 3) / 4, COLS = 32 * CT, KG = LM_THREADS / COLS;  // KG groups of 16 channels at a time
     extern __shared__ uint4 lds[];  // [CT][KS][7][64], then the column sums
     const u32 tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const u32 KS = A.KS, N = A.N;
     u64* colsum = reinterpret_cast<u64*>(lds + CT * KS * LM_DX * 64);
-    const u32 e = blockIdx.y % A.limbs, comp = blockIdx.y / A.limbs;
+    const u32 er = blockIdx.y % A.limbs, e = A.limb0 + er, comp = blockIdx.y / A.limbs;
     const u32 n_split = (A.OT + A.ot_per_wg - 1) / A.ot_per_wg, row = blockIdx.z / n_split, ot_first = blockIdx.z % n_split * A.ot_per_wg;
     const u32 x0 = blockIdx.x * COLS;
     const u64* src = A.in + row * A.in_row + comp * A.in_comp + (size_t)e * N + x0;
+    u64* acc = A.acc + row * A.acc_row + comp * A.acc_comp + (size_t)er * N;
     if (DW > 1 && tid < COLS) colsum[tid] = 0;
     if (DW > 1) __syncthreads();
 
-    // the digits of all channels of the columns: thread (col, kg) takes 16 channels of a column
+    // the digits of all channels of the columns: thread (col, kg) takes groups of 16 channels of a column, two at a time (their 32 loads together)
     {
         const u32 col = tid & (COLS - 1), kg = tid / COLS;
         u64 total = 0;
-        for (u32 g0 = kg; g0 < 2 * KS; g0 += KG) {
-            u64 v[16];
+        auto request = [&](u32 g, u64* v) {
 #pragma unroll
-            for (u32 j = 0; j < 16; j++) {
-                const u32 ch = 16 * g0 + j;
-                v[j] = src[(ch < A.c_in ? ch : A.c_in - 1) * A.in_ct + col];
-            }
+            for (u32 j = 0; j < 16; j++) v[j] = src[(16 * g + j < A.c_in ? 16 * g + j : A.c_in - 1) * A.in_ct + col];
+        };
+        auto convert = [&](u32 g, u64* v) {
 #pragma unroll
             for (u32 j = 0; j < 16; j++)
-                if (16 * g0 + j >= A.c_in) v[j] = 0;
+                if (16 * g + j >= A.c_in) v[j] = 0;
             u32 w[8][4];
 #pragma unroll
             for (u32 m = 0; m < 4; m++) {
@@ -121,9 +127,20 @@ __global__ __launch_bounds__(LM_THREADS, 2) void linear_mfma_kernel(LinearMfmaAr
 #pragma unroll
                 for (u32 i = 0; i < 4; i++) w[i][m] = lo[i], w[4 + i][m] = hi[i];
             }
-            uint4* dst = lds + (((col >> 5) * KS + (g0 >> 1)) * LM_DX) * 64 + 32 * (g0 & 1) + (col & 31);
+            uint4* dst = lds + (((col >> 5) * KS + (g >> 1)) * LM_DX) * 64 + 32 * (g & 1) + (col & 31);
 #pragma unroll
             for (u32 dx = 0; dx < LM_DX; dx++) dst[dx * 64] = make_uint4(w[dx][0], w[dx][1], w[dx][2], w[dx][3]);
+        };
+        for (u32 g = kg; g < 2 * KS; g += 2 * KG) {
+            u64 v0[16], v1[16];
+            request(g, v0);
+            if (g + KG < 2 * KS) {
+                request(g + KG, v1);
+                convert(g, v0);
+                convert(g + KG, v1);
+            } else {
+                convert(g, v0);
+            }
         }
         if (DW > 1) atomicAdd(&colsum[col], total);  // whole numbers below 2^58: any order
     }
@@ -151,17 +168,16 @@ __global__ __launch_bounds__(LM_THREADS, 2) void linear_mfma_kernel(LinearMfmaAr
         for (u32 s = 0; s < DIAGS; s++)
 #pragma unroll
             for (u32 r = 0; r < 16; r++) d[s][r] = 0;
+        // A step's weights are requested a step ahead, in two register sets in turn; no memory operation moves across LM_KEEP_ORDER (left to itself the
+        // compiler requests them where they are used, a round trip to the L2 cache per step)
         const uint4* wa = A.wa + (size_t)ot * KS * DW * 64 + lane;
-        uint4 an[DW];
+        uint4 a0[DW], a1[DW];
+        auto weights = [&](u32 ks, uint4* a) {
+            const uint4* p = wa + min(ks, KS - 1) * (DW * 64);
 #pragma unroll
-        for (u32 dw = 0; dw < DW; dw++) an[dw] = wa[dw * 64];
-        for (u32 ks = 0; ks < KS; ks++) {
-            uint4 a[DW];
-#pragma unroll
-            for (u32 dw = 0; dw < DW; dw++) a[dw] = an[dw];
-            const u32 nx = ks + 1 < KS ? ks + 1 : ks;  // the next step's weights are requested a step ahead
-#pragma unroll
-            for (u32 dw = 0; dw < DW; dw++) an[dw] = wa[(nx * DW + dw) * 64];
+            for (u32 dw = 0; dw < DW; dw++) a[dw] = p[dw * 64];
+        };
+        auto multiply = [&](u32 ks, const uint4* a) {
             v4i b[LM_DX];
 #pragma unroll
             for (u32 dx = 0; dx < LM_DX; dx++) {
@@ -174,30 +190,61 @@ __global__ __launch_bounds__(LM_THREADS, 2) void linear_mfma_kernel(LinearMfmaAr
 #pragma unroll
                 for (u32 dx = 0; dx < LM_DX; dx++) d[dx + dw] = __builtin_amdgcn_mfma_i32_32x32x32_i8(av, b[dx], d[dx + dw], 0, 0, 0);
             }
+        };
+        weights(0, a0);
+        for (u32 ks = 0; ks < KS; ks += 2) {
+            if (DW == 4) { LM_KEEP_ORDER }
+            weights(ks + 1, a1);
+            if (DW == 4) { LM_KEEP_ORDER }
+            multiply(ks, a0);
+            if (DW == 4) { LM_KEEP_ORDER }
+            weights(ks + 2, a0);
+            if (DW == 4) { LM_KEEP_ORDER }
+            if (ks + 1 < KS) multiply(ks + 1, a1);
         }
+        // four rows at a time, what they are added to requested four rows ahead
+        auto at = [&](u32 r) { return 32 * ot + 8 * (r >> 2) + 4 * half + (r & 3); };
+        u64 old[2][4];
+        auto request = [&](u32 q) {
 #pragma unroll
-        for (u32 r = 0; r < 16; r++) {
-            const u32 o = 32 * ot + 8 * (r >> 2) + 4 * half + (r & 3);
+            for (u32 r = 0; r < 4; r++) {
+                const u32 o = at(4 * q + r);
+                old[q & 1][r] = acc[(o < A.c_out ? o : A.c_out - 1) * A.acc_ct + x];
+            }
+        };
+        auto finish = [&](auto whole) {  // the last operations of whole tiles without a branch
+            constexpr bool WHOLE = decltype(whole)::value;
+            if (ADD) request(0);
 #pragma unroll
-            for (u32 g = 0; g < GROUPS; g++) {
-                const u32 top = 4 * g + 3 < DIAGS ? 4 * g + 3 : DIAGS - 1;
-                double t = (double)d[top][r];
-                for (u32 s = top; s > 4 * g; s--) t = __builtin_fma(t, 256.0, (double)d[s - 1][r]);
-                part[g] = t;
+            for (u32 q = 0; q < 4; q++) {
+                if (ADD && q < 3) request(q + 1);
+#pragma unroll
+                for (u32 r = 4 * q; r < 4 * q + 4; r++) {
+                    const u32 o = at(r);
+#pragma unroll
+                    for (u32 g = 0; g < GROUPS; g++) {
+                        const u32 top = 4 * g + 3 < DIAGS ? 4 * g + 3 : DIAGS - 1;
+                        double t = (double)d[top][r];
+                        for (u32 s = top; s > 4 * g; s--) t = __builtin_fma(t, 256.0, (double)d[s - 1][r]);
+                        part[g] = t;
+                    }
+                    double v = DW > 1 ? f64m_dot_w<GROUPS + 1>(part, cw, m.q, m.qinv) : f64m_dot_w<GROUPS>(part, cw, m.q, m.qinv);
+                    if (!WHOLE && o >= A.c_out) continue;
+                    if (!WHOLE && A.bias && comp == 0)
+                        v = f64m_reduce(v + f64m_mulmod_any(f64m_from_u64(A.bias[(size_t)o * A.bias_limbs + e]), K.bias[e], m.q, m.qinv), m.q, m.qinv);
+                    if (ADD) v = f64m_reduce(v + f64m_from_u64(old[q & 1][r & 3]), m.q, m.qinv);
+                    acc[o * A.acc_ct + x] = f64m_canonical(v, m.q);
+                }
             }
-            if (o < A.c_out) {
-                u64* out = A.acc + ((((size_t)row * A.c_out + o) * 2 + comp) * A.limbs + e) * N + x;
-                double v = DW > 1 ? f64m_dot_w<GROUPS + 1>(part, cw, m.q, m.qinv) : f64m_dot_w<GROUPS>(part, cw, m.q, m.qinv);
-                if (A.add) v = f64m_reduce(v + f64m_from_u64(*out), m.q, m.qinv);
-                else if (A.bias && comp == 0) v = f64m_reduce(v + f64m_from_u64(A.bias[(size_t)o * A.limbs + e]), m.q, m.qinv);
-                *out = f64m_canonical(v, m.q);
-            }
-        }
+        };
+        if (DW == 4 && 32 * ot + 32 <= A.c_out && !(A.bias && comp == 0)) finish(std::integral_constant<bool, true>());
+        else finish(std::integral_constant<bool, false>());
     }
 }
 
-// The matrix-core kernel takes moduli below 2^50 and whole column tiles.
-bool linear_mfma_applies(const ckks_ctx* c) { return c->small_q && c->N >= 64; }
+// The matrix-core kernel takes moduli below 2^50, whole column tiles, and more channels than a chain of the vector kernel holds.
+#define LINEAR_F64_CHANNELS 8
+bool linear_mfma_applies(const ckks_ctx* c, u32 c_in) { return c->small_q && c->N >= 64 && c_in > LINEAR_F64_CHANNELS; }
 
 size_t linear_mfma_scratch_elems(u32 c_in, u32 c_out, u32 weight_bytes) {
     return (size_t)((c_out + 31) / 32) * ((c_in + 31) / 32) * weight_bytes * 64 * 2;
@@ -208,55 +255,60 @@ static hipError_t launch_linear_dw(const LinearMfmaArgs& A, const LinearConsts& 
     const u32 CT = A.KS <= 4 ? 2 : 1;
     const dim3 grid(A.N / (32 * CT), 2 * A.limbs, rows * n_split);
     const size_t lds = (size_t)CT * A.KS * LM_DX * 64 * 16 + 64 * 8;
-    if (CT == 2) hipLaunchKernelGGL((linear_mfma_kernel<DW, 2>), grid, dim3(LM_THREADS), lds, st, A, K);
-    else hipLaunchKernelGGL((linear_mfma_kernel<DW, 1>), grid, dim3(LM_THREADS), lds, st, A, K);
+#define LINEAR_MFMA(CT, ADD) hipLaunchKernelGGL((linear_mfma_kernel<DW, CT, ADD>), grid, dim3(LM_THREADS), lds, st, A, K)
+    if (CT == 2 && A.add) LINEAR_MFMA(2, true);
+    else if (CT == 2) LINEAR_MFMA(2, false);
+    else if (A.add) LINEAR_MFMA(1, true);
+    else LINEAR_MFMA(1, false);
+#undef LINEAR_MFMA
     return hipGetLastError();
 }
 
-// scratch: linear_mfma_scratch_elems words
-hipError_t launch_linear_mfma(const ckks_ctx* c, u32 level, u32 rows, const u64* in, size_t in_ct, size_t in_comp, size_t in_row, u32 c_in, u32 c_out,
-                              const void* w, u32 weight_bytes, size_t w_out, size_t w_in, const u64* bias, u64 multiplier, u64* acc, u64* scratch,
-                              hipStream_t st) {
-    const u32 limbs = level + 1;
+hipError_t launch_linear_mfma(const ckks_ctx* c, const LinearSum& S, u64* scratch, bool prepared, hipStream_t st) {
+    const u32 wb = S.weight_bytes;
     LinearConsts K;
     for (u32 i = 0; i < CKKS_MAX_MODULI; i++) {
-        const u64 q = i < limbs ? c->mod[i] : 3;
+        const u64 q = i < c->num_q ? c->mod[i] : 3;
         auto centred = [&](unsigned __int128 v) {
             const u64 r = (u64)(v % q);
             return r > q / 2 ? -(double)(q - r) : (double)r;
         };
-        unsigned __int128 k = multiplier % q;
+        unsigned __int128 k = S.mult.v[i] % q;
         u64 off = 0;  // what the digits leave out
-        for (u32 b = 0; b + 1 < weight_bytes; b++) off = off * 256 + 128;
+        for (u32 b = 0; b + 1 < wb; b++) off = off * 256 + 128;
         K.c[3][i] = centred(k * (off % q));
         for (u32 g = 0; g < 3; g++) {
             K.c[g][i] = centred(k);
             k = k * (((u64)1 << 32) % q) % q;
         }
+        K.bias[i] = centred(S.bias_mult.v[i]);
     }
-    for (u32 c0 = 0; c0 < c_in; c0 += LM_CHUNK) {
-        const u32 nc = c_in - c0 < LM_CHUNK ? c_in - c0 : LM_CHUNK;
-        const char* wc = (const char*)w + c0 * w_in * weight_bytes;
-        const u32 KS = (nc + 31) / 32, OT = (c_out + 31) / 32, prep = OT * KS * weight_bytes * 64;
-        uint4* wa = (uint4*)(scratch + linear_mfma_scratch_elems(c0, c_out, weight_bytes));
-        const dim3 pg((prep + LM_THREADS - 1) / LM_THREADS);
-        if (weight_bytes == 1) hipLaunchKernelGGL(linear_prep_kernel<int8_t>, pg, dim3(LM_THREADS), 0, st, (const int8_t*)wc, w_out, w_in, wa, c_out, nc, KS, OT);
-        else if (weight_bytes == 2) hipLaunchKernelGGL(linear_prep_kernel<int16_t>, pg, dim3(LM_THREADS), 0, st, (const int16_t*)wc, w_out, w_in, wa, c_out, nc, KS, OT);
-        else hipLaunchKernelGGL(linear_prep_kernel<int32_t>, pg, dim3(LM_THREADS), 0, st, (const int32_t*)wc, w_out, w_in, wa, c_out, nc, KS, OT);
+    for (u32 c0 = 0; c0 < S.c_in; c0 += LM_CHUNK) {
+        const u32 nc = S.c_in - c0 < LM_CHUNK ? S.c_in - c0 : LM_CHUNK;
+        const char* wc = (const char*)S.w + c0 * S.w_in * wb;
+        const u32 KS = (nc + 31) / 32, OT = (S.c_out + 31) / 32, prep = OT * KS * wb * 64;
+        uint4* wa = (uint4*)(scratch + linear_mfma_scratch_elems(c0, S.c_out, wb));
+        if (!prepared) {
+            const dim3 pg((prep + LM_THREADS - 1) / LM_THREADS);
+#define LINEAR_PREP(W) hipLaunchKernelGGL(linear_prep_kernel<W>, pg, dim3(LM_THREADS), 0, st, (const W*)wc, S.w_out, S.w_in, wa, S.c_out, nc, KS, OT)
+            if (wb == 1) LINEAR_PREP(int8_t);
+            else if (wb == 2) LINEAR_PREP(int16_t);
+            else LINEAR_PREP(int32_t);
+#undef LINEAR_PREP
+        }
         // outputs of a workgroup: all, unless that leaves the chip short of workgroups
         const u32 ct = KS <= 4 ? 2 : 1, step = 4 / ct;
-        const u64 wgs = (u64)(c->N / (32 * ct)) * 2 * limbs * rows;
+        const u64 wgs = (u64)(c->N / (32 * ct)) * 2 * S.limbs * S.rows;
         u32 n_split = wgs >= 1024 ? 1 : (u32)(1024 / wgs);
         u32 per = (OT + n_split - 1) / n_split;
         per = (per + step - 1) / step * step;
         n_split = (OT + per - 1) / per;
-        for (u32 r0 = 0; r0 < rows;) {  // the launch's third dimension holds 65535 workgroups
-            const u32 most = 65535 / n_split, n = rows - r0 < most ? rows - r0 : most;
-            const LinearMfmaArgs A = {in + r0 * in_row + c0 * in_ct, in_ct, in_comp, in_row, wa, bias, acc + (size_t)r0 * c_out * 2 * limbs * c->N, c->d_mcf,
-                                      c->N, limbs, nc, c_out, KS, OT, per, c0 ? 1u : 0u};
-            ProfScope ps__(c, K_WEIGHTED_SUM, st, 16.0 * n * c->N * limbs * (nc + (c0 ? 2.0 : 1.0) * c_out), 2.0 * n * c->N * limbs * nc * c_out);
-            hipError_t err = weight_bytes == 1 ? launch_linear_dw<1>(A, K, n, n_split, st)
-                                               : (weight_bytes == 2 ? launch_linear_dw<2>(A, K, n, n_split, st) : launch_linear_dw<4>(A, K, n, n_split, st));
+        for (u32 r0 = 0; r0 < S.rows;) {  // the launch's third dimension holds 65535 workgroups
+            const u32 most = 65535 / n_split, n = S.rows - r0 < most ? S.rows - r0 : most, add = c0 || S.add ? 1 : 0;
+            const LinearMfmaArgs A = {S.in + r0 * S.in_row + c0 * S.in_ct, S.in_ct, S.in_comp, S.in_row, wa, c0 ? nullptr : S.bias, S.acc + r0 * S.acc_row, S.acc_ct,
+                                      S.acc_comp, S.acc_row, c->d_mcf, c->N, S.limb0, S.limbs, S.bias_limbs, nc, S.c_out, KS, OT, per, add};
+            ProfScope ps__(c, K_WEIGHTED_SUM, st, 16.0 * n * c->N * S.limbs * (nc + (1.0 + add) * S.c_out), 2.0 * n * c->N * S.limbs * nc * S.c_out);
+            hipError_t err = wb == 1 ? launch_linear_dw<1>(A, K, n, n_split, st) : (wb == 2 ? launch_linear_dw<2>(A, K, n, n_split, st) : launch_linear_dw<4>(A, K, n, n_split, st));
             if (err != hipSuccess) return err;
             r0 += n;
         }

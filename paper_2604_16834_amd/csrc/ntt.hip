@@ -2685,6 +2685,23 @@ hipError_t launch_ntt_rescale(const ckks_ctx* c, u32 level, const double* y, u64
     return launch_ntt_any(c, false, dst, level, dst, level, pl, batch, st, nullptr, epilogue, nullptr, &cp, nullptr, nullptr, NTT_BOTH, mid_per ? &mp : nullptr);
 }
 
+hipError_t launch_ntt_rescale_share(const ckks_ctx* c, u32 level, const double* y, u64* dst, u32 batch, hipStream_t st) {
+    if (level == 0 || !c->d_rescale_neg_f) return hipErrorInvalidValue;
+    ConvPrologue cp = {};
+    cp.y = y;
+    cp.y_bstride = c->N;
+    cp.convf = c->d_rescale_neg_f + (size_t)level * c->num_q * 4;
+    cp.nd = 1;
+    cp.ap = 4;
+    PolyList pl;
+    for (u32 a = 0; a < CKKS_MAX_MODULI; a++) pl.spos[a] = pl.dpos[a] = pl.mod[a] = (unsigned char)(a < level ? a : 0);
+    pl.n = level;
+    const MidPrologue mp = {c->d_itwf, c->d_itwf_val, c->d_rescale_prep_f, level, level};
+    cp.per = mid_conv_per_of(c, 1, 4, level, batch);
+    if (!cp.per) return hipErrorInvalidValue;  // a single source limb always goes through its second pass there
+    return launch_ntt_any(c, false, dst, level, dst, level, pl, batch, st, nullptr, nullptr, nullptr, &cp, nullptr, nullptr, NTT_BOTH, &mp);
+}
+
 hipError_t launch_ntt_lo_mac(const ckks_ctx* c, u32 level, const DigitSrc& digits, const u64* const* keys, u64* const* outs, u32 n,
                              hipStream_t st, u32 inv_from, const MacProduct* prod, const MacRotate* rot, u32* n_part, const MacDivide* div, bool dropped_only) {
     if ((div || dropped_only) && (n_part || inv_from == 0 || inv_from >= c->ext_limbs(level) || (!prod && !rot))) return hipErrorInvalidValue;
