@@ -2203,13 +2203,29 @@ static int rope_check(const ckks_ctx* c, const he_rope_desc* d) {
     if (!d) return set_err(c, CKKS_ERR_INVALID_ARG, "null descriptor");
     if (d->n_heads == 0 || d->head_dim == 0 || d->n_heads > 65536 || d->head_dim > 65536 || d->n_pairs > d->head_dim / 2)
         return set_err(c, CKKS_ERR_INVALID_ARG, "heads, channels or pairs out of range");
+    if ((u64)d->n_heads * d->head_dim > (u64)1 << 24) return set_err(c, CKKS_ERR_INVALID_ARG, "too many channels");
     if (!level_ok(c, d->level) || d->level < 1) return set_err(c, CKKS_ERR_LEVEL_MISMATCH, "rotary positions need 1 <= level < num_q");
     return CKKS_OK;
 }
-#define ROPE_BATCH (CT_BATCH / 2)  // pairs whose sums are rescaled together
+// The products of whole batches of pairs are rescaled from the workspace where that is one launch of the small rings' rescale, and with moduli of 2^50 and more; elsewhere
+// only their dropped limb is stored, and the others are formed by the pass that ends the division (launch_ntt_rescale_vec), as many pairs at a time as the bytes below hold
+// converted limbs of.  Stored / formed at the end in us: 64 channels of 24 limbs at N = 2^16 2216 / 1576
+#define ROPE_BATCH (CT_BATCH / 2)  // pairs whose products are stored and rescaled together
+#define ROPE_CONV_BYTES ((size_t)512 << 20)
+static bool rope_stored(const ckks_ctx* c, const he_rope_desc* d) {
+    const u64 pairs = (u64)d->n_heads * d->n_pairs;
+    return !ntt_has_modup(c) || (pairs <= ROPE_BATCH && ntt_rescale_one_launch(c, d->level, 4 * (u32)pairs));
+}
+static u32 rope_batch(const ckks_ctx* c, const he_rope_desc* d) {
+    const u64 pairs = (u64)d->n_heads * d->n_pairs, fit = rope_stored(c, d) ? ROPE_BATCH : ROPE_CONV_BYTES / ((size_t)32 * d->level * c->N);
+    const u64 n = fit < 1 ? 1 : (fit > 512 ? 512 : fit);  // (the transforms' launches number the components in 16 bits)
+    return (u32)(n < pairs ? n : (pairs ? pairs : 1));
+}
 size_t he_rope_workspace_bytes(const ckks_ctx* c, const he_rope_desc* d) {
     if (!c || rope_check(c, d)) return 0;
-    return blk((size_t)2 * ROPE_BATCH * 2 * (d->level + 1) * c->N) + ws_rescale(c, d->level, 2 * ROPE_BATCH);
+    const size_t n = rope_batch(c, d);
+    if (!rope_stored(c, d)) return blk(4 * n * c->N) + blk(4 * n * d->level * c->N);
+    return blk(n * 4 * (d->level + 1) * c->N) + ws_rescale(c, d->level, (u32)(2 * n));
 }
 
 int he_rope_axes(const ckks_ctx* c, const he_rope_desc* d, const he_ct_array* in, const uint64_t* d_cos, const uint64_t* d_sin,
@@ -2224,14 +2240,23 @@ int he_rope_axes(const ckks_ctx* c, const he_rope_desc* d, const he_ct_array* in
     hipStream_t st = (hipStream_t)stream;
     const size_t N = c->N, ct = (size_t)2 * L1 * N, out_ct = (size_t)2 * level * N;
     Arena ar(d_ws, ws_bytes);
-    u64* y = ar.take((size_t)2 * ROPE_BATCH * ct);
+    const bool stored = rope_stored(c, d);
+    const u32 batch = rope_batch(c, d);
+    u64* y = ar.take(stored ? (size_t)2 * batch * ct : (size_t)4 * batch * N);
+    u64* w = stored ? nullptr : ar.take((size_t)4 * batch * level * N);
     RopePairs P = {d->head_dim, d->n_pairs, d->interleaved ? 1u : 0u, d->inverse ? 1u : 0u, 0};
     const u64 pairs = (u64)d->n_heads * d->n_pairs, rest = (u64)d->n_heads * (d->head_dim - 2 * d->n_pairs);
-    if (pairs >> 32 || rest >> 32) return set_err(c, CKKS_ERR_INVALID_ARG, "too many channels");
-    for (u64 z0 = 0; z0 < pairs; z0 += ROPE_BATCH) {
-        const u32 n = pairs - z0 < ROPE_BATCH ? (u32)(pairs - z0) : ROPE_BATCH;
+    for (u64 z0 = 0; z0 < pairs; z0 += batch) {
+        const u32 n = pairs - z0 < batch ? (u32)(pairs - z0) : batch;
         P.z0 = (u32)z0;
-        HIP_TRY(launch_rope_turn(c, level, n, (const u64*)in->d, in->ct_stride, in->comp_stride, P, (const u64*)d_cos, (const u64*)d_sin, y, st));
+        HIP_TRY(launch_rope_turn(c, level, stored ? 0 : level, n, (const u64*)in->d, in->ct_stride, in->comp_stride, P, (const u64*)d_cos, (const u64*)d_sin, y, st));
+        if (!stored) {
+            HIP_TRY(launch_ntt(c, true, y, 1, y, 1, range_list(0, 1, level), 4 * n, st, nullptr, nullptr, c->d_rescale_prep_f, nullptr, nullptr, NTT_LO));
+            const VecEpilogue ve = {(const u64*)in->d, in->ct_stride, in->comp_stride, (const u64*)d_cos, (const u64*)d_sin, (size_t)L1 * N, (u64*)d_out, out_ct,
+                                    c->d_rescale_ep + (size_t)level * 2 * c->num_q, level, P};
+            HIP_TRY(launch_ntt_rescale_vec(c, level, VEC_TURN, (const double*)y, w, 4 * n, ve, st));
+            continue;
+        }
         const u64* src[2 * ROPE_BATCH];
         u64* dst[2 * ROPE_BATCH];
         for (u32 b = 0; b < n; b++) {
@@ -2383,7 +2408,7 @@ int he_norm_gate(const ckks_ctx* c, const he_norm_desc* d, const int64_t* h_k_ne
         } else {
             ts = (size_t)level * N;
             if (d->gate == HE_GATE_PLAIN) {
-                HIP_TRY(launch_gate_mul(c, level, n, px[0], x->ct_stride, x->comp_stride, pg[0], gate->ct_stride, tmp, st));
+                HIP_TRY(launch_gate_mul(c, level, 0, n, px[0], x->ct_stride, x->comp_stride, pg[0], gate->ct_stride, tmp, st));
                 for (u32 b0 = 0; b0 < n; b0 += CT_BATCH)
                     if ((rc = run_rescale(c, level, ptmp + b0, L1 * N, ot + b0, n - b0 < CT_BATCH ? n - b0 : CT_BATCH, ar.rest(), st))) return rc;
             } else if ((rc = run_ctct_merged(c, level, px, x->comp_stride, pg, gate->comp_stride, nullptr, 0, rlk->d_key, ot, n, ar.rest(), st))) {

@@ -139,31 +139,31 @@ hipError_t launch_linear_sum(const ckks_ctx* c, const LinearSum& S, u64* scratch
 }
 
 // ---- rotation of channel pairs ----------------------------------------------------------------------------
-// pair z: y_a = a C - b S, y_b = a S + b C on limbs 0 .. level (S negated for the inverse); y [2 pairs][2][level + 1][N]: y_a, y_b of each
+// pair z: y_a = a C - b S, y_b = a S + b C on limbs limb0 .. level (S negated for the inverse); y [2 pairs][2][limbs][N]: y_a, y_b of each
 __global__ __launch_bounds__(BK_THREADS) void rope_turn_kernel(const u64* __restrict__ in, size_t in_ct, size_t in_comp, RopePairs P,
                                                                const u64* __restrict__ cs, const u64* __restrict__ sn, u64* __restrict__ y,
-                                                               const ModConst* __restrict__ mc, u32 N, u32 limbs) {
+                                                               const ModConst* __restrict__ mc, u32 N, u32 limb0, u32 limbs) {
     const u32 x = blockIdx.x * BK_THREADS + threadIdx.x;
     if (x >= N) return;
-    const u32 e = blockIdx.y % limbs, comp = blockIdx.y / limbs, z = P.z0 + blockIdx.z;
+    const u32 er = blockIdx.y % limbs, e = limb0 + er, comp = blockIdx.y / limbs, z = P.z0 + blockIdx.z;
     const u32 j = z % P.n_pairs;
-    const size_t head = (size_t)(z / P.n_pairs) * P.head_dim, at = comp * in_comp + (size_t)e * N + x, table = ((size_t)j * limbs + e) * N + x;
+    const size_t head = (size_t)(z / P.n_pairs) * P.head_dim, at = comp * in_comp + (size_t)e * N + x, table = ((size_t)j * (limb0 + limbs) + e) * N + x;
     const ModConst m = mc[e];
     const u64 a = in[(head + P.first(j)) * in_ct + at], b = in[(head + P.second(j)) * in_ct + at];
     const u64 c0 = cs[table], sv = sn[table], s0 = P.inverse && sv ? m.q - sv : sv;
     const u64 ya = sub_mod(mulmod_barrett(a, c0, m), mulmod_barrett(b, s0, m), m.q);
     const u64 yb = add_mod(mulmod_barrett(a, s0, m), mulmod_barrett(b, c0, m), m.q);
-    const size_t out = ((size_t)blockIdx.z * 2 * 2 + comp) * limbs * N + (size_t)e * N + x;
+    const size_t out = ((size_t)blockIdx.z * 2 * 2 + comp) * limbs * N + (size_t)er * N + x;
     y[out] = ya;
     y[out + (size_t)2 * limbs * N] = yb;
 }
 
-hipError_t launch_rope_turn(const ckks_ctx* c, u32 level, u32 n, const u64* in, size_t in_ct, size_t in_comp, const RopePairs& P, const u64* cs,
+hipError_t launch_rope_turn(const ckks_ctx* c, u32 level, u32 limb0, u32 n, const u64* in, size_t in_ct, size_t in_comp, const RopePairs& P, const u64* cs,
                             const u64* sn, u64* y, hipStream_t st) {
-    const u32 limbs = level + 1;
+    const u32 limbs = level + 1 - limb0;
     const dim3 grid((c->N + BK_THREADS - 1) / BK_THREADS, 2 * limbs, n);
     ProfScope ps__(c, K_PTCT_MAC, st, 8.0 * c->N * limbs * n * 10.0, 8.0 * c->N * limbs * n);
-    hipLaunchKernelGGL(rope_turn_kernel, grid, dim3(BK_THREADS), 0, st, in, in_ct, in_comp, P, cs, sn, y, c->d_mc, c->N, limbs);
+    hipLaunchKernelGGL(rope_turn_kernel, grid, dim3(BK_THREADS), 0, st, in, in_ct, in_comp, P, cs, sn, y, c->d_mc, c->N, limb0, limbs);
     return hipGetLastError();
 }
 
@@ -246,22 +246,22 @@ hipError_t launch_affine(const ckks_ctx* c, u32 level, const u64* ct, size_t ct_
 
 // out_z[comp][e] = gate_z[e] * ct_z[comp][e]; ciphertexts and plaintexts at equal distances, out compact
 __global__ __launch_bounds__(BK_THREADS) void gate_mul_kernel(const u64* __restrict__ ct, size_t ct_stride, size_t ct_comp, const u64* __restrict__ gate,
-                                                              size_t gate_stride, u64* __restrict__ out, const ModConst* __restrict__ mc, u32 N, u32 limbs) {
+                                                              size_t gate_stride, u64* __restrict__ out, const ModConst* __restrict__ mc, u32 N, u32 limb0) {
     const u32 x = blockIdx.x * BK_THREADS + threadIdx.x;
     if (x >= N) return;
-    const u32 e = blockIdx.y, z = blockIdx.z;
+    const u32 limbs = gridDim.y, e = limb0 + blockIdx.y, z = blockIdx.z;
     const ModConst m = mc[e];
     const size_t row = (size_t)e * N + x;
     const u64 g = gate[z * gate_stride + row];
 #pragma unroll
     for (u32 comp = 0; comp < 2; comp++)
-        out[((size_t)z * 2 + comp) * limbs * N + row] = mulmod_barrett(ct[z * ct_stride + comp * ct_comp + row], g, m);
+        out[(((size_t)z * 2 + comp) * limbs + blockIdx.y) * N + x] = mulmod_barrett(ct[z * ct_stride + comp * ct_comp + row], g, m);
 }
 
-hipError_t launch_gate_mul(const ckks_ctx* c, u32 level, u32 n, const u64* ct, size_t ct_stride, size_t ct_comp, const u64* gate, size_t gate_stride,
+hipError_t launch_gate_mul(const ckks_ctx* c, u32 level, u32 limb0, u32 n, const u64* ct, size_t ct_stride, size_t ct_comp, const u64* gate, size_t gate_stride,
                            u64* out, hipStream_t st) {
-    const dim3 grid((c->N + BK_THREADS - 1) / BK_THREADS, level + 1, n);
-    ProfScope ps__(c, K_MASK_MUL, st, 40.0 * n * c->N * (level + 1.0), 2.0 * n * c->N * (level + 1.0));
-    hipLaunchKernelGGL(gate_mul_kernel, grid, dim3(BK_THREADS), 0, st, ct, ct_stride, ct_comp, gate, gate_stride, out, c->d_mc, c->N, level + 1);
+    const dim3 grid((c->N + BK_THREADS - 1) / BK_THREADS, level + 1 - limb0, n);
+    ProfScope ps__(c, K_MASK_MUL, st, 40.0 * n * c->N * (level + 1.0 - limb0), 2.0 * n * c->N * (level + 1.0 - limb0));
+    hipLaunchKernelGGL(gate_mul_kernel, grid, dim3(BK_THREADS), 0, st, ct, ct_stride, ct_comp, gate, gate_stride, out, c->d_mc, c->N, limb0);
     return hipGetLastError();
 }

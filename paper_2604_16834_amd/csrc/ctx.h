@@ -265,6 +265,29 @@ u32 ntt_mid_rescale(const ckks_ctx* c, u32 level, u32 polys);
 // The rescale's share of the dropped limb, -NTT(y) q_level^-1 on the limbs of dst [batch][level][N] (y as for launch_ntt_rescale, through the inverse
 // transform's first pass): what is left of Rescale(c) is to add c_i q_level^-1, which the caller folds into the constants of what forms c.
 hipError_t launch_ntt_rescale_share(const ckks_ctx* c, u32 level, const double* y, u64* dst, u32 batch, hipStream_t st);
+// which channels of a head turn together: pair j holds (j, j + n_pairs) or, interleaved, (2j, 2j + 1); pairs are numbered through the heads, z0 is the
+// launch's first
+struct RopePairs {
+    u32 head_dim, n_pairs, interleaved, inverse, z0;
+    __host__ __device__ u32 first(u32 j) const { return interleaved ? 2 * j : j; }
+    __host__ __device__ u32 second(u32 j) const { return interleaved ? 2 * j + 1 : j + n_pairs; }
+};
+// Rescales of products with plaintexts (ntt_fwd_lo_vec_kernel): the limbs behind the dropped one formed from ciphertexts at equal distances and plaintexts p_stride
+// apart; out_ct words between outputs, out [2][level][N].  y: the dropped limbs of the products, [batch][N], through the inverse transform's first pass with
+// d_rescale_prep_f; w [batch][level][N] scratch.  batch: components, numbered as the kernel says.  Contexts with ntt_has_modup.
+enum VecMode { VEC_TURN = 0, VEC_GATE };
+struct VecEpilogue {
+    const u64* in;
+    size_t in_ct, in_comp;
+    const u64 *p0, *p1;
+    size_t p_stride;
+    u64* out;
+    size_t out_ct;
+    const u64* cinv;  // q_level^-1 by limb
+    u32 level;
+    RopePairs P;
+};
+hipError_t launch_ntt_rescale_vec(const ckks_ctx* c, u32 level, VecMode mode, const double* y, u64* w, u32 batch, const VecEpilogue& ve, hipStream_t st);
 bool ntt_rescale_one_launch(const ckks_ctx* c, u32 level, u32 polys);
 // contexts with a modulus of 2^50 or more, two-pass transforms: digits [n][beta][E][N], coefficient form (but each digit's own
 // limbs, which are not touched) -> evaluation form
@@ -374,13 +397,6 @@ hipError_t launch_lincomb2(const ckks_ctx* c, u32 level, const PtrList8& a, size
                            size_t b_cstride, const u64* kb, const u64* add, size_t add_bstride, u64* out, size_t out_bstride, u32 n,
                            hipStream_t st);
 // linear_mfma.hip, block.hip (ciphertexts of a vector at equal distances: ct and component strides in words, limbs N apart)
-// which channels of a head turn together: pair j holds (j, j + n_pairs) or, interleaved, (2j, 2j + 1); pairs are numbered through the heads, z0 is the
-// launch's first
-struct RopePairs {
-    u32 head_dim, n_pairs, interleaved, inverse, z0;
-    __host__ __device__ u32 first(u32 j) const { return interleaved ? 2 * j : j; }
-    __host__ __device__ u32 second(u32 j) const { return interleaved ? 2 * j + 1 : j + n_pairs; }
-};
 // one residue per limb
 struct LimbScalars {
     u64 v[CKKS_MAX_MODULI];
@@ -406,7 +422,8 @@ bool linear_mfma_applies(const ckks_ctx* c, u32 c_in);
 size_t linear_mfma_scratch_elems(u32 c_in, u32 c_out, u32 weight_bytes);
 hipError_t launch_linear_mfma(const ckks_ctx* c, const LinearSum& S, u64* scratch, bool prepared, hipStream_t st);
 // block.hip
-hipError_t launch_rope_turn(const ckks_ctx* c, u32 level, u32 n, const u64* in, size_t in_ct, size_t in_comp, const RopePairs& P, const u64* cs,
+// limbs limb0 .. level of the products: y [2 n][2][level + 1 - limb0][N]
+hipError_t launch_rope_turn(const ckks_ctx* c, u32 level, u32 limb0, u32 n, const u64* in, size_t in_ct, size_t in_comp, const RopePairs& P, const u64* cs,
                             const u64* sn, u64* y, hipStream_t st);
 hipError_t launch_rope_pass(const ckks_ctx* c, u32 level, u32 n, const u64* in, size_t in_ct, size_t in_comp, const RopePairs& P, u64* out,
                             hipStream_t st);
@@ -414,5 +431,6 @@ hipError_t launch_square_sum(const ckks_ctx* c, u32 level, const u64* in, size_t
                              hipStream_t st);
 hipError_t launch_affine(const ckks_ctx* c, u32 level, const u64* ct, size_t ct_comp, const LimbScalars& k, const LimbScalars& add, u64* out,
                          hipStream_t st);
-hipError_t launch_gate_mul(const ckks_ctx* c, u32 level, u32 n, const u64* ct, size_t ct_stride, size_t ct_comp, const u64* gate, size_t gate_stride,
+// limbs limb0 .. level: out [n][2][level + 1 - limb0][N]
+hipError_t launch_gate_mul(const ckks_ctx* c, u32 level, u32 limb0, u32 n, const u64* ct, size_t ct_stride, size_t ct_comp, const u64* gate, size_t gate_stride,
                            u64* out, hipStream_t st);

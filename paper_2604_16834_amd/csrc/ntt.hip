@@ -659,6 +659,107 @@ __global__ __launch_bounds__(NTT_THREADS) void ntt_fwd_lo_div_kernel(NttArgs arg
     div_store<A, EM>(args, ep, i, pl_at(pl.mod, tile.a), b, off, tid, lds1, P.mc, O);
 }
 
+// The same end of a rescale for products with plaintexts, whose limbs are formed from their operands as they are needed and not stored before: out = (v - w) cinv,
+//   MODE VEC_TURN: item 4 z + 2 side + comp is channel first(j) (side 0: v = a C_j - b S_j) or second(j) (side 1: v = a S_j + b C_j) of pair z = z0 + .., (a, b) the pair
+//   MODE VEC_GATE: item 2 z + comp: v = G_z (.) x_z
+// (residues below 2^50; operands are requested a round ahead like div_request's; the items of a slice, which share them, are on one die: lo_tile)
+template <int MODE>
+__global__ __launch_bounds__(NTT_THREADS) void ntt_fwd_lo_vec_kernel(NttArgs args, PolyList pl, VecEpilogue ve) {
+    typedef ArithF64 A;
+    typedef ArithF64W AR;
+    __shared__ double lds0[LDS_PADDED_WORDS];
+    __shared__ double lds1[LDS_PADDED_WORDS];
+    const u32 tid = threadIdx.x;
+    const LoTile tile = lo_tile(args.log_hi, args.lo_group);
+    const u32 blk = tile.blk, b = tile.b;
+    const PolyRef<A> P = poly_ref<A>(args, pl, b, tile.a);
+    const size_t off = (size_t)blk << 11;
+    const u32 TA = (1u << args.log_hi) + blk;
+    const u32 d3 = tid >> 5, x5 = tid & 31, d2 = (tid >> 2) & 7, d0 = tid & 3;
+    double v[8], wa[7], wb[7], wc[7], wd[6];
+    u64 raw[8];
+    load_tw_w<3>(P.tw_val, TA, wa);
+    load_tw_w<3>(P.tw_val, 8 * TA + d3, wb);
+#pragma unroll
+    for (int j = 0; j < 8; j++) raw[j] = P.src[off + tid + 256 * j];
+#pragma unroll
+    for (int j = 0; j < 8; j++) v[j] = A::load_second(raw[j], P.mc);
+    A::fwd_begin(v, P.mc);
+    fwd_rows_pre<AR, 3>(v, wa, P.mc);
+    load_tw_w<3>(P.tw_val, 64 * TA + 8 * d3 + d2, wc);
+#pragma unroll
+    for (int j = 0; j < 8; j++) lds0[LDS_PAD(tid + 256 * j)] = v[j];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 8; j++) v[j] = lds0[LDS_PAD(d3 * 256 + 32 * j + x5)];
+    A::fwd_begin(v, P.mc);
+    fwd_rows_pre<AR, 3>(v, wb, P.mc);
+    load_tw_w<2>(P.tw_val, 512 * TA + 2 * tid, wd);
+    load_tw_w<2>(P.tw_val, 512 * TA + 2 * tid + 1, wd + 3);
+#pragma unroll
+    for (int j = 0; j < 8; j++) lds1[LDS_PAD(d3 * 256 + 32 * j + x5)] = v[j];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 8; j++) v[j] = lds1[LDS_PAD(d3 * 256 + d2 * 32 + 4 * j + d0)];
+    A::fwd_begin(v, P.mc);
+    fwd_rows_pre<AR, 3>(v, wc, P.mc);
+#pragma unroll
+    for (int j = 0; j < 8; j++) lds0[LDS_PAD(d3 * 256 + d2 * 32 + 4 * j + d0)] = v[j];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 8; j++) v[j] = lds0[LDS_PAD(8 * tid + j)];
+    // the operands
+    const u32 i = pl_at(pl.dpos, tile.a), comp = b & 1;
+    const size_t row = ((size_t)i << args.log_n) + off + tid;
+    const u64 *x0, *x1 = nullptr, *p0, *p1 = nullptr;
+    u64* out = ve.out + ((size_t)(comp * ve.level + i) << args.log_n) + off + tid;
+    bool minus = false;
+    if constexpr (MODE == VEC_TURN) {  // x0 p0 +- x1 p1: the channel itself times the cosine, its partner times the sine
+        const u32 z = ve.P.z0 + (b >> 2), j = z % ve.P.n_pairs, side = (b >> 1) & 1;
+        const size_t head = (size_t)(z / ve.P.n_pairs) * ve.P.head_dim;
+        const size_t own = head + (side ? ve.P.second(j) : ve.P.first(j)), other = head + (side ? ve.P.first(j) : ve.P.second(j));
+        x0 = ve.in + own * ve.in_ct + comp * ve.in_comp + row;
+        x1 = ve.in + other * ve.in_ct + comp * ve.in_comp + row;
+        p0 = ve.p0 + j * ve.p_stride + row;
+        p1 = ve.p1 + j * ve.p_stride + row;
+        out += own * ve.out_ct;
+        minus = (side == 0) != (ve.P.inverse != 0);
+    } else {
+        const size_t z = b >> 1;
+        x0 = ve.in + z * ve.in_ct + comp * ve.in_comp + row;
+        p0 = ve.p0 + z * ve.p_stride + row;
+        out += z * ve.out_ct;
+    }
+    u64 o0[8], o1[8], q0[8], q1[8];
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+        o0[j] = x0[256 * j];
+        q0[j] = p0[256 * j];
+        if constexpr (MODE == VEC_TURN) {
+            o1[j] = x1[256 * j];
+            q1[j] = p1[256 * j];
+        }
+    }
+    fwd_rows_pre<AR, 2>(v, wd, P.mc);
+    fwd_rows_pre<AR, 2>(v + 4, wd + 3, P.mc);
+    A::fwd_end(v, P.mc);
+    // back through LDS so that a wave stores 512 contiguous bytes per instruction
+#pragma unroll
+    for (int j = 0; j < 8; j++) lds1[LDS_PAD(8 * tid + j)] = v[j];
+    __syncthreads();
+    const double q = P.mc.q, qinv = P.mc.qinv, cinv = A::from_u64(ve.cinv[i]), cinvq = cinv / q;
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+        double s = A::mulmod_any(A::from_u64(o0[j]), A::from_u64(q0[j]), q, qinv);
+        if constexpr (MODE == VEC_TURN) {
+            const double t = A::mulmod_any(A::from_u64(o1[j]), A::from_u64(q1[j]), q, qinv);
+            s = minus ? s - t : s + t;  // below 1.5 q
+        }
+        const double r = A::mulmod(A::reduce(s - lds1[LDS_PAD(tid + 256 * j)], P.mc), cinv, cinvq, q);
+        out[256 * j] = A::canonical(A::reduce(r, P.mc), P.mc);
+    }
+}
+
 // The lo pass of ModUp's forward transforms with the inner product with the switching key in place of its stores.
 // A workgroup owns one 2^11-point slice of one position e of the extended basis of one batch item: it transforms that
 // slice of every digit whose limb e went through the converting hi pass (all live digits but the one e belongs to; the
@@ -2700,6 +2801,42 @@ hipError_t launch_ntt_rescale_share(const ckks_ctx* c, u32 level, const double* 
     cp.per = mid_conv_per_of(c, 1, 4, level, batch);
     if (!cp.per) return hipErrorInvalidValue;  // a single source limb always goes through its second pass there
     return launch_ntt_any(c, false, dst, level, dst, level, pl, batch, st, nullptr, nullptr, nullptr, &cp, nullptr, nullptr, NTT_BOTH, &mp);
+}
+
+hipError_t launch_ntt_rescale_vec(const ckks_ctx* c, u32 level, VecMode mode, const double* y, u64* w, u32 batch, const VecEpilogue& ve, hipStream_t st) {
+    if (level == 0 || !ntt_has_modup(c)) return hipErrorInvalidValue;
+    ConvPrologue cp = {};
+    cp.y = y;
+    cp.y_bstride = c->N;
+    cp.convf = c->d_rescale_conv_f;
+    cp.nd = 1;
+    cp.ap = 4;
+    PolyList pl;
+    for (u32 a = 0; a < CKKS_MAX_MODULI; a++) pl.spos[a] = pl.dpos[a] = pl.mod[a] = (unsigned char)(a < level ? a : 0);
+    pl.n = level;
+    const MidPrologue mp = {c->d_itwf, c->d_itwf_val, c->d_rescale_prep_f, level, level};
+    cp.per = mid_conv_per_of(c, 1, 4, level, batch);
+    if (!cp.per) return hipErrorInvalidValue;  // a single source limb always goes through its second pass there
+    if (hipError_t e = launch_ntt_any(c, false, w, level, w, level, pl, batch, st, nullptr, nullptr, nullptr, &cp, nullptr, nullptr, NTT_HI, &mp); e != hipSuccess) return e;
+    NttArgs args = {};
+    args.src = args.dst = w;
+    args.src_bstride = args.dst_bstride = level;
+    args.mc = c->d_mcf;
+    args.tw = c->d_twf;
+    args.tw_val = c->d_twf_val;
+    args.log_n = c->log_n;
+    args.log_lo = c->log_lo;
+    args.log_hi = c->log_hi;
+    args.last = 1;
+    args.batch = batch;
+    const u32 slices = level << c->log_hi;
+    for (u32 g = 64; g >= 8; g >>= 1)
+        if (slices % g == 0) { args.lo_group = g; break; }
+    const dim3 grid = args.lo_group ? dim3(args.lo_group, batch, slices / args.lo_group) : dim3(batch, slices);
+    ProfScope ps__(c, K_NTT_FWD_LO, st, (mode == VEC_TURN ? 36.0 : 28.0) * batch * level * c->N, 0.5 * batch * level * c->N * c->log_lo);
+    if (mode == VEC_TURN) hipLaunchKernelGGL(ntt_fwd_lo_vec_kernel<VEC_TURN>, grid, dim3(NTT_THREADS), 0, st, args, pl, ve);
+    else hipLaunchKernelGGL(ntt_fwd_lo_vec_kernel<VEC_GATE>, grid, dim3(NTT_THREADS), 0, st, args, pl, ve);
+    return hipGetLastError();
 }
 
 hipError_t launch_ntt_lo_mac(const ckks_ctx* c, u32 level, const DigitSrc& digits, const u64* const* keys, u64* const* outs, u32 n,
