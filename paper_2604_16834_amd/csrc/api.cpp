@@ -2209,7 +2209,8 @@ static int rope_check(const ckks_ctx* c, const he_rope_desc* d) {
 }
 // The products of whole batches of pairs are rescaled from the workspace where that is one launch of the small rings' rescale, and with moduli of 2^50 and more; elsewhere
 // only their dropped limb is stored, and the others are formed by the pass that ends the division (launch_ntt_rescale_vec), as many pairs at a time as the bytes below hold
-// converted limbs of.  Stored / formed at the end in us: 64 channels of 24 limbs at N = 2^16 2216 / 1576
+// converted limbs of.  Stored / formed at the end in us: eight channels of 4 limbs at N = 2^12 16.5 / 26, 42 of 10 limbs at 2^14 236 / 115, 64
+// of 24 at 2^16 2216 / 1500
 #define ROPE_BATCH (CT_BATCH / 2)  // pairs whose products are stored and rescaled together
 #define ROPE_CONV_BYTES ((size_t)512 << 20)
 static bool rope_stored(const ckks_ctx* c, const he_rope_desc* d) {
@@ -2297,8 +2298,9 @@ static size_t ws_norm(const ckks_ctx* c, const he_norm_desc* d) {
     if (d->iterations && (t = ws_ctct(c, d->level - 2, 2)) > sub) sub = t;
     if ((t = ws_ctct(c, (u32)last, (u32)nb)) > sub) sub = t;
     if (d->gate == HE_GATE_CIPHER && (t = ws_ctct(c, d->level, (u32)nb)) > sub) sub = t;
+    if (d->gate == HE_GATE_PLAIN && ntt_has_modup(c) && (t = blk(2 * nb * d->level * N)) > sub) sub = t;
     return blk(3 * L1 * N) + 2 * blk(2 * L1 * N) + blk(2 * N * d->level) + 2 * blk(2 * N * d->level) +
-           (d->gate ? blk(nb * 2 * d->level * N) : 0) + (d->gate == HE_GATE_PLAIN || !ntt_has_modup(c) ? blk(nb * 2 * L1 * N) : 0) + sub;
+           (d->gate ? blk(nb * 2 * d->level * N) : 0) + (!ntt_has_modup(c) ? blk(nb * 2 * L1 * N) : (d->gate == HE_GATE_PLAIN ? blk(nb * 2 * N) : 0)) + sub;
 }
 size_t he_norm_workspace_bytes(const ckks_ctx* c, const he_norm_desc* d) {
     if (!c || norm_check(c, d)) return 0;
@@ -2333,7 +2335,7 @@ int he_norm_gate(const ckks_ctx* c, const he_norm_desc* d, const int64_t* h_k_ne
     u64* u = ar.take(2 * N * level);
     u64* w = ar.take(2 * N * level);
     u64* t = d->gate ? ar.take(nb * 2 * level * N) : nullptr;
-    u64* tmp = d->gate == HE_GATE_PLAIN || !mac ? ar.take(nb * 2 * L1 * N) : nullptr;
+    u64* tmp = !mac ? ar.take(nb * 2 * L1 * N) : (d->gate == HE_GATE_PLAIN ? ar.take(nb * 2 * N) : nullptr);
     if (!ar.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
     int rc;
 
@@ -2408,9 +2410,20 @@ int he_norm_gate(const ckks_ctx* c, const he_norm_desc* d, const int64_t* h_k_ne
         } else {
             ts = (size_t)level * N;
             if (d->gate == HE_GATE_PLAIN) {
-                HIP_TRY(launch_gate_mul(c, level, 0, n, px[0], x->ct_stride, x->comp_stride, pg[0], gate->ct_stride, tmp, st));
-                for (u32 b0 = 0; b0 < n; b0 += CT_BATCH)
-                    if ((rc = run_rescale(c, level, ptmp + b0, L1 * N, ot + b0, n - b0 < CT_BATCH ? n - b0 : CT_BATCH, ar.rest(), st))) return rc;
+                if (mac) {  // the dropped limb of the products alone; the others where the division ends
+                    Arena sub = ar.rest();
+                    u64* w2 = sub.take((size_t)2 * n * level * N);
+                    if (!sub.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
+                    HIP_TRY(launch_gate_mul(c, level, level, n, px[0], x->ct_stride, x->comp_stride, pg[0], gate->ct_stride, tmp, st));
+                    HIP_TRY(launch_ntt(c, true, tmp, 1, tmp, 1, range_list(0, 1, level), 2 * n, st, nullptr, nullptr, c->d_rescale_prep_f, nullptr, nullptr, NTT_LO));
+                    const VecEpilogue ve = {px[0], x->ct_stride, x->comp_stride, pg[0], nullptr, gate->ct_stride, t, (size_t)2 * level * N,
+                                            c->d_rescale_ep + (size_t)level * 2 * c->num_q, level, RopePairs{}};
+                    HIP_TRY(launch_ntt_rescale_vec(c, level, VEC_GATE, (const double*)tmp, w2, 2 * n, ve, st));
+                } else {
+                    HIP_TRY(launch_gate_mul(c, level, 0, n, px[0], x->ct_stride, x->comp_stride, pg[0], gate->ct_stride, tmp, st));
+                    for (u32 b0 = 0; b0 < n; b0 += CT_BATCH)
+                        if ((rc = run_rescale(c, level, ptmp + b0, L1 * N, ot + b0, n - b0 < CT_BATCH ? n - b0 : CT_BATCH, ar.rest(), st))) return rc;
+                }
             } else if ((rc = run_ctct_merged(c, level, px, x->comp_stride, pg, gate->comp_stride, nullptr, 0, rlk->d_key, ot, n, ar.rest(), st))) {
                 return rc;
             }

@@ -659,107 +659,6 @@ __global__ __launch_bounds__(NTT_THREADS) void ntt_fwd_lo_div_kernel(NttArgs arg
     div_store<A, EM>(args, ep, i, pl_at(pl.mod, tile.a), b, off, tid, lds1, P.mc, O);
 }
 
-// The same end of a rescale for products with plaintexts, whose limbs are formed from their operands as they are needed and not stored before: out = (v - w) cinv,
-//   MODE VEC_TURN: item 4 z + 2 side + comp is channel first(j) (side 0: v = a C_j - b S_j) or second(j) (side 1: v = a S_j + b C_j) of pair z = z0 + .., (a, b) the pair
-//   MODE VEC_GATE: item 2 z + comp: v = G_z (.) x_z
-// (residues below 2^50; operands are requested a round ahead like div_request's; the items of a slice, which share them, are on one die: lo_tile)
-template <int MODE>
-__global__ __launch_bounds__(NTT_THREADS) void ntt_fwd_lo_vec_kernel(NttArgs args, PolyList pl, VecEpilogue ve) {
-    typedef ArithF64 A;
-    typedef ArithF64W AR;
-    __shared__ double lds0[LDS_PADDED_WORDS];
-    __shared__ double lds1[LDS_PADDED_WORDS];
-    const u32 tid = threadIdx.x;
-    const LoTile tile = lo_tile(args.log_hi, args.lo_group);
-    const u32 blk = tile.blk, b = tile.b;
-    const PolyRef<A> P = poly_ref<A>(args, pl, b, tile.a);
-    const size_t off = (size_t)blk << 11;
-    const u32 TA = (1u << args.log_hi) + blk;
-    const u32 d3 = tid >> 5, x5 = tid & 31, d2 = (tid >> 2) & 7, d0 = tid & 3;
-    double v[8], wa[7], wb[7], wc[7], wd[6];
-    u64 raw[8];
-    load_tw_w<3>(P.tw_val, TA, wa);
-    load_tw_w<3>(P.tw_val, 8 * TA + d3, wb);
-#pragma unroll
-    for (int j = 0; j < 8; j++) raw[j] = P.src[off + tid + 256 * j];
-#pragma unroll
-    for (int j = 0; j < 8; j++) v[j] = A::load_second(raw[j], P.mc);
-    A::fwd_begin(v, P.mc);
-    fwd_rows_pre<AR, 3>(v, wa, P.mc);
-    load_tw_w<3>(P.tw_val, 64 * TA + 8 * d3 + d2, wc);
-#pragma unroll
-    for (int j = 0; j < 8; j++) lds0[LDS_PAD(tid + 256 * j)] = v[j];
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 8; j++) v[j] = lds0[LDS_PAD(d3 * 256 + 32 * j + x5)];
-    A::fwd_begin(v, P.mc);
-    fwd_rows_pre<AR, 3>(v, wb, P.mc);
-    load_tw_w<2>(P.tw_val, 512 * TA + 2 * tid, wd);
-    load_tw_w<2>(P.tw_val, 512 * TA + 2 * tid + 1, wd + 3);
-#pragma unroll
-    for (int j = 0; j < 8; j++) lds1[LDS_PAD(d3 * 256 + 32 * j + x5)] = v[j];
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 8; j++) v[j] = lds1[LDS_PAD(d3 * 256 + d2 * 32 + 4 * j + d0)];
-    A::fwd_begin(v, P.mc);
-    fwd_rows_pre<AR, 3>(v, wc, P.mc);
-#pragma unroll
-    for (int j = 0; j < 8; j++) lds0[LDS_PAD(d3 * 256 + d2 * 32 + 4 * j + d0)] = v[j];
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 8; j++) v[j] = lds0[LDS_PAD(8 * tid + j)];
-    // the operands
-    const u32 i = pl_at(pl.dpos, tile.a), comp = b & 1;
-    const size_t row = ((size_t)i << args.log_n) + off + tid;
-    const u64 *x0, *x1 = nullptr, *p0, *p1 = nullptr;
-    u64* out = ve.out + ((size_t)(comp * ve.level + i) << args.log_n) + off + tid;
-    bool minus = false;
-    if constexpr (MODE == VEC_TURN) {  // x0 p0 +- x1 p1: the channel itself times the cosine, its partner times the sine
-        const u32 z = ve.P.z0 + (b >> 2), j = z % ve.P.n_pairs, side = (b >> 1) & 1;
-        const size_t head = (size_t)(z / ve.P.n_pairs) * ve.P.head_dim;
-        const size_t own = head + (side ? ve.P.second(j) : ve.P.first(j)), other = head + (side ? ve.P.first(j) : ve.P.second(j));
-        x0 = ve.in + own * ve.in_ct + comp * ve.in_comp + row;
-        x1 = ve.in + other * ve.in_ct + comp * ve.in_comp + row;
-        p0 = ve.p0 + j * ve.p_stride + row;
-        p1 = ve.p1 + j * ve.p_stride + row;
-        out += own * ve.out_ct;
-        minus = (side == 0) != (ve.P.inverse != 0);
-    } else {
-        const size_t z = b >> 1;
-        x0 = ve.in + z * ve.in_ct + comp * ve.in_comp + row;
-        p0 = ve.p0 + z * ve.p_stride + row;
-        out += z * ve.out_ct;
-    }
-    u64 o0[8], o1[8], q0[8], q1[8];
-#pragma unroll
-    for (int j = 0; j < 8; j++) {
-        o0[j] = x0[256 * j];
-        q0[j] = p0[256 * j];
-        if constexpr (MODE == VEC_TURN) {
-            o1[j] = x1[256 * j];
-            q1[j] = p1[256 * j];
-        }
-    }
-    fwd_rows_pre<AR, 2>(v, wd, P.mc);
-    fwd_rows_pre<AR, 2>(v + 4, wd + 3, P.mc);
-    A::fwd_end(v, P.mc);
-    // back through LDS so that a wave stores 512 contiguous bytes per instruction
-#pragma unroll
-    for (int j = 0; j < 8; j++) lds1[LDS_PAD(8 * tid + j)] = v[j];
-    __syncthreads();
-    const double q = P.mc.q, qinv = P.mc.qinv, cinv = A::from_u64(ve.cinv[i]), cinvq = cinv / q;
-#pragma unroll
-    for (int j = 0; j < 8; j++) {
-        double s = A::mulmod_any(A::from_u64(o0[j]), A::from_u64(q0[j]), q, qinv);
-        if constexpr (MODE == VEC_TURN) {
-            const double t = A::mulmod_any(A::from_u64(o1[j]), A::from_u64(q1[j]), q, qinv);
-            s = minus ? s - t : s + t;  // below 1.5 q
-        }
-        const double r = A::mulmod(A::reduce(s - lds1[LDS_PAD(tid + 256 * j)], P.mc), cinv, cinvq, q);
-        out[256 * j] = A::canonical(A::reduce(r, P.mc), P.mc);
-    }
-}
-
 // The lo pass of ModUp's forward transforms with the inner product with the switching key in place of its stores.
 // A workgroup owns one 2^11-point slice of one position e of the extended basis of one batch item: it transforms that
 // slice of every digit whose limb e went through the converting hi pass (all live digits but the one e belongs to; the
@@ -895,6 +794,92 @@ __device__ __forceinline__ void fwd_lo_rounds(double (&v)[8], double* lds0, doub
 #pragma unroll
     for (int i = 0; i < 8; i++) lds1[LDS_PAD(8 * tid + i)] = v[i];
     __syncthreads();
+}
+
+// The lo pass that ends a rescale of products with plaintexts, whose limbs are formed from their operands as they are needed and not stored before: (v - w) q_level^-1
+// for two results that share operands and the slice's twiddles, one transformed after the other:
+//   VEC_TURN: the pair z = z0 + .., (a, b), of channels, one component: v = a C - b S and a S + b C (batch items 4 z + comp, 4 z + 2 + comp)
+//   VEC_GATE: the two components of ciphertext z: v = G x_0 and G x_1 (batch items 2 z, 2 z + 1)
+// Residues below 2^50.  Bound by HBM: converted limbs, operands and results once each, 1.05 ms for 64 channels of 23 limbs at N = 2^16 (4.2 TB/s).  A workgroup per result
+// took 1.25 ms: its operands and twiddles, seven times the bytes of a result, came from the L2 cache for each.  With the operands requested in front of the second
+// transform (180 registers, two waves per SIMD instead of four) 1.15 ms.
+template <VecMode MODE>
+__global__ __launch_bounds__(NTT_THREADS) void ntt_fwd_lo_vec_kernel(NttArgs args, PolyList pl, VecEpilogue ve) {
+    typedef ArithF64 A;
+    __shared__ double lds0[LDS_PADDED_WORDS];
+    __shared__ double lds1[LDS_PADDED_WORDS];
+    const u32 tid = threadIdx.x;
+    const LoTile tile = lo_tile(args.log_hi, args.lo_group);
+    const u32 blk = tile.blk, i = tile.a, zr = MODE == VEC_TURN ? tile.b >> 1 : tile.b, comp = MODE == VEC_TURN ? tile.b & 1 : 0;
+    const PolyRef<A> P = poly_ref<A>(args, pl, MODE == VEC_TURN ? 4 * zr + comp : 2 * zr, i);
+    const size_t off = (size_t)blk << 11;
+    const u32 TA = (1u << args.log_hi) + blk;
+    const u32 d3 = tid >> 5, d2 = (tid >> 2) & 7;
+    double v[8], wa[7], wb[7], wc[7], wd[6];
+    u64 raw[8], next[8];
+    load_tw_w<3>(P.tw_val, TA, wa);
+    load_tw_w<3>(P.tw_val, 8 * TA + d3, wb);
+    const u64* src = P.src + off + tid;
+#pragma unroll
+    for (int j = 0; j < 8; j++) raw[j] = src[256 * j];
+    load_tw_w<3>(P.tw_val, 64 * TA + 8 * d3 + d2, wc);
+    load_tw_w<2>(P.tw_val, 512 * TA + 2 * tid, wd);
+    load_tw_w<2>(P.tw_val, 512 * TA + 2 * tid + 1, wd + 3);
+    src += ((MODE == VEC_TURN ? 2 : 1) * args.src_bstride) << args.log_n;
+#pragma unroll
+    for (int j = 0; j < 8; j++) next[j] = src[256 * j];
+#pragma unroll
+    for (int j = 0; j < 8; j++) v[j] = A::load_second(raw[j], P.mc);
+    fwd_lo_rounds(v, lds0, lds1, tid, wa, wb, wc, wd, P.mc);
+    double w0[8];
+#pragma unroll
+    for (int j = 0; j < 8; j++) w0[j] = lds1[LDS_PAD(tid + 256 * j)];
+    // (the second item's first exchange writes lds0, and its barrier stands between these reads of lds1 and the next writes to it)
+#pragma unroll
+    for (int j = 0; j < 8; j++) v[j] = A::load_second(next[j], P.mc);
+    fwd_lo_rounds(v, lds0, lds1, tid, wa, wb, wc, wd, P.mc);
+    const size_t row = ((size_t)i << args.log_n) + off + tid;
+    const u64 *x0, *x1, *p0, *p1 = nullptr;
+    u64* o0 = ve.out + ((size_t)(comp * ve.level + i) << args.log_n) + off + tid;
+    u64* o1 = o0;
+    if constexpr (MODE == VEC_TURN) {
+        const u32 z = ve.P.z0 + zr, j = z % ve.P.n_pairs;
+        const size_t head = (size_t)(z / ve.P.n_pairs) * ve.P.head_dim, first = head + ve.P.first(j), second = head + ve.P.second(j);
+        x0 = ve.in + first * ve.in_ct + comp * ve.in_comp + row;
+        x1 = ve.in + second * ve.in_ct + comp * ve.in_comp + row;
+        p0 = ve.p0 + j * ve.p_stride + row;
+        p1 = ve.p1 + j * ve.p_stride + row;
+        o0 += first * ve.out_ct;
+        o1 += second * ve.out_ct;
+    } else {
+        x0 = ve.in + zr * ve.in_ct + row;
+        x1 = x0 + ve.in_comp;
+        p0 = ve.p0 + zr * ve.p_stride + row;
+        o0 += zr * ve.out_ct;
+        o1 = o0 + ((size_t)ve.level << args.log_n);
+    }
+    u64 a[8], b[8], c[8], s[8];
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+        a[j] = x0[256 * j];
+        b[j] = x1[256 * j];
+        c[j] = p0[256 * j];
+        if constexpr (MODE == VEC_TURN) s[j] = p1[256 * j];
+    }
+    const double q = P.mc.q, qinv = P.mc.qinv, cinv = A::from_u64(ve.cinv[i]), cinvq = cinv / q;
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+        const double av = A::from_u64(a[j]), bv = A::from_u64(b[j]), cv = A::from_u64(c[j]);
+        double ya = A::mulmod_any(av, cv, q, qinv), yb = A::mulmod_any(bv, cv, q, qinv);
+        if constexpr (MODE == VEC_TURN) {
+            const double sv = A::from_u64(s[j]), bs = A::mulmod_any(bv, sv, q, qinv), as = A::mulmod_any(av, sv, q, qinv);
+            ya = ve.P.inverse ? ya + bs : ya - bs;  // below 1.5 q
+            yb = ve.P.inverse ? yb - as : yb + as;
+        }
+        const double ra = A::mulmod(A::reduce(ya - w0[j], P.mc), cinv, cinvq, q), rb = A::mulmod(A::reduce(yb - lds1[LDS_PAD(tid + 256 * j)], P.mc), cinv, cinvq, q);
+        o0[256 * j] = A::canonical(A::reduce(ra, P.mc), P.mc);
+        o1[256 * j] = A::canonical(A::reduce(rb, P.mc), P.mc);
+    }
 }
 
 // PROD, LIN, ROT, SUM, MASK, DIV, HOIST (see MacEpilogue) are template arguments so that what follows the digits is straight-line code: with the
@@ -2804,7 +2789,7 @@ hipError_t launch_ntt_rescale_share(const ckks_ctx* c, u32 level, const double* 
 }
 
 hipError_t launch_ntt_rescale_vec(const ckks_ctx* c, u32 level, VecMode mode, const double* y, u64* w, u32 batch, const VecEpilogue& ve, hipStream_t st) {
-    if (level == 0 || !ntt_has_modup(c)) return hipErrorInvalidValue;
+    if (level == 0 || !ntt_has_modup(c) || batch % (mode == VEC_TURN ? 4 : 2)) return hipErrorInvalidValue;
     ConvPrologue cp = {};
     cp.y = y;
     cp.y_bstride = c->N;
@@ -2832,7 +2817,8 @@ hipError_t launch_ntt_rescale_vec(const ckks_ctx* c, u32 level, VecMode mode, co
     const u32 slices = level << c->log_hi;
     for (u32 g = 64; g >= 8; g >>= 1)
         if (slices % g == 0) { args.lo_group = g; break; }
-    const dim3 grid = args.lo_group ? dim3(args.lo_group, batch, slices / args.lo_group) : dim3(batch, slices);
+    const u32 items = batch / 2;  // two results a workgroup
+    const dim3 grid = args.lo_group ? dim3(args.lo_group, items, slices / args.lo_group) : dim3(items, slices);
     ProfScope ps__(c, K_NTT_FWD_LO, st, (mode == VEC_TURN ? 36.0 : 28.0) * batch * level * c->N, 0.5 * batch * level * c->N * c->log_lo);
     if (mode == VEC_TURN) hipLaunchKernelGGL(ntt_fwd_lo_vec_kernel<VEC_TURN>, grid, dim3(NTT_THREADS), 0, st, args, pl, ve);
     else hipLaunchKernelGGL(ntt_fwd_lo_vec_kernel<VEC_GATE>, grid, dim3(NTT_THREADS), 0, st, args, pl, ve);
