@@ -859,8 +859,9 @@ class Oracle:
         return np.stack(out)
 
     def norm_gate(self, x, level: int, k_eps: int, k_slope: int, k_start: int, k_newton: Sequence[int], rlk, gate=None, residual=None,
-                  k_residual: int = 0) -> List[np.ndarray]:
-        """x: channel ciphertexts [2][level+1][N]; gate: plaintexts [level+1][N] or ciphertexts; residual: ciphertexts of as many limbs or more."""
+                  k_residual: int = 0, only: Optional[Sequence[int]] = None) -> List[np.ndarray]:
+        """x: channel ciphertexts [2][level+1][N]; gate: plaintexts [level+1][N] or ciphertexts; residual: ciphertexts of as many limbs or more;
+        only: the channels whose outputs are wanted."""
         idx = list(range(level + 1))
         d = [np.zeros((level + 1, self.N), dtype=np.uint64) for _ in range(3)]
         for ct in x:
@@ -877,7 +878,8 @@ class Oracle:
             r = self.ctct_mul_relin_rescale(u, w, rlk, m - 1, addend=scaled(r, k, m - 1))
             m -= 2
         out = []
-        for c, ct in enumerate(x):
+        for c in range(len(x)) if only is None else only:
+            ct = x[c]
             t = _u64(ct)
             if gate is not None and np.ndim(gate[c]) == 2:
                 t = self.rescale(np.stack([self.mul(t[i], gate[c], idx) for i in range(2)]), level)

@@ -179,7 +179,7 @@ int run_modup(const ckks_ctx* c, u32 level, const u64* const* srcs, u32 n, const
 }
 
 // What the forward transform of the converted dropped part does to its results instead of storing them (see FwdEpilogue).
-FwdEpilogue moddown_epilogue(const ckks_ctx* c, u32 level, bool merged, const u64* v, const FinalItem* items, u32 n) {
+FwdEpilogue moddown_epilogue(const ckks_ctx* c, u32 level, bool merged, const u64* v, const FinalItem* items, u32 n, u32 keep = 0) {
     FwdEpilogue ep;
     const u32 kp = merged ? c->k2_pad : c->k_pad;
     const u64* tab = merged ? c->moddown_rs_table(level) : c->d_moddown;
@@ -187,7 +187,7 @@ FwdEpilogue moddown_epilogue(const ckks_ctx* c, u32 level, bool merged, const u6
     ep.cinv = tab + 2 * kp + (size_t)kp * c->num_q;
     ep.mci = c->d_mc;
     ep.E = c->ext_limbs(level);
-    ep.n_out = merged ? level : level + 1;
+    ep.n_out = keep ? keep : (merged ? level : level + 1);
     ep.num_q = c->num_q;
     ep.use_vl = 0;
     ep.v_cstride = ep.v2_cstride = 0;
@@ -205,8 +205,9 @@ u32 dropped_from(u32 level, bool merged) { return merged ? level : level + 1; }
 // level and the special primes, the results are [2][level][N].
 // items null (with lo_done): all but the second pass of the converted parts' forward transforms and the last step (run_inner_divide).
 // lo_done: the dropped limbs have been through the first pass of their inverse transform (launch_ntt_lo_mac with inv_from).
+// keep (merged, with the fused passes): nothing but the first `keep` limbs of the quotients, results [2][keep][N]; 0: all.
 int run_moddown(const ckks_ctx* c, u32 level, const KsWs& ws, u32 n, const FinalItem* items, hipStream_t st, bool merged = false,
-                bool lo_done = false) {
+                bool lo_done = false, u32 keep = 0) {
     const u32 L1 = level + 1, E = c->ext_limbs(level), k = c->num_p;
     const u32 mid = ntt_mid_moddown(c, level, merged, 2 * n, lo_done);
     if (merged) {
@@ -218,11 +219,11 @@ int run_moddown(const ckks_ctx* c, u32 level, const KsWs& ws, u32 n, const Final
                 HIP_TRY(launch_ntt(c, true, ws.v, E, ws.v, E, dl, 2 * n, st, nullptr, nullptr, c->d_moddown_rs_prep_f + (size_t)level * c->M,
                                    nullptr, nullptr, lo_done ? NTT_HI : (mid ? NTT_LO : NTT_BOTH)));
             if (!items) {
-                HIP_TRY(launch_ntt_moddown(c, level, true, (const double*)ws.v, ws.w, 2 * n, st, nullptr, mid));
+                HIP_TRY(launch_ntt_moddown(c, level, true, (const double*)ws.v, ws.w, 2 * n, st, nullptr, mid, keep));
                 return CKKS_OK;
             }
-            const FwdEpilogue ep = moddown_epilogue(c, level, true, ws.v, items, n);
-            HIP_TRY(launch_ntt_moddown(c, level, true, (const double*)ws.v, ws.w, 2 * n, st, &ep, mid));
+            const FwdEpilogue ep = moddown_epilogue(c, level, true, ws.v, items, n, keep);
+            HIP_TRY(launch_ntt_moddown(c, level, true, (const double*)ws.v, ws.w, 2 * n, st, &ep, mid, keep));
             return CKKS_OK;
         }
         HIP_TRY(launch_ntt(c, true, ws.v, E, ws.v, E, dl, 2 * n, st));
@@ -274,7 +275,7 @@ int run_moddown(const ckks_ctx* c, u32 level, const KsWs& ws, u32 n, const Final
 // sixteen (6144 a batch) 993 / 981 / 840
 #define DIVIDE_INSIDE_HOISTED 900
 int run_inner_divide(const ckks_ctx* c, u32 level, const KsWs& ws, const u64* const* keys, u32 n, u64* const* outs, const u64* const* accs, hipStream_t st,
-                     bool merged, const MacProduct* prod, const MacRotate* rot) {
+                     bool merged, const MacProduct* prod, const MacRotate* rot, u32 keep = 0) {  // keep: see run_moddown
     u64* vs[KS_MAX_BATCH];
     for (u32 b = 0; b < n; b++) vs[b] = ws.v + b * ws.v_b;
     const u32 from = dropped_from(level, merged);
@@ -283,14 +284,14 @@ int run_inner_divide(const ckks_ctx* c, u32 level, const KsWs& ws, const u64* co
         HIP_TRY(launch_ntt_lo_mac(c, level, dsrc(c, ws, 0), keys, vs, n, st, from, prod, rot));
         FinalItem items[KS_MAX_BATCH];
         for (u32 b = 0; b < n; b++) items[b] = FinalItem{nullptr, nullptr, nullptr, outs[b], 1, 0, accs ? accs[b] : nullptr};
-        return run_moddown(c, level, ws, n, items, st, merged, true);
+        return run_moddown(c, level, ws, n, items, st, merged, true, keep);
     }
     HIP_TRY(launch_ntt_lo_mac(c, level, dsrc(c, ws, 0), keys, vs, n, st, from, prod, rot, nullptr, nullptr, true));
-    if (int rc = run_moddown(c, level, ws, n, nullptr, st, merged, true)) return rc;
+    if (int rc = run_moddown(c, level, ws, n, nullptr, st, merged, true, keep)) return rc;
     const u64* tab = merged ? c->moddown_rs_table(level) : c->d_moddown;
     const u32 kp = merged ? c->k2_pad : c->k_pad;
     const MacDivide div = {(const double*)ws.w, tab + 2 * kp + (size_t)kp * c->num_q, outs, accs};
-    HIP_TRY(launch_ntt_lo_mac(c, level, dsrc(c, ws, 0), keys, vs, n, st, from, prod, rot, nullptr, &div));
+    HIP_TRY(launch_ntt_lo_mac(c, level, dsrc(c, ws, 0), keys, vs, n, st, keep ? keep : from, prod, rot, nullptr, &div));
     return CKKS_OK;
 }
 
@@ -399,7 +400,7 @@ struct LinAddend {
 // a1 (.) b1 is formed as the inverse transform loads it, P d0, P d1 and the own-limb term as the inner product's last terms, all
 // from the operands themselves (b, b1: the two components of the second one); dividing the sums by P (merged: by P*q_level) is then the whole product.
 int run_product(const ckks_ctx* c, u32 level, const u64* const* a, size_t a_cstride, const u64* const* b, const u64* const* b1, const u64* d_rlk,
-                u64* const* outs, u32 n, const KsWs& ws, hipStream_t st, bool merged, const LinAddend* lin = nullptr) {
+                u64* const* outs, u32 n, const KsWs& ws, hipStream_t st, bool merged, const LinAddend* lin = nullptr, u32 keep = 0) {
     const u64 *a1[KS_MAX_BATCH], *keys[KS_MAX_BATCH];
     for (u32 i = 0; i < n; i++) {
         a1[i] = a[i] + a_cstride;
@@ -416,7 +417,7 @@ int run_product(const ckks_ctx* c, u32 level, const u64* const* a, size_t a_cstr
         prod.y_cstride = lin->y_cstride;
         prod.kb = lin->kb;
     }
-    return run_inner_divide(c, level, ws, keys, n, outs, nullptr, st, merged, &prod, nullptr);
+    return run_inner_divide(c, level, ws, keys, n, outs, nullptr, st, merged, &prod, nullptr, keep);
 }
 
 // n products a[b]*b[b] (as many as ks_batch, CT_BATCH without the fused inner product) with relinearisation (operands possibly at a higher level:
@@ -2291,20 +2292,48 @@ static u32 norm_batch(const ckks_ctx* c, const he_norm_desc* d) {
     const u32 most = ks_batch(c);
     return d->channels < most ? d->channels : most;
 }
-static size_t ws_norm(const ckks_ctx* c, const he_norm_desc* d) {
-    const size_t N = c->N, L1 = d->level + 1, nb = norm_batch(c, d), last = d->level - 2 - 2 * d->iterations;
-    size_t sub = ws_ks(c, d->level, 1, 1), t;
-    if ((t = ws_rescale(c, d->level, CT_BATCH)) > sub) sub = t;
-    if (d->iterations && (t = ws_ctct(c, d->level - 2, 2)) > sub) sub = t;
-    if ((t = ws_ctct(c, (u32)last, (u32)nb)) > sub) sub = t;
+// The gates' products beside Newton's chain, whose launches leave most of the chip idle, and batches of channels in turn, on the context's second stream: where its share is
+// worth the fork and the join.  One stream / two in us, millions of coefficients that the line counts in brackets: ciphertext gates, 16 channels of 14 + 5 limbs at N = 2^13
+// (2.5) 455 / 441, 32 at 2^14 (10) 978 / 845, 16 of 21 + 8 at 2^16 (30) 2826 / 2605; plaintext gates, 12 of 14 + 5 at 2^14 (3.7) 504 / 521, 16 at 2^15 (10) 819 / 805; batches
+// in turn, 32 of 14 + 5 at 2^14 (5.8) 640 / 639, 64 (11.5) 914 / 872, 64 of 24 + 8 at 2^16 (92) 4690 / 4520
+static bool norm_overlap(const ckks_ctx* c, const he_norm_desc* d, bool gates) {
+    const u64 n = (u64)d->channels * c->N * c->ext_limbs(gates ? d->level : d->level - 2 - 2 * d->iterations);
+    if (!ntt_has_modup(c)) return false;
+    if (gates) return d->gate != HE_GATE_NONE && n >= (u64)1 << (d->gate == HE_GATE_CIPHER ? 21 : 23);
+    return d->channels > norm_batch(c, d) && n >= (u64)1 << 23;
+}
+// limbs of a gated channel: those that the last product reads
+static u32 norm_gated_limbs(const ckks_ctx* c, const he_norm_desc* d) { return ntt_has_modup(c) ? d->level - 1 - 2 * d->iterations : d->level; }
+// gated channels that are kept at a time
+#define NORM_GATED_BYTES ((size_t)4 << 30)
+static u32 norm_chunk(const ckks_ctx* c, const he_norm_desc* d) {
+    if (d->gate == HE_GATE_NONE) return d->channels;
+    const size_t nb = norm_batch(c, d), fit = NORM_GATED_BYTES / ((size_t)16 * norm_gated_limbs(c, d) * c->N) / nb * nb;
+    return fit < nb ? (u32)nb : (fit < d->channels ? (u32)fit : d->channels);
+}
+// scratch of a stream's gates and last products
+static size_t ws_norm_lane(const ckks_ctx* c, const he_norm_desc* d) {
+    const size_t N = c->N, nb = norm_batch(c, d), last = d->level - 2 - 2 * d->iterations, L1 = d->level + 1;
+    size_t sub = ws_ctct(c, (u32)last, (u32)nb) + (ntt_has_modup(c) ? 0 : blk(nb * 2 * (last + 1) * N)), t;
     if (d->gate == HE_GATE_CIPHER && (t = ws_ctct(c, d->level, (u32)nb)) > sub) sub = t;
-    if (d->gate == HE_GATE_PLAIN && ntt_has_modup(c) && (t = blk(2 * nb * d->level * N)) > sub) sub = t;
-    return blk(3 * L1 * N) + 2 * blk(2 * L1 * N) + blk(2 * N * d->level) + 2 * blk(2 * N * d->level) +
-           (d->gate ? blk(nb * 2 * d->level * N) : 0) + (!ntt_has_modup(c) ? blk(nb * 2 * L1 * N) : (d->gate == HE_GATE_PLAIN ? blk(nb * 2 * N) : 0)) + sub;
+    if (d->gate == HE_GATE_PLAIN) {
+        t = ntt_has_modup(c) ? blk(nb * 2 * N) + blk(2 * nb * norm_gated_limbs(c, d) * N) : blk(nb * 2 * L1 * N) + ws_rescale(c, d->level, CT_BATCH);
+        if (t > sub) sub = t;
+    }
+    return sub;
+}
+static size_t ws_norm(const ckks_ctx* c, const he_norm_desc* d, bool two) {
+    const size_t N = c->N, L1 = d->level + 1, lane = ws_norm_lane(c, d);
+    size_t sub = ws_ks(c, d->level, 1, 1), t;  // the chain's
+    if ((t = ws_rescale(c, d->level - 1, 1)) > sub) sub = t;
+    if (d->iterations && (t = ws_ctct(c, d->level - 2, ntt_has_modup(c) ? 2 : 1) + (ntt_has_modup(c) ? 0 : blk(2 * L1 * N))) > sub) sub = t;
+    if (lane > sub) sub = lane;
+    return blk(3 * L1 * N) + 2 * blk(2 * L1 * N) + 3 * blk(2 * N * d->level) + (d->gate ? blk((size_t)norm_chunk(c, d) * 2 * norm_gated_limbs(c, d) * N) : 0) + sub +
+           (two ? lane : 0);
 }
 size_t he_norm_workspace_bytes(const ckks_ctx* c, const he_norm_desc* d) {
     if (!c || norm_check(c, d)) return 0;
-    return ws_norm(c, d);
+    return ws_norm(c, d, c->side && (norm_overlap(c, d, true) || norm_overlap(c, d, false)));  // sized for overlap on
 }
 
 int he_norm_gate(const ckks_ctx* c, const he_norm_desc* d, const int64_t* h_k_newton, const he_ct_array* x, const he_ct_array* gate,
@@ -2322,11 +2351,13 @@ int he_norm_gate(const ckks_ctx* c, const he_norm_desc* d, const int64_t* h_k_ne
     const bool add = residual && residual->d;
     if (add)
         if (int rc = check_array(c, residual, d->channels, last + 1, 2)) return rc;
-    if (!d_ws || ws_bytes < ws_norm(c, d)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
+    if (!d_ws || ws_bytes < ws_norm(c, d, false)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
     hipStream_t st = (hipStream_t)stream;
     const bool mac = ntt_has_modup(c);
-    const size_t N = c->N, L1 = level + 1;
-    const u32 nb = norm_batch(c, d);
+    const size_t N = c->N, L1 = level + 1, gl = norm_gated_limbs(c, d);
+    const u32 nb = norm_batch(c, d), chunk = norm_chunk(c, d);
+    const bool two = c->side_stream() && ws_bytes >= ws_norm(c, d, true);  // room for the second stream's scratch
+    const bool gates_aside = two && norm_overlap(c, d, true), batches_aside = two && norm_overlap(c, d, false);
     Arena ar(d_ws, ws_bytes);
     u64* sq3 = ar.take(3 * L1 * N);             // the three polynomials of the sum of squares
     u64* ra = ar.take(2 * L1 * N);              // the guess before and after its iterations, in turn
@@ -2334,109 +2365,161 @@ int he_norm_gate(const ckks_ctx* c, const he_norm_desc* d, const int64_t* h_k_ne
     u64* s = ar.take(2 * N * level);            // level - 1
     u64* u = ar.take(2 * N * level);
     u64* w = ar.take(2 * N * level);
-    u64* t = d->gate ? ar.take(nb * 2 * level * N) : nullptr;
-    u64* tmp = !mac ? ar.take(nb * 2 * L1 * N) : (d->gate == HE_GATE_PLAIN ? ar.take(nb * 2 * N) : nullptr);
+    u64* t = d->gate ? ar.take((size_t)chunk * 2 * gl * N) : nullptr;  // gated channels, [2][gl][N]
+    const size_t lane_bytes = ws_norm_lane(c, d);
+    Arena aside(nullptr, 0);
+    if (gates_aside || batches_aside) aside = Arena(ar.take(lane_bytes / sizeof(u64)), lane_bytes);
     if (!ar.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
-    int rc;
 
-    // s: a constant k joins a quotient by B exactly as B k joins the dividend (it vanishes modulo every dropped limb), and the addends of the
-    // inner product are multiplied by P already
-    auto times_limb = [&](int64_t k, u32 lv) {
-        LimbScalars v = limb_scalars(c, lv, k);
-        for (u32 i = 0; i <= lv; i++) v.v[i] = (u64)((unsigned __int128)v.v[i] * (c->mod[lv] % c->mod[i]) % c->mod[i]);
-        return v;
-    };
-    HIP_TRY(launch_square_sum(c, level, (const u64*)x->d, x->ct_stride, x->comp_stride, d->channels, times_limb(d->k_eps, level), sq3, st));
-    {
-        KsWs ws;
-        Arena sub = ar.rest();
-        if (!carve_ks(c, level, 1, 1, sub, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
-        const u64 *d0 = sq3, *d1 = sq3 + L1 * N, *d2 = sq3 + 2 * L1 * N;
-        u64* v = ws.v;
-        if ((rc = run_modup(c, level, &d2, 1, ws, st))) return rc;
-        HIP_TRY(launch_key_inner_ext(c, level, dsrc(c, ws, 0), rlk->d_key, 1, &d0, &d1, nullptr, &v, 1, st));
-        const FinalItem item = {nullptr, nullptr, nullptr, s, 1, 0, nullptr};
-        if ((rc = run_moddown(c, level, ws, 1, &item, st, true))) return rc;
-    }
-    // the first guess
-    const size_t ss = (size_t)level * N;  // component stride of s
-    HIP_TRY(launch_affine(c, level - 1, s, ss, limb_scalars(c, level - 1, d->k_slope), times_limb(d->k_start, level - 1), rb, st));
-    const u64* prb = rb;
-    if ((rc = run_rescale(c, level - 1, &prb, ss, &ra, 1, ar.rest(), st))) return rc;
-    // Newton's iterations, r at level m
-    u32 m = level - 2;
-    for (u32 it = 0; it < d->iterations; it++, m -= 2) {
-        const size_t rs = (size_t)(m + 1) * N, us = (size_t)m * N;
-        const u64 *pr = ra, *ps = s, *pu = u, *pw = w;
-        if (mac) {  // r r and r s side by side
-            const u64 *pa[2] = {ra, ra}, *pb0[2] = {ra, s}, *pb1[2] = {ra + rs, s + ss};
-            u64* po[2] = {u, w};
-            KsWs ws;
-            Arena sub = ar.rest();
-            if (!carve_ks(c, m, 2, 2, sub, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
-            if ((rc = run_product(c, m, pa, rs, pb0, pb1, rlk->d_key, po, 2, ws, st, true))) return rc;
-            const LimbScalars kn = limb_scalars(c, m - 1, h_k_newton[it]), zero = limb_scalars(c, m - 1, 0);
-            const LinAddend lin = {&pr, rs, kn.v, &pr, rs, zero.v};
-            if ((rc = run_ctct_merged(c, m - 1, &pu, us, &pw, us, nullptr, 0, rlk->d_key, &rb, 1, ar.rest(), st, &lin))) return rc;
-        } else {
-            if ((rc = run_ctct_merged(c, m, &pr, rs, &pr, rs, nullptr, 0, rlk->d_key, &u, 1, ar.rest(), st))) return rc;
-            if ((rc = run_ctct_merged(c, m, &pr, rs, &ps, ss, nullptr, 0, rlk->d_key, &w, 1, ar.rest(), st))) return rc;
-            HIP_TRY(launch_affine(c, m - 1, ra, rs, limb_scalars(c, m - 1, h_k_newton[it]), limb_scalars(c, m - 1, 0), tmp, st));
-            if ((rc = run_ctct_merged(c, m - 1, &pu, us, &pw, us, tmp, 0, rlk->d_key, &rb, 1, ar.rest(), st))) return rc;
-        }
-        u64* other = ra;
-        ra = rb;
-        rb = other;
-    }
-    // the channels, in batches
-    const size_t rs = (size_t)(last + 1) * N, out_ct = (size_t)2 * last * N;
-    const LimbScalars kr = limb_scalars(c, last, d->k_residual), zero = limb_scalars(c, last, 0);
-    for (u32 i0 = 0; i0 < d->channels; i0 += nb) {
-        const u32 n = d->channels - i0 < nb ? d->channels - i0 : nb;
-        const u64 *px[KS_MAX_BATCH], *pt[KS_MAX_BATCH], *pr[KS_MAX_BATCH], *pg[KS_MAX_BATCH], *pres[KS_MAX_BATCH], *ptmp[KS_MAX_BATCH];
-        u64 *ot[KS_MAX_BATCH], *out[KS_MAX_BATCH];
+    // t for channels i0 .. i0 + n - 1, the first of a chunk that starts at c0
+    auto run_gates = [&](u32 c0, u32 i0, u32 n, Arena sub, hipStream_t on) -> int {
+        const u64 *px[KS_MAX_BATCH], *pg[KS_MAX_BATCH];
+        u64* ot[KS_MAX_BATCH];
         for (u32 b = 0; b < n; b++) {
             px[b] = (const u64*)x->d + (size_t)(i0 + b) * x->ct_stride;
-            pt[b] = ot[b] = t + (size_t)b * 2 * level * N;
+            pg[b] = (const u64*)gate->d + (size_t)(i0 + b) * gate->ct_stride;
+            ot[b] = t + (size_t)(i0 - c0 + b) * 2 * gl * N;
+        }
+        if (d->gate == HE_GATE_CIPHER) {
+            if (!mac) return run_ctct_merged(c, level, px, x->comp_stride, pg, gate->comp_stride, nullptr, 0, rlk->d_key, ot, n, sub, on);
+            const u64* pg1[KS_MAX_BATCH];
+            for (u32 b = 0; b < n; b++) pg1[b] = pg[b] + gate->comp_stride;
+            KsWs ws;
+            if (!carve_ks(c, level, n, n, sub, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
+            return run_product(c, level, px, x->comp_stride, pg, pg1, rlk->d_key, ot, n, ws, on, true, nullptr, (u32)gl);
+        }
+        if (mac) {  // the dropped limb of the products alone; the others where the division ends
+            u64* y = sub.take((size_t)2 * n * N);
+            u64* conv = sub.take((size_t)2 * n * gl * N);
+            if (!sub.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
+            HIP_TRY(launch_gate_mul(c, level, level, n, px[0], x->ct_stride, x->comp_stride, pg[0], gate->ct_stride, y, on));
+            HIP_TRY(launch_ntt(c, true, y, 1, y, 1, range_list(0, 1, level), 2 * n, on, nullptr, nullptr, c->d_rescale_prep_f, nullptr, nullptr, NTT_LO));
+            const VecEpilogue ve = {px[0], x->ct_stride, x->comp_stride, pg[0], nullptr, gate->ct_stride, ot[0], 2 * gl * N,
+                                    c->d_rescale_ep + (size_t)level * 2 * c->num_q, (u32)gl, RopePairs{}};
+            HIP_TRY(launch_ntt_rescale_vec(c, level, VEC_GATE, (const double*)y, conv, 2 * n, ve, on));
+            return CKKS_OK;
+        }
+        u64* prod = sub.take((size_t)n * 2 * L1 * N);
+        if (!sub.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
+        HIP_TRY(launch_gate_mul(c, level, 0, n, px[0], x->ct_stride, x->comp_stride, pg[0], gate->ct_stride, prod, on));
+        for (u32 b = 0; b < n; b++) px[b] = prod + (size_t)b * 2 * L1 * N;
+        return run_rescale(c, level, px, L1 * N, ot, n, sub.rest(), on);  // (n <= CT_BATCH without the fused passes)
+    };
+    // s and Newton's iterations
+    auto run_chain = [&]() -> int {
+        int rc;
+        // a constant k joins a quotient by B exactly as B k joins the dividend (it vanishes modulo every dropped limb), and the addends of the
+        // inner product are multiplied by P already
+        auto times_limb = [&](int64_t k, u32 lv) {
+            LimbScalars v = limb_scalars(c, lv, k);
+            for (u32 i = 0; i <= lv; i++) v.v[i] = (u64)((unsigned __int128)v.v[i] * (c->mod[lv] % c->mod[i]) % c->mod[i]);
+            return v;
+        };
+        HIP_TRY(launch_square_sum(c, level, (const u64*)x->d, x->ct_stride, x->comp_stride, d->channels, times_limb(d->k_eps, level), sq3, st));
+        {
+            KsWs ws;
+            Arena sub = ar.rest();
+            if (!carve_ks(c, level, 1, 1, sub, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
+            const u64 *d0 = sq3, *d1 = sq3 + L1 * N, *d2 = sq3 + 2 * L1 * N;
+            u64* v = ws.v;
+            if ((rc = run_modup(c, level, &d2, 1, ws, st))) return rc;
+            HIP_TRY(launch_key_inner_ext(c, level, dsrc(c, ws, 0), rlk->d_key, 1, &d0, &d1, nullptr, &v, 1, st));
+            const FinalItem item = {nullptr, nullptr, nullptr, s, 1, 0, nullptr};
+            if ((rc = run_moddown(c, level, ws, 1, &item, st, true))) return rc;
+        }
+        // the first guess
+        const size_t ss = (size_t)level * N;  // component stride of s
+        HIP_TRY(launch_affine(c, level - 1, s, ss, limb_scalars(c, level - 1, d->k_slope), times_limb(d->k_start, level - 1), rb, st));
+        const u64* prb = rb;
+        if ((rc = run_rescale(c, level - 1, &prb, ss, &ra, 1, ar.rest(), st))) return rc;
+        // r at level m
+        u32 m = level - 2;
+        for (u32 it = 0; it < d->iterations; it++, m -= 2) {
+            const size_t rs = (size_t)(m + 1) * N, us = (size_t)m * N;
+            const u64 *pr = ra, *ps = s, *pu = u, *pw = w;
+            Arena sub = ar.rest();
+            if (mac) {  // r r and r s side by side
+                const u64 *pa[2] = {ra, ra}, *pb0[2] = {ra, s}, *pb1[2] = {ra + rs, s + ss};
+                u64* po[2] = {u, w};
+                KsWs ws;
+                if (!carve_ks(c, m, 2, 2, sub, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
+                if ((rc = run_product(c, m, pa, rs, pb0, pb1, rlk->d_key, po, 2, ws, st, true))) return rc;
+                const LimbScalars kn = limb_scalars(c, m - 1, h_k_newton[it]), zero = limb_scalars(c, m - 1, 0);
+                const LinAddend lin = {&pr, rs, kn.v, &pr, rs, zero.v};
+                if ((rc = run_ctct_merged(c, m - 1, &pu, us, &pw, us, nullptr, 0, rlk->d_key, &rb, 1, ar.rest(), st, &lin))) return rc;
+            } else {
+                u64* add = sub.take(2 * us);
+                if (!sub.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
+                if ((rc = run_ctct_merged(c, m, &pr, rs, &pr, rs, nullptr, 0, rlk->d_key, &u, 1, sub.rest(), st))) return rc;
+                if ((rc = run_ctct_merged(c, m, &pr, rs, &ps, ss, nullptr, 0, rlk->d_key, &w, 1, sub.rest(), st))) return rc;
+                HIP_TRY(launch_affine(c, m - 1, ra, rs, limb_scalars(c, m - 1, h_k_newton[it]), limb_scalars(c, m - 1, 0), add, st));
+                if ((rc = run_ctct_merged(c, m - 1, &pu, us, &pw, us, add, 0, rlk->d_key, &rb, 1, sub.rest(), st))) return rc;
+            }
+            u64* other = ra;
+            ra = rb;
+            rb = other;
+        }
+        return CKKS_OK;
+    };
+    // the last products
+    const size_t rs = (size_t)(last + 1) * N, out_ct = (size_t)2 * last * N;
+    const LimbScalars kr = limb_scalars(c, last, d->k_residual), zero = limb_scalars(c, last, 0);
+    auto run_last = [&](u32 c0, u32 i0, u32 n, Arena sub, hipStream_t on) -> int {
+        const u64 *pt[KS_MAX_BATCH], *pr[KS_MAX_BATCH], *pres[KS_MAX_BATCH];
+        u64* out[KS_MAX_BATCH];
+        for (u32 b = 0; b < n; b++) {
+            pt[b] = d->gate ? t + (size_t)(i0 - c0 + b) * 2 * gl * N : (const u64*)x->d + (size_t)(i0 + b) * x->ct_stride;
             pr[b] = ra;
-            pg[b] = d->gate ? (const u64*)gate->d + (size_t)(i0 + b) * gate->ct_stride : nullptr;
             pres[b] = add ? (const u64*)residual->d + (size_t)(i0 + b) * residual->ct_stride : nullptr;
-            ptmp[b] = tmp + (size_t)b * 2 * L1 * N;
             out[b] = (u64*)d_out + (size_t)(i0 + b) * out_ct;
         }
-        size_t ts = x->comp_stride;
-        if (d->gate == HE_GATE_NONE) {
-            for (u32 b = 0; b < n; b++) pt[b] = px[b];
-        } else {
-            ts = (size_t)level * N;
-            if (d->gate == HE_GATE_PLAIN) {
-                if (mac) {  // the dropped limb of the products alone; the others where the division ends
-                    Arena sub = ar.rest();
-                    u64* w2 = sub.take((size_t)2 * n * level * N);
-                    if (!sub.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
-                    HIP_TRY(launch_gate_mul(c, level, level, n, px[0], x->ct_stride, x->comp_stride, pg[0], gate->ct_stride, tmp, st));
-                    HIP_TRY(launch_ntt(c, true, tmp, 1, tmp, 1, range_list(0, 1, level), 2 * n, st, nullptr, nullptr, c->d_rescale_prep_f, nullptr, nullptr, NTT_LO));
-                    const VecEpilogue ve = {px[0], x->ct_stride, x->comp_stride, pg[0], nullptr, gate->ct_stride, t, (size_t)2 * level * N,
-                                            c->d_rescale_ep + (size_t)level * 2 * c->num_q, level, RopePairs{}};
-                    HIP_TRY(launch_ntt_rescale_vec(c, level, VEC_GATE, (const double*)tmp, w2, 2 * n, ve, st));
-                } else {
-                    HIP_TRY(launch_gate_mul(c, level, 0, n, px[0], x->ct_stride, x->comp_stride, pg[0], gate->ct_stride, tmp, st));
-                    for (u32 b0 = 0; b0 < n; b0 += CT_BATCH)
-                        if ((rc = run_rescale(c, level, ptmp + b0, L1 * N, ot + b0, n - b0 < CT_BATCH ? n - b0 : CT_BATCH, ar.rest(), st))) return rc;
-                }
-            } else if ((rc = run_ctct_merged(c, level, px, x->comp_stride, pg, gate->comp_stride, nullptr, 0, rlk->d_key, ot, n, ar.rest(), st))) {
-                return rc;
-            }
-        }
-        if (!add) {
-            if ((rc = run_ctct_merged(c, last, pt, ts, pr, rs, nullptr, 0, rlk->d_key, out, n, ar.rest(), st))) return rc;
-        } else if (mac) {
+        const size_t ts = d->gate ? gl * N : x->comp_stride;
+        if (!add) return run_ctct_merged(c, last, pt, ts, pr, rs, nullptr, 0, rlk->d_key, out, n, sub, on);
+        if (mac) {
             const LinAddend lin = {pres, residual->comp_stride, kr.v, pres, residual->comp_stride, zero.v};
-            if ((rc = run_ctct_merged(c, last, pt, ts, pr, rs, nullptr, 0, rlk->d_key, out, n, ar.rest(), st, &lin))) return rc;
-        } else {  // the scaled residuals, compact
-            for (u32 b = 0; b < n; b++) HIP_TRY(launch_affine(c, last, pres[b], residual->comp_stride, kr, zero, tmp + (size_t)b * 2 * rs, st));
-            if ((rc = run_ctct_merged(c, last, pt, ts, pr, rs, tmp, 2 * rs, rlk->d_key, out, n, ar.rest(), st))) return rc;
+            return run_ctct_merged(c, last, pt, ts, pr, rs, nullptr, 0, rlk->d_key, out, n, sub, on, &lin);
         }
+        u64* scaled = sub.take((size_t)n * 2 * rs);
+        if (!sub.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
+        for (u32 b = 0; b < n; b++) HIP_TRY(launch_affine(c, last, pres[b], residual->comp_stride, kr, zero, scaled + (size_t)b * 2 * rs, on));
+        return run_ctct_merged(c, last, pt, ts, pr, rs, scaled, 2 * rs, rlk->d_key, out, n, sub.rest(), on);
+    };
+    auto fork = [&]() -> int {
+        HIP_TRY(hipEventRecord(c->ev_fork, st));
+        HIP_TRY(hipStreamWaitEvent(c->side, c->ev_fork, 0));
+        return CKKS_OK;
+    };
+    auto join = [&](int rc) -> int {  // also on the error paths: the caller's stream never runs ahead of the second one
+        hipError_t e = hipEventRecord(c->ev_join, c->side);
+        if (e == hipSuccess) e = hipStreamWaitEvent(st, c->ev_join, 0);
+        if (e != hipSuccess && rc == CKKS_OK) return set_hip_err(c, e);
+        return rc;
+    };
+    auto gates_of = [&](u32 c0, Arena sub, hipStream_t on) -> int {
+        const u32 end = d->channels - c0 < chunk ? d->channels : c0 + chunk;
+        for (u32 i0 = c0; i0 < end; i0 += nb)
+            if (int rc = run_gates(c0, i0, end - i0 < nb ? end - i0 : nb, sub, on)) return rc;
+        return CKKS_OK;
+    };
+    int rc;
+    if (gates_aside) {
+        if ((rc = fork())) return rc;
+        rc = gates_of(0, aside, c->side);
+        if (rc == CKKS_OK) rc = run_chain();
+        if ((rc = join(rc))) return rc;
+    } else {
+        if ((rc = run_chain())) return rc;
+    }
+    for (u32 c0 = 0; c0 < d->channels; c0 += chunk) {
+        if (d->gate && (c0 || !gates_aside))
+            if ((rc = gates_of(c0, ar.rest(), st))) return rc;
+        const u32 end = d->channels - c0 < chunk ? d->channels : c0 + chunk;
+        const bool turns = batches_aside && end - c0 > nb;
+        if (turns && (rc = fork())) return rc;
+        for (u32 i0 = c0, no = 0; i0 < end && rc == CKKS_OK; i0 += nb, no++)
+            rc = run_last(c0, i0, end - i0 < nb ? end - i0 : nb, turns && (no & 1) ? aside : ar.rest(), turns && (no & 1) ? c->side : st);
+        if (turns) rc = join(rc);
+        if (rc) return rc;
     }
     return CKKS_OK;
 }

@@ -244,8 +244,9 @@ inline bool ntt_has_modup(const ckks_ctx* c) { return c->ntt_f64 && c->log_n > C
 // The same for ModDown's conversion: y are the 2*batch extended polynomials ([E][N] each, the dropped limbs left as scaled
 // centred doubles by launch_ntt with the moddown prep table), dst the converted dropped part ([n_out][N] per polynomial,
 // NTT form), epilogue what the second pass does with it (null: the second pass is left out).  merged: the dropped set is {q_level, p_0..p_{k-1}}.
+// keep: that many limbs of the quotient (n_out), 0: all.
 hipError_t launch_ntt_moddown(const ckks_ctx* c, u32 level, bool merged, const double* y, u64* dst, u32 batch, hipStream_t st,
-                              const FwdEpilogue* epilogue, u32 mid_per = 0);
+                              const FwdEpilogue* epilogue, u32 mid_per = 0, u32 keep = 0);
 // The same for the rescale: y [batch][N] is the dropped limb `level` of every component (centred doubles, from launch_ntt
 // with d_rescale_prep_f), dst [batch][level][N] scratch, epilogue the subtraction and the multiplication by q_level^-1.
 hipError_t launch_ntt_rescale(const ckks_ctx* c, u32 level, const double* y, u64* dst, u32 batch, hipStream_t st,
@@ -273,8 +274,8 @@ struct RopePairs {
     __host__ __device__ u32 second(u32 j) const { return interleaved ? 2 * j + 1 : j + n_pairs; }
 };
 // Rescales of products with plaintexts (ntt_fwd_lo_vec_kernel): the limbs behind the dropped one formed from ciphertexts at equal distances and plaintexts p_stride
-// apart; out_ct words between outputs, out [2][level][N].  y: the dropped limbs of the products, [batch][N], through the inverse transform's first pass with
-// d_rescale_prep_f; w [batch][level][N] scratch.  batch: components, numbered as the kernel says.  Contexts with ntt_has_modup.
+// apart; out_ct words between outputs, out [2][n_out][N].  y: the dropped limbs of the products, [batch][N], through the inverse transform's first pass with
+// d_rescale_prep_f; w [batch][n_out][N] scratch.  batch: components, numbered as the kernel says.  Contexts with ntt_has_modup.
 enum VecMode { VEC_TURN = 0, VEC_GATE };
 struct VecEpilogue {
     const u64* in;
@@ -284,7 +285,7 @@ struct VecEpilogue {
     u64* out;
     size_t out_ct;
     const u64* cinv;  // q_level^-1 by limb
-    u32 level;
+    u32 n_out;        // limbs of a result, up to `level`
     RopePairs P;
 };
 hipError_t launch_ntt_rescale_vec(const ckks_ctx* c, u32 level, VecMode mode, const double* y, u64* w, u32 batch, const VecEpilogue& ve, hipStream_t st);
@@ -320,7 +321,7 @@ struct MacRotate {
     bool hoisted = false;  // all items rotate one ciphertext, whose own digits are finished (launch_ntt_modup without hi_only)
 };
 // n_part (with rot): the positions below inv_from are added up over the items, into *n_part partial sums at outs[0], outs[1], ...
-// dropped_only: nothing but the positions from inv_from on.  div: nothing but those below it, and the division's last step on them: outs[b] [2][inv_from][N] =
+// dropped_only: nothing but the positions from inv_from on.  div: nothing but those below it (which may be fewer than the division keeps), and the division's last step on them: outs[b] [2][inv_from][N] =
 // (sums - w) cinv + adds[b], w what launch_ntt_moddown left without an epilogue.
 struct MacDivide {
     const double* w;

@@ -840,7 +840,7 @@ __global__ __launch_bounds__(NTT_THREADS) void ntt_fwd_lo_vec_kernel(NttArgs arg
     fwd_lo_rounds(v, lds0, lds1, tid, wa, wb, wc, wd, P.mc);
     const size_t row = ((size_t)i << args.log_n) + off + tid;
     const u64 *x0, *x1, *p0, *p1 = nullptr;
-    u64* o0 = ve.out + ((size_t)(comp * ve.level + i) << args.log_n) + off + tid;
+    u64* o0 = ve.out + ((size_t)(comp * ve.n_out + i) << args.log_n) + off + tid;
     u64* o1 = o0;
     if constexpr (MODE == VEC_TURN) {
         const u32 z = ve.P.z0 + zr, j = z % ve.P.n_pairs;
@@ -856,7 +856,7 @@ __global__ __launch_bounds__(NTT_THREADS) void ntt_fwd_lo_vec_kernel(NttArgs arg
         x1 = x0 + ve.in_comp;
         p0 = ve.p0 + zr * ve.p_stride + row;
         o0 += zr * ve.out_ct;
-        o1 = o0 + ((size_t)ve.level << args.log_n);
+        o1 = o0 + ((size_t)ve.n_out << args.log_n);
     }
     u64 a[8], b[8], c[8], s[8];
 #pragma unroll
@@ -2789,7 +2789,8 @@ hipError_t launch_ntt_rescale_share(const ckks_ctx* c, u32 level, const double* 
 }
 
 hipError_t launch_ntt_rescale_vec(const ckks_ctx* c, u32 level, VecMode mode, const double* y, u64* w, u32 batch, const VecEpilogue& ve, hipStream_t st) {
-    if (level == 0 || !ntt_has_modup(c) || batch % (mode == VEC_TURN ? 4 : 2)) return hipErrorInvalidValue;
+    if (level == 0 || !ntt_has_modup(c) || ve.n_out == 0 || ve.n_out > level || batch % (mode == VEC_TURN ? 4 : 2)) return hipErrorInvalidValue;
+    const u32 n_out = ve.n_out;
     ConvPrologue cp = {};
     cp.y = y;
     cp.y_bstride = c->N;
@@ -2797,15 +2798,15 @@ hipError_t launch_ntt_rescale_vec(const ckks_ctx* c, u32 level, VecMode mode, co
     cp.nd = 1;
     cp.ap = 4;
     PolyList pl;
-    for (u32 a = 0; a < CKKS_MAX_MODULI; a++) pl.spos[a] = pl.dpos[a] = pl.mod[a] = (unsigned char)(a < level ? a : 0);
-    pl.n = level;
+    for (u32 a = 0; a < CKKS_MAX_MODULI; a++) pl.spos[a] = pl.dpos[a] = pl.mod[a] = (unsigned char)(a < n_out ? a : 0);
+    pl.n = n_out;
     const MidPrologue mp = {c->d_itwf, c->d_itwf_val, c->d_rescale_prep_f, level, level};
-    cp.per = mid_conv_per_of(c, 1, 4, level, batch);
+    cp.per = mid_conv_per_of(c, 1, 4, n_out, batch);
     if (!cp.per) return hipErrorInvalidValue;  // a single source limb always goes through its second pass there
-    if (hipError_t e = launch_ntt_any(c, false, w, level, w, level, pl, batch, st, nullptr, nullptr, nullptr, &cp, nullptr, nullptr, NTT_HI, &mp); e != hipSuccess) return e;
+    if (hipError_t e = launch_ntt_any(c, false, w, n_out, w, n_out, pl, batch, st, nullptr, nullptr, nullptr, &cp, nullptr, nullptr, NTT_HI, &mp); e != hipSuccess) return e;
     NttArgs args = {};
     args.src = args.dst = w;
-    args.src_bstride = args.dst_bstride = level;
+    args.src_bstride = args.dst_bstride = n_out;
     args.mc = c->d_mcf;
     args.tw = c->d_twf;
     args.tw_val = c->d_twf_val;
@@ -2814,12 +2815,12 @@ hipError_t launch_ntt_rescale_vec(const ckks_ctx* c, u32 level, VecMode mode, co
     args.log_hi = c->log_hi;
     args.last = 1;
     args.batch = batch;
-    const u32 slices = level << c->log_hi;
+    const u32 slices = n_out << c->log_hi;
     for (u32 g = 64; g >= 8; g >>= 1)
         if (slices % g == 0) { args.lo_group = g; break; }
     const u32 items = batch / 2;  // two results a workgroup
     const dim3 grid = args.lo_group ? dim3(args.lo_group, items, slices / args.lo_group) : dim3(items, slices);
-    ProfScope ps__(c, K_NTT_FWD_LO, st, (mode == VEC_TURN ? 36.0 : 28.0) * batch * level * c->N, 0.5 * batch * level * c->N * c->log_lo);
+    ProfScope ps__(c, K_NTT_FWD_LO, st, (mode == VEC_TURN ? 36.0 : 28.0) * batch * n_out * c->N, 0.5 * batch * n_out * c->N * c->log_lo);
     if (mode == VEC_TURN) hipLaunchKernelGGL(ntt_fwd_lo_vec_kernel<VEC_TURN>, grid, dim3(NTT_THREADS), 0, st, args, pl, ve);
     else hipLaunchKernelGGL(ntt_fwd_lo_vec_kernel<VEC_GATE>, grid, dim3(NTT_THREADS), 0, st, args, pl, ve);
     return hipGetLastError();
@@ -2935,9 +2936,9 @@ hipError_t launch_ntt_lo_mac(const ckks_ctx* c, u32 level, const DigitSrc& digit
 }
 
 hipError_t launch_ntt_moddown(const ckks_ctx* c, u32 level, bool merged, const double* y, u64* dst, u32 batch, hipStream_t st,
-                              const FwdEpilogue* epilogue, u32 mid_per) {
+                              const FwdEpilogue* epilogue, u32 mid_per, u32 keep) {
     if (merged && level == 0) return hipErrorInvalidValue;
-    const u32 n_out = merged ? level : level + 1;
+    const u32 n_out = keep ? keep : (merged ? level : level + 1);
     ConvPrologue cp;
     cp.y = y;
     cp.y_bstride = (size_t)c->ext_limbs(level) * c->N;

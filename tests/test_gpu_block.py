@@ -239,6 +239,84 @@ def test_norm_of_a_large_ring():
     norm_case((16, 6, 2, 3, 50), 5, 4, 1, "cipher", True, 8, strided=True)
 
 
+@pytest.mark.parametrize("gate,residual", [("cipher", True), ("plain", False), (None, True)])
+def test_norm_over_two_streams(gate, residual):
+    """Sizes at which the gates run beside the chain and the last products in turn on two streams, with the inner products of the limbs that stay
+    inside the division: the residues of one stream, of a workspace for one stream, and (three channels) of the oracle; then from a graph."""
+    p, orc, ctx = world(16, 6, 2, 3)
+    rng = np.random.default_rng(21)
+    level, channels, its = 5, 40, 1
+    last = level - 2 - 2 * its
+    x = ciphertexts(rng, p, level, channels)
+    g = {None: None, "plain": np.stack([rand_poly(rng, p.moduli[:level + 1], orc.N) for _ in range(channels)]), "cipher": ciphertexts(rng, p, level, channels)}[gate]
+    res = ciphertexts(rng, p, last, channels) if residual else None
+    key = np.stack([rand_ct(rng, p.moduli, p.num_q + p.num_p - 1, orc.N) for _ in range(p.dnum)])
+    rlk, k = hx.ckks_key_load(ctx, hx.from_host(key), 0), (1 << 40, -(3 << 47), 5 << 48, 1 << 49, -(3 << 49))
+    dx, dg, dr = (None if a is None else hx.from_host(a) for a in (x, g, res))
+
+    def call(ws=None, out=None):
+        return hx.he_norm_gate(ctx, level, dx, k[0], k[1], k[2], k[4:], rlk, dg, dr, k[3], ws=ws, out=out)
+    two = hx.to_host(call())
+    kind = {None: B.HE_GATE_NONE, "plain": B.HE_GATE_PLAIN, "cipher": B.HE_GATE_CIPHER}[gate]
+    need = hx.he_norm_workspace_bytes(ctx, level, channels, its, kind)
+    try:
+        hx.ckks_ctx_set_overlap(ctx, False)
+        assert np.array_equal(hx.to_host(call()), two)
+    finally:
+        hx.ckks_ctx_set_overlap(ctx, True)
+    only = (0, 17, 39)
+    want = orc.norm_gate(x, level, k[0], k[1], k[2], k[4:], key, g, res, k[3], only=only)
+    for c, w in zip(only, want):
+        assert np.array_equal(two[c], w), c
+    ws, out = torch.empty(need, dtype=torch.uint8, device="cuda"), hx.empty(channels, 2, last, orc.N)
+    call(ws, out)
+    torch.cuda.synchronize()
+    st, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        call(ws, out)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(hx.to_host(out), two)
+        assert np.array_equal(hx.to_host(call(torch.empty_like(ws))), two)
+
+
+@pytest.mark.parametrize("bits", [50, 56])
+def test_grouped_product_of_more_outputs_than_go_together(bits):
+    """1100 outputs: two parts of a row, the second ragged (the transforms number 1024 outputs' components), in both arithmetics."""
+    p, orc, ctx = world(12, 3, 1, 1, bits)
+    rng = np.random.default_rng(bits)
+    x = ciphertexts(rng, p, 1, 2 * 9)
+    w = rng.integers(-32768, 32768, size=(1, 1100, 9)).astype(np.int16)
+    b = np.stack([rng.integers(0, q, size=(1, 1100), dtype=np.uint64) for q in p.moduli[:2]], -1)
+    got = hx.to_host(hx.he_linear_grouped(ctx, 1, (2,), hx.from_host(x).unflatten(0, (2, 9)), torch.from_numpy(w).cuda(), 77, hx.from_host(b)))
+    for t, o in ((0, 0), (0, 639), (1, 640), (1, 1023), (0, 1024), (1, 1099)):
+        want = orc.linear_grouped([x[9 * t:9 * t + 9]], 1, (1,), w[:, o:o + 1], 77, b[:, o:o + 1])
+        assert np.array_equal(got[t, o], want[0][0]), (t, o)
+
+
+def test_grouped_product_and_rotary_positions_in_several_batches():
+    """More outputs and pairs than go through the transforms together (1024 components' limbs, 512 MB of converted limbs): one group of 600 rows on a small ring, and
+    36 pairs of 2^16 points and 6 limbs, against the same calls in parts."""
+    p, orc, ctx = world(12, 3, 1, 1)
+    rng = np.random.default_rng(31)
+    x = hx.from_host(ciphertexts(rng, p, 2, 600 * 3)).unflatten(0, (600, 3))
+    w = torch.from_numpy(rng.integers(-128, 128, size=(1, 2, 3)).astype(np.int8)).cuda()
+    whole = hx.he_linear_grouped(ctx, 2, (600,), x, w, 12345)
+    for r in (0, 511, 512, 599):
+        assert torch.equal(whole[r:r + 1], hx.he_linear_grouped(ctx, 2, (1,), x[r:r + 1], w, 12345)), r
+    assert np.array_equal(hx.to_host(whole[599]), np.array(orc.linear_grouped([hx.to_host(x[599])], 2, (1,), w.cpu().numpy(), 12345)[0]))
+    p, orc, ctx = world(16, 6, 2, 3)
+    level, heads, n_pairs = 5, 9, 4
+    x = hx.from_host(ciphertexts(rng, p, level, 9)).repeat(heads, 1, 1, 1).unflatten(0, (heads, 9))
+    x[1:] = x[1:].flip(1)
+    tab = [hx.from_host(np.stack([rand_poly(rng, p.moduli[:level + 1], orc.N) for _ in range(n_pairs)])) for _ in range(2)]
+    whole = hx.he_rope_axes(ctx, level, x, *tab, interleaved=True)
+    for h in (0, 1, 5, 8):
+        assert torch.equal(whole[h:h + 1], hx.he_rope_axes(ctx, level, x[h:h + 1], *tab, interleaved=True)), h
+
+
 # ------------------------------------------------------------------------------------------ together, streams, graphs, refusals
 def block_calls(ctx, level, x, w, tab, rlk, k, ws):
     h = hx.he_norm_gate(ctx, level, x, k[0], k[1], k[2], k[3:], rlk, ws=ws)
