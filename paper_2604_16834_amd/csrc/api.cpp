@@ -2070,8 +2070,14 @@ struct LinearPlan {
     u64 rows;      // in all
     bool share;
     u32 outs;      // outputs of a row at a time
-    u32 row_step;  // rows at a time
+    u32 row_step;  // rows at a time, of any groups
+    u32 groups;    // groups at a time, by the digits of their weights
 };
+// Weights' digits in the workspace: of as many groups as these bytes hold
+#define LINEAR_DIGIT_BYTES ((size_t)256 << 20)
+static size_t linear_digits(const ckks_ctx* c, const he_linear_desc* d, u32 outs) {
+    return linear_mfma_applies(c, d->c_in) ? linear_mfma_scratch_elems(d->c_in, outs, d->weight_type) : 0;
+}
 static int linear_plan(const ckks_ctx* c, const he_linear_desc* d, const u32* h_rows, LinearPlan* p) {
     if (!d || !h_rows) return set_err(c, CKKS_ERR_INVALID_ARG, "null descriptor or row counts");
     if (d->c_in == 0 || d->c_out == 0 || d->n_groups == 0 || d->c_in > 65536 || d->c_out > 65536)
@@ -2081,10 +2087,10 @@ static int linear_plan(const ckks_ctx* c, const he_linear_desc* d, const u32* h_
     if (d->multiplier == 0) return set_err(c, CKKS_ERR_INVALID_ARG, "multiplier is zero");
     if (!level_ok(c, d->level) || d->level < 1) return set_err(c, CKKS_ERR_LEVEL_MISMATCH, "grouped product needs 1 <= level < num_q");
     p->rows = 0;
-    u32 most = 0;
+    u32 used = 0;
     for (u32 g = 0; g < d->n_groups; g++) {
         p->rows += h_rows[g];
-        if (h_rows[g] > most) most = h_rows[g];
+        if (h_rows[g]) used++;
     }
     if (p->rows > (u64)1 << 24) return set_err(c, CKKS_ERR_INVALID_ARG, "too many rows");
     p->share = ntt_has_modup(c) && !(p->rows * d->c_out <= CT_BATCH && ntt_rescale_one_launch(c, d->level, 2 * (u32)p->rows * d->c_out));
@@ -2096,16 +2102,15 @@ static int linear_plan(const ckks_ctx* c, const he_linear_desc* d, const u32* h_
         p->outs = even < cap ? even : cap;
     }
     p->row_step = p->outs < d->c_out ? 1 : cap / p->outs;
-    if (p->row_step > most) p->row_step = most;
-    if (p->row_step == 0) p->row_step = 1;
+    if (p->row_step > p->rows) p->row_step = p->rows ? (u32)p->rows : 1;
+    const size_t bytes = linear_digits(c, d, p->outs) * sizeof(u64), g = bytes ? LINEAR_DIGIT_BYTES / bytes : LINEAR_GROUPS;
+    p->groups = g < 1 ? 1 : (g > LINEAR_GROUPS ? LINEAR_GROUPS : (u32)g);
+    if (p->groups > used) p->groups = used ? used : 1;
     return CKKS_OK;
-}
-static size_t linear_digits(const ckks_ctx* c, const he_linear_desc* d, const LinearPlan& p) {
-    return linear_mfma_applies(c, d->c_in) ? linear_mfma_scratch_elems(d->c_in, p.outs, d->weight_type) : 0;
 }
 static size_t ws_linear(const ckks_ctx* c, const he_linear_desc* d, const LinearPlan& p) {
     const size_t outs = (size_t)p.row_step * p.outs;
-    return blk(outs * 2 * (p.share ? 1 : d->level + 1) * c->N) + blk(linear_digits(c, d, p)) + (p.share ? 0 : ws_rescale(c, d->level, CT_BATCH));
+    return blk(outs * 2 * (p.share ? 1 : d->level + 1) * c->N) + blk(p.groups * linear_digits(c, d, p.outs)) + (p.share ? 0 : ws_rescale(c, d->level, CT_BATCH));
 }
 size_t he_linear_workspace_bytes(const ckks_ctx* c, const he_linear_desc* d, const uint32_t* h_group_rows) {
     LinearPlan p;
@@ -2128,7 +2133,7 @@ int he_linear_grouped(const ckks_ctx* c, const he_linear_desc* d, const uint32_t
     const size_t N = c->N, out_ct = (size_t)2 * level * N;
     Arena ar(d_ws, ws_bytes);
     u64* sums = ar.take((size_t)p.row_step * p.outs * 2 * (p.share ? 1 : L1) * N);
-    u64* digits = ar.take(linear_digits(c, d, p));
+    u64* digits = ar.take(p.groups * linear_digits(c, d, p.outs));
     LinearSum S;
     S.in_ct = in->ct_stride;
     S.in_comp = in->comp_stride;
@@ -2137,6 +2142,8 @@ int he_linear_grouped(const ckks_ctx* c, const he_linear_desc* d, const uint32_t
     S.weight_bytes = d->weight_type;
     S.w_out = d->transposed ? 1 : d->c_in;
     S.w_in = d->transposed ? d->c_out : 1;
+    S.w_group = (size_t)d->c_in * d->c_out;
+    S.bias_group = (size_t)d->c_out * L1;
     S.bias_limbs = L1;
     LimbScalars mult, one, mult_q, inv_q;  // (.. q_level^-1)
     for (u32 i = 0; i < CKKS_MAX_MODULI; i++) {
@@ -2146,54 +2153,64 @@ int he_linear_grouped(const ckks_ctx* c, const he_linear_desc* d, const uint32_t
         inv_q.v[i] = q && p.share ? c->rescale_inv[(size_t)level * c->num_q + i] : 0;
         mult_q.v[i] = q ? (u64)((unsigned __int128)mult.v[i] * inv_q.v[i] % q) : 0;
     }
-    u64 t0 = 0;
-    for (u32 g = 0; g < d->n_groups; t0 += h_group_rows[g], g++) {
+    u32 g = 0, done = 0;  // the next row is row `done` of group g
+    for (u64 t0 = 0; t0 < p.rows; t0 += S.rows) {
+        // the rows of this round: up to row_step, of up to `groups` groups
+        S.rows = 0;
+        S.groups.n = S.groups.pad = 0;
+        for (u32 i = 0; i < LINEAR_GROUPS; i++) S.groups.row_end[i] = S.groups.id[i] = 0;
+        while (g < d->n_groups && S.rows < p.row_step) {
+            const u32 left = h_group_rows[g] - done, n = left < p.row_step - S.rows ? left : p.row_step - S.rows;
+            if (n) {
+                if (S.groups.n == p.groups) break;
+                S.rows += n;
+                S.groups.id[S.groups.n] = g;
+                S.groups.row_end[S.groups.n++] = S.rows;
+            }
+            if (n == left) g++, done = 0;
+            else done += n;
+        }
         for (u32 o0 = 0; o0 < d->c_out; o0 += p.outs) {
-            const u32 no = d->c_out - o0 < p.outs ? d->c_out - o0 : p.outs;
+            const u32 no = d->c_out - o0 < p.outs ? d->c_out - o0 : p.outs, n_ct = S.rows * no;
+            u64* out = (u64*)d_out + (t0 * d->c_out + o0) * out_ct;  // (several rows only where a row goes as a whole: their outputs follow each other)
             S.c_out = no;
-            S.w = (const char*)d_w + ((size_t)g * d->c_in * d->c_out + o0 * S.w_out) * d->weight_type;
-            S.bias = d_bias ? (const u64*)d_bias + ((size_t)g * d->c_out + o0) * L1 : nullptr;
-            for (u32 r0 = 0; r0 < h_group_rows[g]; r0 += p.row_step) {
-                const u32 nr = h_group_rows[g] - r0 < p.row_step ? h_group_rows[g] - r0 : p.row_step;
-                u64* out = (u64*)d_out + ((t0 + r0) * d->c_out + o0) * out_ct;
-                S.rows = nr;
-                S.in = (const u64*)in->d + (t0 + r0) * S.in_row;
-                S.add = 0;
-                S.mult = mult;
-                S.bias_mult = one;
-                S.acc = sums;
-                S.limb0 = p.share ? level : 0;
-                S.limbs = p.share ? 1 : L1;
-                S.acc_comp = S.limbs * N;
-                S.acc_ct = 2 * S.acc_comp;
-                S.acc_row = no * S.acc_ct;
-                HIP_TRY(launch_linear_sum(c, S, digits, r0 > 0, st));
-                if (p.share) {  // (nr > 1 only for whole rows: the outputs follow each other)
-                    HIP_TRY(launch_ntt(c, true, sums, 1, sums, 1, range_list(0, 1, level), 2 * nr * no, st, nullptr, nullptr, c->d_rescale_prep_f, nullptr, nullptr, NTT_LO));
-                    HIP_TRY(launch_ntt_rescale_share(c, level, (const double*)sums, out, 2 * nr * no, st));
-                    S.add = 1;
-                    S.mult = mult_q;
-                    S.bias_mult = inv_q;
-                    S.limb0 = 0;
-                    S.limbs = level;
-                    S.acc = out;
-                    S.acc_comp = (size_t)level * N;
-                    S.acc_ct = out_ct;
-                    S.acc_row = no * out_ct;
-                    HIP_TRY(launch_linear_sum(c, S, digits, true, st));
-                    continue;
+            S.w = (const char*)d_w + o0 * S.w_out * d->weight_type;
+            S.bias = d_bias ? (const u64*)d_bias + (size_t)o0 * L1 : nullptr;
+            S.in = (const u64*)in->d + t0 * S.in_row;
+            S.add = 0;
+            S.mult = mult;
+            S.bias_mult = one;
+            S.acc = sums;
+            S.limb0 = p.share ? level : 0;
+            S.limbs = p.share ? 1 : L1;
+            S.acc_comp = S.limbs * N;
+            S.acc_ct = 2 * S.acc_comp;
+            S.acc_row = no * S.acc_ct;
+            HIP_TRY(launch_linear_sum(c, S, digits, false, st));
+            if (p.share) {
+                HIP_TRY(launch_ntt(c, true, sums, 1, sums, 1, range_list(0, 1, level), 2 * n_ct, st, nullptr, nullptr, c->d_rescale_prep_f, nullptr, nullptr, NTT_LO));
+                HIP_TRY(launch_ntt_rescale_share(c, level, (const double*)sums, out, 2 * n_ct, st));
+                S.add = 1;
+                S.mult = mult_q;
+                S.bias_mult = inv_q;
+                S.limb0 = 0;
+                S.limbs = level;
+                S.acc = out;
+                S.acc_comp = (size_t)level * N;
+                S.acc_ct = out_ct;
+                S.acc_row = no * out_ct;
+                HIP_TRY(launch_linear_sum(c, S, digits, true, st));
+                continue;
+            }
+            for (u32 i0 = 0; i0 < n_ct; i0 += CT_BATCH) {
+                const u32 n = n_ct - i0 < CT_BATCH ? n_ct - i0 : CT_BATCH;
+                const u64* src[CT_BATCH];
+                u64* dst[CT_BATCH];
+                for (u32 b = 0; b < n; b++) {
+                    src[b] = sums + (i0 + b) * S.acc_ct;
+                    dst[b] = out + (i0 + b) * out_ct;
                 }
-                for (u32 i0 = 0; i0 < nr * no; i0 += CT_BATCH) {
-                    const u32 n = nr * no - i0 < CT_BATCH ? nr * no - i0 : CT_BATCH;
-                    const u64* src[CT_BATCH];
-                    u64* dst[CT_BATCH];
-                    for (u32 b = 0; b < n; b++) {
-                        const u32 i = i0 + b;
-                        src[b] = sums + i * S.acc_ct;
-                        dst[b] = out + ((size_t)(i / no) * d->c_out + i % no) * out_ct;
-                    }
-                    if (int rc = run_rescale(c, level, src, (size_t)L1 * N, dst, n, ar.rest(), st)) return rc;
-                }
+                if (int rc = run_rescale(c, level, src, (size_t)L1 * N, dst, n, ar.rest(), st)) return rc;
             }
         }
     }

@@ -10,12 +10,13 @@ struct LinearArgs {
     const u64* in;
     size_t in_ct, in_comp, in_row;
     const void* w;
-    size_t w_out, w_in;
+    size_t w_out, w_in, w_group, bias_group;
     const u64* bias;
     u64* acc;
     size_t acc_ct, acc_comp, acc_row;
     u32 N, limb0, limbs, bias_limbs, c_in, c_out, o_tiles, add;
     LimbScalars mult, bias_mult;
+    LinearGroups groups;
 };
 // Any modulus.  The products are summed as signed 128-bit integers: a term is below 2^31 q in magnitude, 2^16 of them below 2^47 q, so with 2^48 q
 // added the sum is positive and below 2^49 q, which barrett_reduce takes.
@@ -27,7 +28,9 @@ __global__ __launch_bounds__(BK_THREADS) void linear_sum_kernel(LinearArgs A, co
     const u32 er = blockIdx.y % A.limbs, e = A.limb0 + er, comp = blockIdx.y / A.limbs, row = blockIdx.z / A.o_tiles, o0 = blockIdx.z % A.o_tiles * LG_OUT_TILE;
     const ModConst m = mc[e];
     const u64* src = A.in + row * A.in_row + comp * A.in_comp + (size_t)e * A.N + x;
-    const W* w = (const W*)A.w;
+    const u32 group = A.groups.id[A.groups.of_row(row)];
+    const W* w = (const W*)A.w + group * A.w_group;
+    const u64* bias = A.bias ? A.bias + group * A.bias_group : nullptr;
     __int128 sum[LG_OUT_TILE];
 #pragma unroll
     for (u32 t = 0; t < LG_OUT_TILE; t++) sum[t] = 0;
@@ -48,7 +51,7 @@ __global__ __launch_bounds__(BK_THREADS) void linear_sum_kernel(LinearArgs A, co
         r.lo = (u64)s;
         r.hi = (u64)(s >> 64);
         u64 v = mulmod_barrett(barrett_reduce(r, m), A.mult.v[e], m);
-        if (A.bias && comp == 0) v = add_mod(v, mulmod_barrett(A.bias[(size_t)o * A.bias_limbs + e], A.bias_mult.v[e], m), m.q);
+        if (bias && comp == 0) v = add_mod(v, mulmod_barrett(bias[(size_t)o * A.bias_limbs + e], A.bias_mult.v[e], m), m.q);
         u64* acc = A.acc + row * A.acc_row + o * A.acc_ct + comp * A.acc_comp + (size_t)er * A.N + x;
         *acc = A.add ? add_mod(v, *acc, m.q) : v;
     }
@@ -62,6 +65,9 @@ __global__ __launch_bounds__(BK_THREADS) void linear_sum_f64_kernel(LinearArgs A
     const u32 tid = threadIdx.x, x = blockIdx.x * BK_THREADS + tid, xc = x < A.N ? x : A.N - 1;
     const u32 er = blockIdx.y % A.limbs, e = A.limb0 + er, comp = blockIdx.y / A.limbs, row = blockIdx.z / A.o_tiles, o0 = blockIdx.z % A.o_tiles * OT;
     const ModConstF m = mcf[e];
+    const u32 group = A.groups.id[A.groups.of_row(row)];
+    const W* w = (const W*)A.w + group * A.w_group;
+    const u64* bias = A.bias ? A.bias + group * A.bias_group : nullptr;
     const u64* src = A.in + row * A.in_row + comp * A.in_comp + (size_t)e * A.N + xc;
     u64* acc = A.acc + row * A.acc_row + o0 * A.acc_ct + comp * A.acc_comp + (size_t)er * A.N + xc;
     const u32 n_out = A.c_out - o0 < OT ? A.c_out - o0 : OT;
@@ -82,7 +88,7 @@ __global__ __launch_bounds__(BK_THREADS) void linear_sum_f64_kernel(LinearArgs A
         if (c0) __syncthreads();
         if (tid < 8 * OT) {
             const u32 a = tid / OT, t = tid % OT;
-            lw[tid] = a < n && t < n_out ? (double)(int)((const W*)A.w)[(o0 + t) * A.w_out + (c0 + a) * A.w_in] : 0.0;
+            lw[tid] = a < n && t < n_out ? (double)(int)w[(o0 + t) * A.w_out + (c0 + a) * A.w_in] : 0.0;
         }
         __syncthreads();
         double tt[OT], lo[OT];
@@ -104,8 +110,8 @@ __global__ __launch_bounds__(BK_THREADS) void linear_sum_f64_kernel(LinearArgs A
     for (u32 t = 0; t < OT; t++) {
         if (t >= n_out) return;
         double v = f64m_mulmod_any(sum[t], k, m.q, m.qinv);
-        if (A.bias && comp == 0)
-            v = f64m_reduce(v + f64m_mulmod_any(f64m_from_u64(A.bias[(size_t)(o0 + t) * A.bias_limbs + e]), kb, m.q, m.qinv), m.q, m.qinv);
+        if (bias && comp == 0)
+            v = f64m_reduce(v + f64m_mulmod_any(f64m_from_u64(bias[(size_t)(o0 + t) * A.bias_limbs + e]), kb, m.q, m.qinv), m.q, m.qinv);
         if (A.add) v = f64m_reduce(v + f64m_from_u64(old[t]), m.q, m.qinv);
         acc[t * A.acc_ct] = f64m_canonical(v, m.q);
     }
@@ -114,12 +120,11 @@ __global__ __launch_bounds__(BK_THREADS) void linear_sum_f64_kernel(LinearArgs A
 hipError_t launch_linear_sum(const ckks_ctx* c, const LinearSum& S, u64* scratch, bool prepared, hipStream_t st) {
     if (linear_mfma_applies(c, S.c_in)) return launch_linear_mfma(c, S, scratch, prepared, st);
     const u32 tile = c->small_q ? (S.c_out <= 2 ? S.c_out : 8) : LG_OUT_TILE, o_tiles = (S.c_out + tile - 1) / tile;
-    for (u32 r0 = 0; r0 < S.rows;) {  // the launch's third dimension holds 65535 workgroups
-        const u32 most = 65535 / o_tiles, n = S.rows - r0 < most ? S.rows - r0 : most;
-        const dim3 grid((c->N + BK_THREADS - 1) / BK_THREADS, 2 * S.limbs, n * o_tiles);
-        const LinearArgs A = {S.in + r0 * S.in_row, S.in_ct, S.in_comp, S.in_row, S.w, S.w_out, S.w_in, S.bias, S.acc + r0 * S.acc_row, S.acc_ct, S.acc_comp, S.acc_row,
-                              c->N, S.limb0, S.limbs, S.bias_limbs, S.c_in, S.c_out, o_tiles, S.add, S.mult, S.bias_mult};
-        ProfScope ps__(c, K_WEIGHTED_SUM, st, 16.0 * n * c->N * S.limbs * (S.c_in + (1.0 + S.add) * S.c_out), 2.0 * n * c->N * S.limbs * S.c_in * S.c_out);
+    if (S.groups.n == 0 || S.groups.n > LINEAR_GROUPS || (u64)S.rows * S.c_out > 1024) return hipErrorInvalidValue;  // (the grid's third dimension)
+    const dim3 grid((c->N + BK_THREADS - 1) / BK_THREADS, 2 * S.limbs, S.rows * o_tiles);
+    const LinearArgs A = {S.in, S.in_ct, S.in_comp, S.in_row, S.w, S.w_out, S.w_in, S.w_group, S.bias_group, S.bias, S.acc, S.acc_ct, S.acc_comp, S.acc_row,
+                          c->N, S.limb0, S.limbs, S.bias_limbs, S.c_in, S.c_out, o_tiles, S.add, S.mult, S.bias_mult, S.groups};
+    ProfScope ps__(c, K_WEIGHTED_SUM, st, 16.0 * S.rows * c->N * S.limbs * (S.c_in + (1.0 + S.add) * S.c_out), 2.0 * S.rows * c->N * S.limbs * S.c_in * S.c_out);
 #define LINEAR_F64(W, OT) hipLaunchKernelGGL((linear_sum_f64_kernel<W, OT>), grid, dim3(BK_THREADS), 0, st, A, c->d_mcf)
 #define LINEAR_SUM(W)                                                                                            \
     {                                                                                                            \
@@ -128,13 +133,11 @@ hipError_t launch_linear_sum(const ckks_ctx* c, const LinearSum& S, u64* scratch
         else if (tile == 2) LINEAR_F64(W, 2);                                                                    \
         else LINEAR_F64(W, 8);                                                                                   \
     }
-        if (S.weight_bytes == 1) LINEAR_SUM(int8_t)
-        else if (S.weight_bytes == 2) LINEAR_SUM(int16_t)
-        else LINEAR_SUM(int32_t)
+    if (S.weight_bytes == 1) LINEAR_SUM(int8_t)
+    else if (S.weight_bytes == 2) LINEAR_SUM(int16_t)
+    else LINEAR_SUM(int32_t)
 #undef LINEAR_SUM
 #undef LINEAR_F64
-        r0 += n;
-    }
     return hipGetLastError();
 }
 

@@ -402,21 +402,35 @@ hipError_t launch_lincomb2(const ckks_ctx* c, u32 level, const PtrList8& a, size
 struct LimbScalars {
     u64 v[CKKS_MAX_MODULI];
 };
-// Sums over channels for one expert's rows, on limbs limb0 .. limb0 + limbs - 1:  acc = (add ? acc : 0) + mult * sum_c W in + bias_mult * bias (component 0)
+// Sums over channels for the rows of up to LINEAR_GROUPS experts, on limbs limb0 .. limb0 + limbs - 1:
+//   acc = (add ? acc : 0) + mult * sum_c W_g in + bias_mult * bias_g (component 0)
+#define LINEAR_GROUPS 64
+struct LinearGroups {
+    u32 n, pad;
+    u32 row_end[LINEAR_GROUPS];  // rows row_end[i - 1] .. row_end[i] - 1 of the launch belong to group id[i]
+    u32 id[LINEAR_GROUPS];
+    __host__ __device__ u32 of_row(u32 row) const {
+        u32 i = 0;
+        while (i + 1 < n && row >= row_end[i]) i++;
+        return i;
+    }
+};
 struct LinearSum {
     const u64* in;                  // limb 0
     size_t in_ct, in_comp, in_row;  // words
-    u32 rows, c_in, c_out;
+    u32 rows, c_in, c_out;          // rows * c_out <= 1024
+    LinearGroups groups;
     const void* w;
     u32 weight_bytes;
-    size_t w_out, w_in;
-    const u64* bias;                // [c_out][bias_limbs], or null
+    size_t w_out, w_in, w_group;    // weights
+    const u64* bias;                // [c_out][bias_limbs] of group 0, or null
+    size_t bias_group;
     u32 bias_limbs, limb0, limbs, add;
     u64* acc;                       // limb limb0 of the first output
     size_t acc_ct, acc_comp, acc_row;
     LimbScalars mult, bias_mult;    // by modulus
 };
-// scratch: linear_mfma_scratch_elems words where linear_mfma_applies; prepared: they hold this expert's weights from the call before
+// scratch: groups.n times linear_mfma_scratch_elems words where linear_mfma_applies; prepared: they hold these groups' weights from the call before
 hipError_t launch_linear_sum(const ckks_ctx* c, const LinearSum& S, u64* scratch, bool prepared, hipStream_t st);
 // linear_mfma.hip
 bool linear_mfma_applies(const ckks_ctx* c, u32 c_in);

@@ -31,14 +31,16 @@ typedef int v16i __attribute__((ext_vector_type(16)));
 #define LM_CHUNK 256                 // channels of a launch
 #define LM_KEEP_ORDER asm volatile("" ::: "memory"); __builtin_amdgcn_sched_barrier(0);
 
-// ---- weights -> digit planes in A-operand layout: wa[((ot*KS + ks)*DW + dw)*64 + lane] = 16 bytes, digit dw of
+// ---- weights -> digit planes in A-operand layout, group by group (blockIdx.y): wa[((ot*KS + ks)*DW + dw)*64 + lane] = 16 bytes, digit dw of
 //   W[32*ot + lane%32][32*ks + 16*(lane/32) + j], j < 16  (zero beyond c_out and c_in)
 template <class W>
-__global__ __launch_bounds__(LM_THREADS) void linear_prep_kernel(const W* __restrict__ w, size_t w_out, size_t w_in, uint4* __restrict__ wa, u32 c_out,
-                                                                 u32 c_in, u32 KS, u32 OT) {
+__global__ __launch_bounds__(LM_THREADS) void linear_prep_kernel(const W* __restrict__ w, size_t w_out, size_t w_in, size_t w_group, LinearGroups groups,
+                                                                 uint4* __restrict__ wa, size_t wa_group, u32 c_out, u32 c_in, u32 KS, u32 OT) {
     constexpr u32 DW = sizeof(W);
     const u32 idx = blockIdx.x * LM_THREADS + threadIdx.x;
     if (idx >= OT * KS * DW * 64) return;
+    w += groups.id[blockIdx.y] * w_group;
+    wa += blockIdx.y * wa_group;
     const u32 lane = idx & 63, dw = (idx >> 6) % DW, ks = (idx >> 6) / DW % KS, ot = (idx >> 6) / DW / KS;
     const u32 o = 32 * ot + (lane & 31), c0 = 32 * ks + 16 * (lane >> 5);
     u32 words[4];
@@ -74,11 +76,13 @@ struct LinearMfmaArgs {
     const u64* in;
     size_t in_ct, in_comp, in_row;
     const uint4* wa;
+    size_t wa_group, bias_group;
     const u64* bias;
     u64* acc;
     size_t acc_ct, acc_comp, acc_row;
     const ModConstF* mcf;
     u32 N, limb0, limbs, bias_limbs, c_in, c_out, KS, OT, ot_per_wg, add;
+    LinearGroups groups;
 };
 // per limb: K 2^(32 g) mod q, centred, g < 3, and the column sum's constant
 struct LinearConsts {
@@ -94,7 +98,8 @@ __global__ __launch_bounds__(LM_THREADS, 2) void linear_mfma_kernel(LinearMfmaAr
     u64* colsum = reinterpret_cast<u64*>(lds + CT * KS * LM_DX * 64);
     const u32 er = blockIdx.y % A.limbs, e = A.limb0 + er, comp = blockIdx.y / A.limbs;
     const u32 n_split = (A.OT + A.ot_per_wg - 1) / A.ot_per_wg, row = blockIdx.z / n_split, ot_first = blockIdx.z % n_split * A.ot_per_wg;
-    const u32 x0 = blockIdx.x * COLS;
+    const u32 x0 = blockIdx.x * COLS, gi = A.groups.of_row(row);
+    const u64* bias = A.bias ? A.bias + A.groups.id[gi] * A.bias_group : nullptr;
     const u64* src = A.in + row * A.in_row + comp * A.in_comp + (size_t)e * N + x0;
     u64* acc = A.acc + row * A.acc_row + comp * A.acc_comp + (size_t)er * N;
     if (DW > 1 && tid < COLS) colsum[tid] = 0;
@@ -170,7 +175,7 @@ __global__ __launch_bounds__(LM_THREADS, 2) void linear_mfma_kernel(LinearMfmaAr
             for (u32 r = 0; r < 16; r++) d[s][r] = 0;
         // A step's weights are requested a step ahead, in two register sets in turn; no memory operation moves across LM_KEEP_ORDER (left to itself the
         // compiler requests them where they are used, a round trip to the L2 cache per step)
-        const uint4* wa = A.wa + (size_t)ot * KS * DW * 64 + lane;
+        const uint4* wa = A.wa + gi * A.wa_group + (size_t)ot * KS * DW * 64 + lane;
         uint4 a0[DW], a1[DW];
         auto weights = [&](u32 ks, uint4* a) {
             const uint4* p = wa + min(ks, KS - 1) * (DW * 64);
@@ -230,14 +235,14 @@ __global__ __launch_bounds__(LM_THREADS, 2) void linear_mfma_kernel(LinearMfmaAr
                     }
                     double v = DW > 1 ? f64m_dot_w<GROUPS + 1>(part, cw, m.q, m.qinv) : f64m_dot_w<GROUPS>(part, cw, m.q, m.qinv);
                     if (!WHOLE && o >= A.c_out) continue;
-                    if (!WHOLE && A.bias && comp == 0)
-                        v = f64m_reduce(v + f64m_mulmod_any(f64m_from_u64(A.bias[(size_t)o * A.bias_limbs + e]), K.bias[e], m.q, m.qinv), m.q, m.qinv);
+                    if (!WHOLE && bias && comp == 0)
+                        v = f64m_reduce(v + f64m_mulmod_any(f64m_from_u64(bias[(size_t)o * A.bias_limbs + e]), K.bias[e], m.q, m.qinv), m.q, m.qinv);
                     if (ADD) v = f64m_reduce(v + f64m_from_u64(old[q & 1][r & 3]), m.q, m.qinv);
                     acc[o * A.acc_ct + x] = f64m_canonical(v, m.q);
                 }
             }
         };
-        if (DW == 4 && 32 * ot + 32 <= A.c_out && !(A.bias && comp == 0)) finish(std::integral_constant<bool, true>());
+        if (DW == 4 && 32 * ot + 32 <= A.c_out && !(bias && comp == 0)) finish(std::integral_constant<bool, true>());
         else finish(std::integral_constant<bool, false>());
     }
 }
@@ -251,9 +256,9 @@ size_t linear_mfma_scratch_elems(u32 c_in, u32 c_out, u32 weight_bytes) {
 }
 
 template <u32 DW>
-static hipError_t launch_linear_dw(const LinearMfmaArgs& A, const LinearConsts& K, u32 rows, u32 n_split, hipStream_t st) {
+static hipError_t launch_linear_dw(const LinearMfmaArgs& A, const LinearConsts& K, u32 rows, hipStream_t st) {
     const u32 CT = A.KS <= 4 ? 2 : 1;
-    const dim3 grid(A.N / (32 * CT), 2 * A.limbs, rows * n_split);
+    const dim3 grid(A.N / (32 * CT), 2 * A.limbs, rows);
     const size_t lds = (size_t)CT * A.KS * LM_DX * 64 * 16 + 64 * 8;
 #define LINEAR_MFMA(CT, ADD) hipLaunchKernelGGL((linear_mfma_kernel<DW, CT, ADD>), grid, dim3(LM_THREADS), lds, st, A, K)
     if (CT == 2 && A.add) LINEAR_MFMA(2, true);
@@ -265,6 +270,7 @@ static hipError_t launch_linear_dw(const LinearMfmaArgs& A, const LinearConsts& 
 }
 
 hipError_t launch_linear_mfma(const ckks_ctx* c, const LinearSum& S, u64* scratch, bool prepared, hipStream_t st) {
+    if (S.groups.n == 0 || S.groups.n > LINEAR_GROUPS || (u64)S.rows * S.c_out > 1024) return hipErrorInvalidValue;  // (the grid's third dimension)
     const u32 wb = S.weight_bytes;
     LinearConsts K;
     for (u32 i = 0; i < CKKS_MAX_MODULI; i++) {
@@ -287,10 +293,10 @@ hipError_t launch_linear_mfma(const ckks_ctx* c, const LinearSum& S, u64* scratc
         const u32 nc = S.c_in - c0 < LM_CHUNK ? S.c_in - c0 : LM_CHUNK;
         const char* wc = (const char*)S.w + c0 * S.w_in * wb;
         const u32 KS = (nc + 31) / 32, OT = (S.c_out + 31) / 32, prep = OT * KS * wb * 64;
-        uint4* wa = (uint4*)(scratch + linear_mfma_scratch_elems(c0, S.c_out, wb));
+        uint4* wa = (uint4*)(scratch + S.groups.n * linear_mfma_scratch_elems(c0, S.c_out, wb));
         if (!prepared) {
-            const dim3 pg((prep + LM_THREADS - 1) / LM_THREADS);
-#define LINEAR_PREP(W) hipLaunchKernelGGL(linear_prep_kernel<W>, pg, dim3(LM_THREADS), 0, st, (const W*)wc, S.w_out, S.w_in, wa, S.c_out, nc, KS, OT)
+            const dim3 pg((prep + LM_THREADS - 1) / LM_THREADS, S.groups.n);
+#define LINEAR_PREP(W) hipLaunchKernelGGL(linear_prep_kernel<W>, pg, dim3(LM_THREADS), 0, st, (const W*)wc, S.w_out, S.w_in, S.w_group, S.groups, wa, prep, S.c_out, nc, KS, OT)
             if (wb == 1) LINEAR_PREP(int8_t);
             else if (wb == 2) LINEAR_PREP(int16_t);
             else LINEAR_PREP(int32_t);
@@ -303,15 +309,13 @@ hipError_t launch_linear_mfma(const ckks_ctx* c, const LinearSum& S, u64* scratc
         u32 per = (OT + n_split - 1) / n_split;
         per = (per + step - 1) / step * step;
         n_split = (OT + per - 1) / per;
-        for (u32 r0 = 0; r0 < S.rows;) {  // the launch's third dimension holds 65535 workgroups
-            const u32 most = 65535 / n_split, n = S.rows - r0 < most ? S.rows - r0 : most, add = c0 || S.add ? 1 : 0;
-            const LinearMfmaArgs A = {S.in + r0 * S.in_row + c0 * S.in_ct, S.in_ct, S.in_comp, S.in_row, wa, c0 ? nullptr : S.bias, S.acc + r0 * S.acc_row, S.acc_ct,
-                                      S.acc_comp, S.acc_row, c->d_mcf, c->N, S.limb0, S.limbs, S.bias_limbs, nc, S.c_out, KS, OT, per, add};
-            ProfScope ps__(c, K_WEIGHTED_SUM, st, 16.0 * n * c->N * S.limbs * (nc + (1.0 + add) * S.c_out), 2.0 * n * c->N * S.limbs * nc * S.c_out);
-            hipError_t err = wb == 1 ? launch_linear_dw<1>(A, K, n, n_split, st) : (wb == 2 ? launch_linear_dw<2>(A, K, n, n_split, st) : launch_linear_dw<4>(A, K, n, n_split, st));
-            if (err != hipSuccess) return err;
-            r0 += n;
-        }
+        const u32 add = c0 || S.add ? 1 : 0;
+        const LinearMfmaArgs A = {S.in + c0 * S.in_ct, S.in_ct, S.in_comp, S.in_row, wa, prep, S.bias_group, c0 ? nullptr : S.bias, S.acc, S.acc_ct, S.acc_comp, S.acc_row,
+                                  c->d_mcf, c->N, S.limb0, S.limbs, S.bias_limbs, nc, S.c_out, KS, OT, per, add, S.groups};
+        ProfScope ps__(c, K_WEIGHTED_SUM, st, 16.0 * S.rows * c->N * S.limbs * (nc + (1.0 + add) * S.c_out), 2.0 * S.rows * c->N * S.limbs * nc * S.c_out);
+        const u32 rows = S.rows * n_split;
+        hipError_t err = wb == 1 ? launch_linear_dw<1>(A, K, rows, st) : (wb == 2 ? launch_linear_dw<2>(A, K, rows, st) : launch_linear_dw<4>(A, K, rows, st));
+        if (err != hipSuccess) return err;
     }
     return hipSuccess;
 }

@@ -112,6 +112,20 @@ def test_grouped_product_in_chunks_of_rows_and_outputs():
     assert tuple(many.shape) == (1, 70, 2, level, 1 << 17) and tuple(one.shape) == (1, 1, 2, level, 1 << 17)
 
 
+def test_grouped_product_of_many_small_groups():
+    """150 groups, every third without rows: more than one launch takes, each with its own weights and biases."""
+    p, orc, ctx = world(12, 3, 1, 1)
+    rng = np.random.default_rng(9)
+    rows = [(0, 1, 2)[g % 3] for g in range(150)]
+    for c_in in (3, 11):
+        x = ciphertexts(rng, p, 1, sum(rows) * c_in)
+        w = rng.integers(-128, 128, size=(150, 2, c_in)).astype(np.int8)
+        b = np.stack([rng.integers(0, q, size=(150, 2), dtype=np.uint64) for q in p.moduli[:2]], -1)
+        got = hx.he_linear_grouped(ctx, 1, rows, hx.from_host(x).unflatten(0, (sum(rows), c_in)), torch.from_numpy(w).cuda(), 1 << 42, hx.from_host(b))
+        want = orc.linear_grouped(x.reshape(sum(rows), c_in, 2, 2, orc.N), 1, rows, w, 1 << 42, b)
+        assert np.array_equal(hx.to_host(got), np.array(want))
+
+
 def test_grouped_product_of_nothing():
     p, orc, ctx = world(12, 4, 2, 2)
     out = hx.he_linear_grouped(ctx, 3, (0, 0), hx.empty(0, 5, 2, 4, orc.N), torch.zeros(2, 3, 5, dtype=torch.int8, device="cuda"), 1)
