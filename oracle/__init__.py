@@ -2,8 +2,8 @@
 
 Python face of the plain CPU RNS-CKKS in ``ckks_oracle.cpp`` plus the floating-point client
 side (slot encoding / decoding with numpy's FFT as a library step, float64 reference
-convolution, the odd degree-7 activation polynomial).  Only ``tests/``, the smoke check and the
-benchmark's ``cpu_baseline`` leg may import this package; the HIP library never does.
+convolution, the odd degree-7 activation polynomial).  Only ``tests/``, the smoke check, the
+benchmark's ``cpu_baseline`` leg and ``examples/`` (for the client's side) may import this package; the HIP library never does.
 
 Paper passages followed: Background ("The CKKS Scheme": slots through the canonical embedding;
 "Rotations and Key Switching"), Methodology ("Encrypted Input Representation", Eqs. 2-5: channel-

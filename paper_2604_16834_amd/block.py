@@ -19,9 +19,9 @@ class QuantisedWeights(NamedTuple):
         return scale * self.multiplier / self.step
 
 
-def quantise_weights(weights, q_level: int, bits: int = 32) -> QuantisedWeights:
-    """Weights rounded to integers of 8, 16 or 32 bits; with the multiplier round(step * q_level) the product's outputs have the scale of its
-    inputs times q_level * step / multiplier, which ``linear_scale`` gives exactly."""
+def quantise_weights(weights, q_level: int, bits: int = 32, gain: float = 1.0) -> QuantisedWeights:
+    """Weights rounded to integers of 8, 16 or 32 bits, and the multiplier round(step * q_level * gain): the product's outputs have `gain` times the scale of its
+    inputs but for the rounding, exactly what ``linear_scale`` gives."""
     w = np.asarray(weights, dtype=np.float64)
     if bits not in (8, 16, 32):
         raise ValueError("bits must be 8, 16 or 32")
@@ -31,7 +31,10 @@ def quantise_weights(weights, q_level: int, bits: int = 32) -> QuantisedWeights:
     # below 2^-(bits - 1) of q the multiplier would lose the step's accuracy: steps are kept above 2^-40
     step = max(top / (2 ** (bits - 1) - 1), 2.0 ** -40)
     dtype = {8: np.int8, 16: np.int16, 32: np.int32}[bits]
-    return QuantisedWeights(np.round(w / step).astype(dtype), max(1, round(step * q_level)), step)
+    multiplier = max(1, round(step * q_level * gain))
+    if multiplier >= 1 << 64:
+        raise ValueError("the multiplier passes 64 bits")
+    return QuantisedWeights(np.round(w / step).astype(dtype), multiplier, step)
 
 
 def linear_scale(scale: float, weights: QuantisedWeights, q_level: int) -> float:

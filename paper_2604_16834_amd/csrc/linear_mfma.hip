@@ -11,7 +11,7 @@
 // 2^49; the two or three groups and the column's sum are then one chain of fused multiply-adds with the constants K 2^(32 g) mod q, centred
 // (f64m_dot_w): 45 double-precision operations an output, the multiplier included.
 //
-// A workgroup owns 64 (CT = 2) or 32 columns of one row, component and limb: it reads them once, for all channels, turns them into digits in LDS, and its
+// A workgroup owns 128, 64 or 32 columns (CT = 4, 2, 1) of one row, component and limb: it reads them once, for all channels, turns them into digits in LDS, and its
 // four waves take the 32-output tiles in turn, so X streams from HBM exactly once for any number of outputs.  Bound by HBM up to 64 x 64 channels (a column
 // is 8 (c_in + 2 c_out) bytes with what is added to, against c_in c_out 7 DW digit products): 64 -> 64, 8-bit weights, two rows of 23 limbs at N = 2^16 2.4 ms,
 // 3.7 TB/s.  With 256 -> 192 channels and 32-bit weights (two rows of 12 limbs, 6.5 ms) the matrix pipe is busy 30 % and the vector units 34 % of the time, the two
@@ -255,13 +255,19 @@ size_t linear_mfma_scratch_elems(u32 c_in, u32 c_out, u32 weight_bytes) {
     return (size_t)((c_out + 31) / 32) * ((c_in + 31) / 32) * weight_bytes * 64 * 2;
 }
 
+// 32-column tiles of a workgroup: the four waves take column tiles x output tiles, and 256 channels' digits of one column tile are 56 KB of LDS.  Four where a
+// single output tile would leave two waves idle (37 -> 29 channels, six rows of 5 limbs at N = 2^13: two 228 us, four 193).
+static u32 linear_col_tiles(u32 N, u32 KS, u32 OT) { return OT == 1 && KS <= 2 && N >= 128 ? 4 : (KS <= 4 ? 2 : 1); }
+
 template <u32 DW>
 static hipError_t launch_linear_dw(const LinearMfmaArgs& A, const LinearConsts& K, u32 rows, hipStream_t st) {
-    const u32 CT = A.KS <= 4 ? 2 : 1;
+    const u32 CT = linear_col_tiles(A.N, A.KS, A.OT);
     const dim3 grid(A.N / (32 * CT), 2 * A.limbs, rows);
-    const size_t lds = (size_t)CT * A.KS * LM_DX * 64 * 16 + 64 * 8;
+    const size_t lds = (size_t)CT * A.KS * LM_DX * 64 * 16 + 32 * CT * 8;  // at most 57 KB and the sums: two workgroups per CU
 #define LINEAR_MFMA(CT, ADD) hipLaunchKernelGGL((linear_mfma_kernel<DW, CT, ADD>), grid, dim3(LM_THREADS), lds, st, A, K)
-    if (CT == 2 && A.add) LINEAR_MFMA(2, true);
+    if (CT == 4 && A.add) LINEAR_MFMA(4, true);
+    else if (CT == 4) LINEAR_MFMA(4, false);
+    else if (CT == 2 && A.add) LINEAR_MFMA(2, true);
     else if (CT == 2) LINEAR_MFMA(2, false);
     else if (A.add) LINEAR_MFMA(1, true);
     else LINEAR_MFMA(1, false);
@@ -303,7 +309,7 @@ hipError_t launch_linear_mfma(const ckks_ctx* c, const LinearSum& S, u64* scratc
 #undef LINEAR_PREP
         }
         // outputs of a workgroup: all, unless that leaves the chip short of workgroups
-        const u32 ct = KS <= 4 ? 2 : 1, step = 4 / ct;
+        const u32 ct = linear_col_tiles(c->N, KS, OT), step = 4 / ct;
         const u64 wgs = (u64)(c->N / (32 * ct)) * 2 * S.limbs * S.rows;
         u32 n_split = wgs >= 1024 ? 1 : (u32)(1024 / wgs);
         u32 per = (OT + n_split - 1) / n_split;

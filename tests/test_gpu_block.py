@@ -374,6 +374,18 @@ def test_block_on_another_stream_and_from_a_graph(ring):
         assert torch.equal(block_calls(ctx, level, xs[i], w, tab, rlk, k, torch.empty_like(ws)), eager[i])  # eager work between replays
 
 
+def test_the_block_of_the_example():
+    """examples/encrypted_block.py: the three operators together, decrypted, against float64 within what the Newton iterations leave."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "encrypted_block.py")
+    spec = importlib.util.spec_from_file_location("encrypted_block", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    diff, bound = example.run(12, verbose=False)
+    assert diff <= bound
+
+
 def raises(code, text, call):
     with pytest.raises(hx.CkksError) as e:
         call()
