@@ -678,7 +678,7 @@ def he_linear_grouped(ctx: Context, level: int, group_rows: Sequence[int], x: to
         raise ValueError("bias must be [groups][c_out][level+1]")
     out = _out(ctx, out, total, c_out, 2, level, ctx.N)
     arr = _ct_array(ctx, x, total * c_in, level + 1, "x")
-    ws = _ws(ctx, ws, he_linear_workspace_bytes(ctx, level, group_rows, c_in, c_out, w.dtype))
+    ws = ctx.workspace(int(_lib.he_linear_workspace_bytes(ctx.handle, C.byref(d), rows))) if ws is None else ws
     ctx._check(_lib.he_linear_grouped(ctx.handle, C.byref(d), rows, C.byref(arr), w.data_ptr(), _ptr(bias), _ptr(out), _ptr(ws),
                                       ws.numel() * ws.element_size(), _stream(stream)))
     return out
@@ -699,7 +699,7 @@ def he_rope_axes(ctx: Context, level: int, x: torch.Tensor, cos: torch.Tensor, s
     d = _RopeDesc(heads, head_dim, n_pairs, level, int(bool(interleaved)), int(bool(inverse)))
     out = _out(ctx, out, heads, head_dim, 2, level, ctx.N)
     arr = _ct_array(ctx, x, heads * head_dim, level + 1, "x")
-    ws = _ws(ctx, ws, he_rope_workspace_bytes(ctx, level, heads, head_dim, n_pairs))
+    ws = ctx.workspace(int(_lib.he_rope_workspace_bytes(ctx.handle, C.byref(d)))) if ws is None else ws
     ctx._check(_lib.he_rope_axes(ctx.handle, C.byref(d), C.byref(arr), _ptr(cos), _ptr(sin), _ptr(out), _ptr(ws), ws.numel() * ws.element_size(),
                                  _stream(stream)))
     return out
@@ -729,7 +729,7 @@ def he_norm_gate(ctx: Context, level: int, x: torch.Tensor, k_eps: int, k_slope:
     xa = _ct_array(ctx, x, channels, limbs, "x")
     ga = _ct_array(ctx, gate, channels, limbs, "gate", plain=kind == HE_GATE_PLAIN) if kind else None
     ra = _ct_array(ctx, residual, channels, max(last, 0) + 1, "residual") if residual is not None else None
-    ws = _ws(ctx, ws, he_norm_workspace_bytes(ctx, level, channels, its, kind))
+    ws = ctx.workspace(int(_lib.he_norm_workspace_bytes(ctx.handle, C.byref(d)))) if ws is None else ws
     ctx._check(_lib.he_norm_gate(ctx.handle, C.byref(d), kn, C.byref(xa), C.byref(ga) if ga else None, C.byref(ra) if ra else None,
                                  rlk.handle if rlk else None, _ptr(out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
     return out

@@ -278,9 +278,9 @@ static hipError_t launch_linear_dw(const LinearMfmaArgs& A, const LinearConsts& 
 hipError_t launch_linear_mfma(const ckks_ctx* c, const LinearSum& S, u64* scratch, bool prepared, hipStream_t st) {
     if (S.groups.n == 0 || S.groups.n > LINEAR_GROUPS || (u64)S.rows * S.c_out > 1024) return hipErrorInvalidValue;  // (the grid's third dimension)
     const u32 wb = S.weight_bytes;
-    LinearConsts K;
-    for (u32 i = 0; i < CKKS_MAX_MODULI; i++) {
-        const u64 q = i < c->num_q ? c->mod[i] : 3;
+    LinearConsts K = {};
+    for (u32 i = S.limb0; i < S.limb0 + S.limbs; i++) {
+        const u64 q = c->mod[i];
         auto centred = [&](unsigned __int128 v) {
             const u64 r = (u64)(v % q);
             return r > q / 2 ? -(double)(q - r) : (double)r;
