@@ -2076,7 +2076,7 @@ struct LinearPlan {
 // Weights' digits in the workspace: of as many groups as these bytes hold
 #define LINEAR_DIGIT_BYTES ((size_t)256 << 20)
 static size_t linear_digits(const ckks_ctx* c, const he_linear_desc* d, u32 outs) {
-    return linear_mfma_applies(c, d->c_in) ? linear_mfma_scratch_elems(d->c_in, outs, d->weight_type) : 0;
+    return linear_mfma_applies(c, d->c_in, outs) ? linear_mfma_scratch_elems(d->c_in, outs, d->weight_type) : 0;
 }
 static int linear_plan(const ckks_ctx* c, const he_linear_desc* d, const u32* h_rows, LinearPlan* p) {
     if (!d || !h_rows) return set_err(c, CKKS_ERR_INVALID_ARG, "null descriptor or row counts");

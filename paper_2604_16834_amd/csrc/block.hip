@@ -57,7 +57,7 @@ __global__ __launch_bounds__(BK_THREADS) void linear_sum_kernel(LinearArgs A, co
     }
 }
 
-// Moduli below 2^50 and few channels, in double precision (f64m_dot_w: chains of eight exact products of centred residues and weights): a thread reads a
+// Moduli below 2^50, few channels or outputs, in double precision (f64m_dot_w: chains of eight exact products of centred residues and weights): a thread reads a
 // column's channels eight at a time and adds a chain to each of OT outputs, whose weights are in LDS.
 template <class W, u32 OT>
 __global__ __launch_bounds__(BK_THREADS) void linear_sum_f64_kernel(LinearArgs A, const ModConstF* __restrict__ mcf) {
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(BK_THREADS) void linear_sum_f64_kernel(LinearArgs A
 }
 
 hipError_t launch_linear_sum(const ckks_ctx* c, const LinearSum& S, u64* scratch, bool prepared, hipStream_t st) {
-    if (linear_mfma_applies(c, S.c_in)) return launch_linear_mfma(c, S, scratch, prepared, st);
+    if (linear_mfma_applies(c, S.c_in, S.c_out)) return launch_linear_mfma(c, S, scratch, prepared, st);
     const u32 tile = c->small_q ? (S.c_out <= 2 ? S.c_out : 8) : LG_OUT_TILE, o_tiles = (S.c_out + tile - 1) / tile;
     if (S.groups.n == 0 || S.groups.n > LINEAR_GROUPS || (u64)S.rows * S.c_out > 1024) return hipErrorInvalidValue;  // (the grid's third dimension)
     const dim3 grid((c->N + BK_THREADS - 1) / BK_THREADS, 2 * S.limbs, S.rows * o_tiles);

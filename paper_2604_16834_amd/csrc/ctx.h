@@ -433,7 +433,7 @@ struct LinearSum {
 // scratch: groups.n times linear_mfma_scratch_elems words where linear_mfma_applies; prepared: they hold these groups' weights from the call before
 hipError_t launch_linear_sum(const ckks_ctx* c, const LinearSum& S, u64* scratch, bool prepared, hipStream_t st);
 // linear_mfma.hip
-bool linear_mfma_applies(const ckks_ctx* c, u32 c_in);
+bool linear_mfma_applies(const ckks_ctx* c, u32 c_in, u32 c_out);  // (as c_in or c_out grows, once true it stays so)
 size_t linear_mfma_scratch_elems(u32 c_in, u32 c_out, u32 weight_bytes);
 hipError_t launch_linear_mfma(const ckks_ctx* c, const LinearSum& S, u64* scratch, bool prepared, hipStream_t st);
 // block.hip

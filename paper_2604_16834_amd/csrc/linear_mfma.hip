@@ -11,28 +11,25 @@
 // 2^49; the two or three groups and the column's sum are then one chain of fused multiply-adds with the constants K 2^(32 g) mod q, centred
 // (f64m_dot_w): 45 double-precision operations an output, the multiplier included.
 //
-// A workgroup owns 128, 64 or 32 columns (CT = 4, 2, 1) of one row, component and limb: it reads them once, for all channels, turns them into digits in LDS, and its
-// four waves take the 32-output tiles in turn, so X streams from HBM exactly once for any number of outputs.  Bound by HBM up to 64 x 64 channels (a column
-// is 8 (c_in + 2 c_out) bytes with what is added to, against c_in c_out 7 DW digit products): 64 -> 64, 8-bit weights, two rows of 23 limbs at N = 2^16 2.4 ms,
-// 3.7 TB/s.  With 256 -> 192 channels and 32-bit weights (two rows of 12 limbs, 6.5 ms) the matrix pipe is busy 30 % and the vector units 34 % of the time, the two
-// workgroups of a CU load, multiply and fold in step.  Tried and slower there: one persistent workgroup of eight waves per CU, two of which read and convert the next
-// tile while six multiply (6.9 to 9 ms; 8-bit 64 -> 64 6.1 instead of 3.6 ms: too few loads in flight); four diagonals at a time with 64 accumulator registers and
-// three waves per SIMD (7.2 ms: spills).  More than 256 channels: launches that add to what the one before them left.
-#include <type_traits>
-
+// A workgroup owns 64 columns (up to 64 channels) or 32 of one row, component and limb: it reads them once, for all channels, turns them into digits in LDS, and its
+// waves take units of 16 outputs x 16 columns in turn, so X streams from HBM exactly once for any number of outputs.  Such a unit's diagonals are 28 to 40 registers, and
+// four waves per SIMD hide each other's loads, products and folds.  Bound by HBM (a column is 8 (c_in + 2 c_out) bytes with what is added to, against c_in c_out 7 DW
+// digit products): 64 -> 64 channels, 8-bit weights, three rows of 23 limbs at N = 2^16 3.03 ms, 4.6 TB/s; 256 -> 192, 32-bit weights, two rows of 12 limbs 5.7 ms, 2.8 TB/s.
+// Tried and slower: units of 32 x 32 (160 registers of diagonals, two waves per SIMD: 3.25 and 6.5 ms, the matrix pipe 30 % and the vector units 34 % busy, the two
+// workgroups of a CU load, multiply and fold in step); one persistent workgroup of eight waves per CU, two of which read and convert the next tile while six multiply
+// (6.9 to 9 ms in the second case: too few loads in flight); the next step's weights requested a step ahead (2 % slower: registers); what is added to requested behind
+// the products (1 %).  More than 256 channels: launches that add to what the one before them left.
 #include "ctx.h"
 
 typedef int v4i __attribute__((ext_vector_type(4)));
-typedef int v16i __attribute__((ext_vector_type(16)));
 
-#define LM_THREADS 256
+#define LM_THREADS 256  // linear_prep_kernel
 #define LM_DX 7                      // digits of a residue
 #define LM_BIAS 0x0080808080808080ull
 #define LM_CHUNK 256                 // channels of a launch
-#define LM_KEEP_ORDER asm volatile("" ::: "memory"); __builtin_amdgcn_sched_barrier(0);
 
 // ---- weights -> digit planes in A-operand layout, group by group (blockIdx.y): wa[((ot*KS + ks)*DW + dw)*64 + lane] = 16 bytes, digit dw of
-//   W[32*ot + lane%32][32*ks + 16*(lane/32) + j], j < 16  (zero beyond c_out and c_in)
+//   W[16*ot + lane%16][64*ks + 16*(lane/16) + j], j < 16  (zero beyond c_out and c_in)
 template <class W>
 __global__ __launch_bounds__(LM_THREADS) void linear_prep_kernel(const W* __restrict__ w, size_t w_out, size_t w_in, size_t w_group, LinearGroups groups,
                                                                  uint4* __restrict__ wa, size_t wa_group, u32 c_out, u32 c_in, u32 KS, u32 OT) {
@@ -42,7 +39,7 @@ __global__ __launch_bounds__(LM_THREADS) void linear_prep_kernel(const W* __rest
     w += groups.id[blockIdx.y] * w_group;
     wa += blockIdx.y * wa_group;
     const u32 lane = idx & 63, dw = (idx >> 6) % DW, ks = (idx >> 6) / DW % KS, ot = (idx >> 6) / DW / KS;
-    const u32 o = 32 * ot + (lane & 31), c0 = 32 * ks + 16 * (lane >> 5);
+    const u32 o = 16 * ot + (lane & 15), c0 = 64 * ks + 16 * (lane >> 4);
     u32 words[4];
 #pragma unroll
     for (u32 m = 0; m < 4; m++) {
@@ -89,76 +86,67 @@ struct LinearConsts {
     double c[4][CKKS_MAX_MODULI], bias[CKKS_MAX_MODULI];
 };
 
-template <u32 DW, u32 CT, bool ADD>
-__global__ __launch_bounds__(LM_THREADS, 2) void linear_mfma_kernel(LinearMfmaArgs A, LinearConsts K) {
-    constexpr u32 DIAGS = LM_DX + DW - 1, GROUPS = (DIAGS + 3) / 4, COLS = 32 * CT, KG = LM_THREADS / COLS;  // KG groups of 16 channels at a time
+template <u32 DW, u32 CT, u32 THREADS, bool ADD>
+__global__ __launch_bounds__(THREADS, 4) void linear_mfma_kernel(LinearMfmaArgs A, LinearConsts K) {
+    constexpr u32 DIAGS = LM_DX + DW - 1, GROUPS = (DIAGS + 3) / 4, COLS = 16 * CT, OT_STEP = THREADS / 64 / CT;
     extern __shared__ uint4 lds[];  // [CT][KS][7][64], then the column sums
     const u32 tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const u32 KS = A.KS, N = A.N;
+    // (a number of steps known here: 64 -> 64 with 32-bit weights 6.54 -> 6.36 ms, 128 -> 96 with 16-bit ones 3.76 -> 3.56; with 8-bit ones the registers that the
+    // compiler then takes for loads ahead cost a wave per SIMD, 6.15 instead of 5.9 ms)
+    const u32 KS = DW == 1 ? A.KS : (CT == 4 ? 1 : (THREADS == 256 ? 2 : A.KS)), N = A.N;
     u64* colsum = reinterpret_cast<u64*>(lds + CT * KS * LM_DX * 64);
     const u32 er = blockIdx.y % A.limbs, e = A.limb0 + er, comp = blockIdx.y / A.limbs;
     const u32 n_split = (A.OT + A.ot_per_wg - 1) / A.ot_per_wg, row = blockIdx.z / n_split, ot_first = blockIdx.z % n_split * A.ot_per_wg;
     const u32 x0 = blockIdx.x * COLS, gi = A.groups.of_row(row);
     const u64* bias = A.bias ? A.bias + A.groups.id[gi] * A.bias_group : nullptr;
-    const u64* src = A.in + row * A.in_row + comp * A.in_comp + (size_t)e * N + x0;
     u64* acc = A.acc + row * A.acc_row + comp * A.acc_comp + (size_t)er * N;
     if (DW > 1 && tid < COLS) colsum[tid] = 0;
     if (DW > 1) __syncthreads();
 
-    // the digits of all channels of the columns: thread (col, kg) takes groups of 16 channels of a column, two at a time (their 32 loads together)
-    {
-        const u32 col = tid & (COLS - 1), kg = tid / COLS;
-        u64 total = 0;
-        auto request = [&](u32 g, u64* v) {
+    // the digits of all channels of the columns: a thread takes 16 channels of a column (4 KS groups of 16; CT KS is THREADS / 64 at most)
+    const u32 col = tid & (COLS - 1), g = tid / COLS;
+    if (g < 4 * KS) {
+        const u64* src = A.in + row * A.in_row + comp * A.in_comp + (size_t)e * N + x0 + col;
+        u64 v[16];
+        if (16 * g < A.c_in) {
 #pragma unroll
-            for (u32 j = 0; j < 16; j++) v[j] = src[(16 * g + j < A.c_in ? 16 * g + j : A.c_in - 1) * A.in_ct + col];
-        };
-        auto convert = [&](u32 g, u64* v) {
+            for (u32 j = 0; j < 16; j++) v[j] = src[(16 * g + j < A.c_in ? 16 * g + j : A.c_in - 1) * A.in_ct];
+        } else {
 #pragma unroll
-            for (u32 j = 0; j < 16; j++)
-                if (16 * g + j >= A.c_in) v[j] = 0;
-            u32 w[8][4];
-#pragma unroll
-            for (u32 m = 0; m < 4; m++) {
-                u64 s[4];
-#pragma unroll
-                for (u32 j = 0; j < 4; j++) {
-                    if (DW > 1) total += v[4 * m + j];
-                    s[j] = (v[4 * m + j] + LM_BIAS) ^ LM_BIAS;
-                }
-                u32 lo[4], hi[4];
-                lm_transpose((u32)s[0], (u32)s[1], (u32)s[2], (u32)s[3], lo);
-                lm_transpose((u32)(s[0] >> 32), (u32)(s[1] >> 32), (u32)(s[2] >> 32), (u32)(s[3] >> 32), hi);
-#pragma unroll
-                for (u32 i = 0; i < 4; i++) w[i][m] = lo[i], w[4 + i][m] = hi[i];
-            }
-            uint4* dst = lds + (((col >> 5) * KS + (g >> 1)) * LM_DX) * 64 + 32 * (g & 1) + (col & 31);
-#pragma unroll
-            for (u32 dx = 0; dx < LM_DX; dx++) dst[dx * 64] = make_uint4(w[dx][0], w[dx][1], w[dx][2], w[dx][3]);
-        };
-        for (u32 g = kg; g < 2 * KS; g += 2 * KG) {
-            u64 v0[16], v1[16];
-            request(g, v0);
-            if (g + KG < 2 * KS) {
-                request(g + KG, v1);
-                convert(g, v0);
-                convert(g + KG, v1);
-            } else {
-                convert(g, v0);
-            }
+            for (u32 j = 0; j < 16; j++) v[j] = 0;
         }
+        u64 total = 0;
+        u32 w[8][4];
+#pragma unroll
+        for (u32 m = 0; m < 4; m++) {
+            u64 s[4];
+#pragma unroll
+            for (u32 j = 0; j < 4; j++) {
+                if (16 * g + 4 * m + j >= A.c_in) v[4 * m + j] = 0;
+                if (DW > 1) total += v[4 * m + j];
+                s[j] = (v[4 * m + j] + LM_BIAS) ^ LM_BIAS;
+            }
+            u32 lo[4], hi[4];
+            lm_transpose((u32)s[0], (u32)s[1], (u32)s[2], (u32)s[3], lo);
+            lm_transpose((u32)(s[0] >> 32), (u32)(s[1] >> 32), (u32)(s[2] >> 32), (u32)(s[3] >> 32), hi);
+#pragma unroll
+            for (u32 i = 0; i < 4; i++) w[i][m] = lo[i], w[4 + i][m] = hi[i];
+        }
+        uint4* dst = lds + (((col >> 4) * KS + (g >> 2)) * LM_DX) * 64 + 16 * (g & 3) + (col & 15);
+#pragma unroll
+        for (u32 dx = 0; dx < LM_DX; dx++) dst[dx * 64] = make_uint4(w[dx][0], w[dx][1], w[dx][2], w[dx][3]);
         if (DW > 1) atomicAdd(&colsum[col], total);  // whole numbers below 2^58: any order
     }
     __syncthreads();
 
-    const u32 ct = wave % CT, x = x0 + 32 * ct + (lane & 31), half = lane >> 5;
+    const u32 ct = wave % CT, x = x0 + 16 * ct + (lane & 15), quarter = lane >> 4;
     const ModConstF m = A.mcf[e];
     double cw[GROUPS + 1], part[GROUPS + 1];
 #pragma unroll
-    for (u32 g = 0; g < GROUPS; g++) cw[g] = K.c[g][e];
+    for (u32 i = 0; i < GROUPS; i++) cw[i] = K.c[i][e];
     cw[GROUPS] = K.c[3][e];
     if (DW > 1) {  // below 2^58: two halves joined modulo q
-        const u64 s = colsum[32 * ct + (lane & 31)];
+        const u64 s = colsum[16 * ct + (lane & 15)];
         const double hi = f64m_reduce((double)(u32)(s >> 32), m.q, m.qinv), lo = (double)(u32)s;
         const double two32 = f64m_reduce(4294967296.0, m.q, m.qinv);
         part[GROUPS] = f64m_reduce(f64m_mulmod_any(hi, two32, m.q, m.qinv) + lo, m.q, m.qinv);
@@ -167,110 +155,82 @@ __global__ __launch_bounds__(LM_THREADS, 2) void linear_mfma_kernel(LinearMfmaAr
     }
     const uint4* lb = lds + (ct * KS) * LM_DX * 64 + lane;
     const u32 ot_last = min(ot_first + A.ot_per_wg, A.OT);
-    for (u32 ot = ot_first + wave / CT; ot < ot_last; ot += 4 / CT) {
-        v16i d[DIAGS];
+    for (u32 ot = ot_first + wave / CT; ot < ot_last; ot += OT_STEP) {
+        u64 old[4];
+        if (ADD) {  // requested ahead of the products
 #pragma unroll
-        for (u32 s = 0; s < DIAGS; s++)
+            for (u32 r = 0; r < 4; r++) {
+                const u32 o = 16 * ot + 4 * quarter + r;
+                old[r] = acc[(o < A.c_out ? o : A.c_out - 1) * A.acc_ct + x];
+            }
+        }
+        v4i d[DIAGS];
 #pragma unroll
-            for (u32 r = 0; r < 16; r++) d[s][r] = 0;
-        // A step's weights are requested a step ahead, in two register sets in turn; no memory operation moves across LM_KEEP_ORDER (left to itself the
-        // compiler requests them where they are used, a round trip to the L2 cache per step)
+        for (u32 s = 0; s < DIAGS; s++) d[s] = (v4i){0, 0, 0, 0};
         const uint4* wa = A.wa + gi * A.wa_group + (size_t)ot * KS * DW * 64 + lane;
-        uint4 a0[DW], a1[DW];
-        auto weights = [&](u32 ks, uint4* a) {
-            const uint4* p = wa + min(ks, KS - 1) * (DW * 64);
+        for (u32 ks = 0; ks < KS; ks++) {
+            v4i a[DW];
 #pragma unroll
-            for (u32 dw = 0; dw < DW; dw++) a[dw] = p[dw * 64];
-        };
-        auto multiply = [&](u32 ks, const uint4* a) {
-            v4i b[LM_DX];
+            for (u32 dw = 0; dw < DW; dw++) {
+                const uint4 t = wa[(ks * DW + dw) * 64];
+                a[dw] = (v4i){(int)t.x, (int)t.y, (int)t.z, (int)t.w};
+            }
 #pragma unroll
             for (u32 dx = 0; dx < LM_DX; dx++) {
                 const uint4 t = lb[(ks * LM_DX + dx) * 64];
-                b[dx] = (v4i){(int)t.x, (int)t.y, (int)t.z, (int)t.w};
-            }
+                const v4i b = (v4i){(int)t.x, (int)t.y, (int)t.z, (int)t.w};
 #pragma unroll
-            for (u32 dw = 0; dw < DW; dw++) {
-                const v4i av = (v4i){(int)a[dw].x, (int)a[dw].y, (int)a[dw].z, (int)a[dw].w};
-#pragma unroll
-                for (u32 dx = 0; dx < LM_DX; dx++) d[dx + dw] = __builtin_amdgcn_mfma_i32_32x32x32_i8(av, b[dx], d[dx + dw], 0, 0, 0);
+                for (u32 dw = 0; dw < DW; dw++) d[dx + dw] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[dw], b, d[dx + dw], 0, 0, 0);
             }
-        };
-        weights(0, a0);
-        for (u32 ks = 0; ks < KS; ks += 2) {
-            if (DW == 4) { LM_KEEP_ORDER }
-            weights(ks + 1, a1);
-            if (DW == 4) { LM_KEEP_ORDER }
-            multiply(ks, a0);
-            if (DW == 4) { LM_KEEP_ORDER }
-            weights(ks + 2, a0);
-            if (DW == 4) { LM_KEEP_ORDER }
-            if (ks + 1 < KS) multiply(ks + 1, a1);
         }
-        // four rows at a time, what they are added to requested four rows ahead
-        auto at = [&](u32 r) { return 32 * ot + 8 * (r >> 2) + 4 * half + (r & 3); };
-        u64 old[2][4];
-        auto request = [&](u32 q) {
 #pragma unroll
-            for (u32 r = 0; r < 4; r++) {
-                const u32 o = at(4 * q + r);
-                old[q & 1][r] = acc[(o < A.c_out ? o : A.c_out - 1) * A.acc_ct + x];
+        for (u32 r = 0; r < 4; r++) {
+            const u32 o = 16 * ot + 4 * quarter + r;
+#pragma unroll
+            for (u32 i = 0; i < GROUPS; i++) {
+                const u32 top = 4 * i + 3 < DIAGS ? 4 * i + 3 : DIAGS - 1;
+                double t = (double)d[top][r];
+                for (u32 s = top; s > 4 * i; s--) t = __builtin_fma(t, 256.0, (double)d[s - 1][r]);
+                part[i] = t;
             }
-        };
-        auto finish = [&](auto whole) {  // the last operations of whole tiles without a branch
-            constexpr bool WHOLE = decltype(whole)::value;
-            if (ADD) request(0);
-#pragma unroll
-            for (u32 q = 0; q < 4; q++) {
-                if (ADD && q < 3) request(q + 1);
-#pragma unroll
-                for (u32 r = 4 * q; r < 4 * q + 4; r++) {
-                    const u32 o = at(r);
-#pragma unroll
-                    for (u32 g = 0; g < GROUPS; g++) {
-                        const u32 top = 4 * g + 3 < DIAGS ? 4 * g + 3 : DIAGS - 1;
-                        double t = (double)d[top][r];
-                        for (u32 s = top; s > 4 * g; s--) t = __builtin_fma(t, 256.0, (double)d[s - 1][r]);
-                        part[g] = t;
-                    }
-                    double v = DW > 1 ? f64m_dot_w<GROUPS + 1>(part, cw, m.q, m.qinv) : f64m_dot_w<GROUPS>(part, cw, m.q, m.qinv);
-                    if (!WHOLE && o >= A.c_out) continue;
-                    if (!WHOLE && bias && comp == 0)
-                        v = f64m_reduce(v + f64m_mulmod_any(f64m_from_u64(bias[(size_t)o * A.bias_limbs + e]), K.bias[e], m.q, m.qinv), m.q, m.qinv);
-                    if (ADD) v = f64m_reduce(v + f64m_from_u64(old[q & 1][r & 3]), m.q, m.qinv);
-                    acc[o * A.acc_ct + x] = f64m_canonical(v, m.q);
-                }
-            }
-        };
-        if (DW == 4 && 32 * ot + 32 <= A.c_out && !(bias && comp == 0)) finish(std::integral_constant<bool, true>());
-        else finish(std::integral_constant<bool, false>());
+            double v = DW > 1 ? f64m_dot_w<GROUPS + 1>(part, cw, m.q, m.qinv) : f64m_dot_w<GROUPS>(part, cw, m.q, m.qinv);
+            if (o >= A.c_out) continue;
+            if (bias && comp == 0)
+                v = f64m_reduce(v + f64m_mulmod_any(f64m_from_u64(bias[(size_t)o * A.bias_limbs + e]), K.bias[e], m.q, m.qinv), m.q, m.qinv);
+            if (ADD) v = f64m_reduce(v + f64m_from_u64(old[r]), m.q, m.qinv);
+            acc[o * A.acc_ct + x] = f64m_canonical(v, m.q);
+        }
     }
 }
 
-// The matrix-core kernel takes moduli below 2^50, whole column tiles, and more channels than a chain of the vector kernel holds.
-#define LINEAR_F64_CHANNELS 8
-bool linear_mfma_applies(const ckks_ctx* c, u32 c_in) { return c->small_q && c->N >= 64 && c_in > LINEAR_F64_CHANNELS; }
-
-size_t linear_mfma_scratch_elems(u32 c_in, u32 c_out, u32 weight_bytes) {
-    return (size_t)((c_out + 31) / 32) * ((c_in + 31) / 32) * weight_bytes * 64 * 2;
+// The matrix-core kernel takes moduli below 2^50, whole column tiles, and sums that fill its tiles (64 channels x 16 outputs): a chain of the vector kernel holds 8
+// channels and 8 outputs.  Vector / matrix kernel in us, four rows of 10 limbs at N = 2^14, 8-bit weights: 8 -> 24 channels 312 / 307, 12 -> 8 131 / 150, 16 -> 24
+// 399 / 311, 12 -> 2 64 / 100, 40 -> 1 128 / 129, 40 -> 3 219 / 152.
+bool linear_mfma_applies(const ckks_ctx* c, u32 c_in, u32 c_out) {
+    if (!c->small_q || c->N < 64) return false;
+    return c_in <= 16 ? c_in > 8 && c_out > 8 : c_in > 32 || c_out > 2;
 }
 
-// 32-column tiles of a workgroup: the four waves take column tiles x output tiles, and 256 channels' digits of one column tile are 56 KB of LDS.  Four where a
-// single output tile would leave two waves idle (37 -> 29 channels, six rows of 5 limbs at N = 2^13: two 228 us, four 193).
-static u32 linear_col_tiles(u32 N, u32 KS, u32 OT) { return OT == 1 && KS <= 2 && N >= 128 ? 4 : (KS <= 4 ? 2 : 1); }
+size_t linear_mfma_scratch_elems(u32 c_in, u32 c_out, u32 weight_bytes) {
+    return (size_t)((c_out + 15) / 16) * ((c_in + 63) / 64) * weight_bytes * 64 * 2;
+}
+
+// Threads and 16-column tiles of a workgroup by the number of 64-channel steps: 28 KB of digits, or 42 and 56 KB, for four waves per SIMD
+static u32 linear_threads(u32 KS) { return KS <= 2 ? 256 : 512; }
+static u32 linear_col_tiles(u32 KS) { return KS == 1 ? 4 : 2; }
 
 template <u32 DW>
 static hipError_t launch_linear_dw(const LinearMfmaArgs& A, const LinearConsts& K, u32 rows, hipStream_t st) {
-    const u32 CT = linear_col_tiles(A.N, A.KS, A.OT);
-    const dim3 grid(A.N / (32 * CT), 2 * A.limbs, rows);
-    const size_t lds = (size_t)CT * A.KS * LM_DX * 64 * 16 + 32 * CT * 8;  // at most 57 KB and the sums: two workgroups per CU
-#define LINEAR_MFMA(CT, ADD) hipLaunchKernelGGL((linear_mfma_kernel<DW, CT, ADD>), grid, dim3(LM_THREADS), lds, st, A, K)
-    if (CT == 4 && A.add) LINEAR_MFMA(4, true);
-    else if (CT == 4) LINEAR_MFMA(4, false);
-    else if (CT == 2 && A.add) LINEAR_MFMA(2, true);
-    else if (CT == 2) LINEAR_MFMA(2, false);
-    else if (A.add) LINEAR_MFMA(1, true);
-    else LINEAR_MFMA(1, false);
+    const u32 CT = linear_col_tiles(A.KS), threads = linear_threads(A.KS);
+    const dim3 grid(A.N / (16 * CT), 2 * A.limbs, rows);
+    const size_t lds = (size_t)CT * A.KS * LM_DX * 64 * 16 + 16 * CT * 8;
+#define LINEAR_MFMA(CT, T, ADD) hipLaunchKernelGGL((linear_mfma_kernel<DW, CT, T, ADD>), grid, dim3(T), lds, st, A, K)
+    if (CT == 4 && A.add) LINEAR_MFMA(4, 256, true);
+    else if (CT == 4) LINEAR_MFMA(4, 256, false);
+    else if (threads == 256 && A.add) LINEAR_MFMA(2, 256, true);
+    else if (threads == 256) LINEAR_MFMA(2, 256, false);
+    else if (A.add) LINEAR_MFMA(2, 512, true);
+    else LINEAR_MFMA(2, 512, false);
 #undef LINEAR_MFMA
     return hipGetLastError();
 }
@@ -298,7 +258,7 @@ hipError_t launch_linear_mfma(const ckks_ctx* c, const LinearSum& S, u64* scratc
     for (u32 c0 = 0; c0 < S.c_in; c0 += LM_CHUNK) {
         const u32 nc = S.c_in - c0 < LM_CHUNK ? S.c_in - c0 : LM_CHUNK;
         const char* wc = (const char*)S.w + c0 * S.w_in * wb;
-        const u32 KS = (nc + 31) / 32, OT = (S.c_out + 31) / 32, prep = OT * KS * wb * 64;
+        const u32 KS = (nc + 63) / 64, OT = (S.c_out + 15) / 16, prep = OT * KS * wb * 64;
         uint4* wa = (uint4*)(scratch + S.groups.n * linear_mfma_scratch_elems(c0, S.c_out, wb));
         if (!prepared) {
             const dim3 pg((prep + LM_THREADS - 1) / LM_THREADS, S.groups.n);
@@ -309,8 +269,8 @@ hipError_t launch_linear_mfma(const ckks_ctx* c, const LinearSum& S, u64* scratc
 #undef LINEAR_PREP
         }
         // outputs of a workgroup: all, unless that leaves the chip short of workgroups
-        const u32 ct = linear_col_tiles(c->N, KS, OT), step = 4 / ct;
-        const u64 wgs = (u64)(c->N / (32 * ct)) * 2 * S.limbs * S.rows;
+        const u32 ct = linear_col_tiles(KS), step = linear_threads(KS) / 64 / ct;
+        const u64 wgs = (u64)(c->N / (16 * ct)) * 2 * S.limbs * S.rows;
         u32 n_split = wgs >= 1024 ? 1 : (u32)(1024 / wgs);
         u32 per = (OT + n_split - 1) / n_split;
         per = (per + step - 1) / step * step;

@@ -91,6 +91,14 @@ def test_grouped_product_of_extreme_values(ring, dtype):
     linear_case(ring, ring[1] - 1, (1,), 70, 5, dtype, True, False, (1 << 64) - 1, 9, extremes=True)
 
 
+@pytest.mark.parametrize("dtype", [np.int8, np.int32])
+@pytest.mark.parametrize("c_in,c_out", [(9, 8), (16, 3), (16, 9), (17, 1), (17, 3), (32, 2), (33, 1), (8, 9), (48, 15), (64, 17), (192, 16), (193, 18)])
+def test_grouped_product_where_the_kernels_change(c_in, c_out, dtype):
+    """Both sides of the rule that names the kernel, and tiles of 16 outputs and 64 channels filled, by one short of and by one past."""
+    linear_case((13, 3, 1, 2, 50), 2, (1, 0, 2), c_in, c_out, dtype, True, False, 5 << 41, 7 * c_in + c_out)
+    linear_case((12, 3, 1, 2, 50), 1, (1,), c_in, c_out, dtype, True, True, (1 << 64) - 1, c_out, extremes=True)
+
+
 def test_grouped_product_of_a_large_ring():
     linear_case((16, 3, 1, 1, 50), 2, (1, 1), 9, 10, np.int32, True, False, 1 << 20, 4, strided=True)
 
