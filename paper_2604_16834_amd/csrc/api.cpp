@@ -2228,17 +2228,19 @@ static int rope_check(const ckks_ctx* c, const he_rope_desc* d) {
 // The products of whole batches of pairs are rescaled from the workspace where that is one launch of the small rings' rescale, and with moduli of 2^50 and more; elsewhere
 // only their dropped limb is stored, and the others are formed by the pass that ends the division (launch_ntt_rescale_vec), as many pairs at a time as the bytes below hold
 // converted limbs of.  Stored / formed at the end in us: eight channels of 4 limbs at N = 2^12 16.5 / 26, 42 of 10 limbs at 2^14 236 / 115, 64
-// of 24 at 2^16 2216 / 1500
+// of 24 at 2^16 2216 / 1374.  Bytes at a time, 64 of 24 limbs at 2^16 and 128 of 19 at 2^15 in us: 64 MB 1954 and 1503, 256 MB 1606 and 1269 (the last-level cache
+// does not pay for the launches' tails), 512 MB 1504 and 1192, 1 GB 1444 and 1131, 2 GB 1374 and 1103
 #define ROPE_BATCH (CT_BATCH / 2)  // pairs whose products are stored and rescaled together
-#define ROPE_CONV_BYTES ((size_t)512 << 20)
+#define ROPE_CONV_BYTES ((size_t)2048 << 20)
 static bool rope_stored(const ckks_ctx* c, const he_rope_desc* d) {
     const u64 pairs = (u64)d->n_heads * d->n_pairs;
     return !ntt_has_modup(c) || (pairs <= ROPE_BATCH && ntt_rescale_one_launch(c, d->level, 4 * (u32)pairs));
 }
 static u32 rope_batch(const ckks_ctx* c, const he_rope_desc* d) {
     const u64 pairs = (u64)d->n_heads * d->n_pairs, fit = rope_stored(c, d) ? ROPE_BATCH : ROPE_CONV_BYTES / ((size_t)32 * d->level * c->N);
-    const u64 n = fit < 1 ? 1 : (fit > 512 ? 512 : fit);  // (the transforms' launches number the components in 16 bits)
-    return (u32)(n < pairs ? n : (pairs ? pairs : 1));
+    const u64 most = fit < 1 ? 1 : (fit > 512 ? 512 : fit);  // (the transforms' launches number the components in 16 bits)
+    const u64 parts = (pairs + most - 1) / most;             // even ones
+    return parts ? (u32)((pairs + parts - 1) / parts) : 1;
 }
 size_t he_rope_workspace_bytes(const ckks_ctx* c, const he_rope_desc* d) {
     if (!c || rope_check(c, d)) return 0;

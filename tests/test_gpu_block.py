@@ -339,6 +339,28 @@ def test_grouped_product_and_rotary_positions_in_several_batches():
         assert torch.equal(whole[h:h + 1], hx.he_rope_axes(ctx, level, x[h:h + 1], *tab, interleaved=True)), h
 
 
+def device_residues(seed, p, limbs, *lead):
+    """[*lead][limbs][N] uniform residues made on the GPU."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    q = torch.tensor(p.moduli[:limbs], dtype=torch.int64, device="cuda").unsqueeze(-1)
+    return torch.randint(0, (1 << 62), (*lead, limbs, p.n), generator=gen, device="cuda").remainder_(q)
+
+
+@pytest.mark.parametrize("ring,heads,n_pairs,rest", [((17, 18, 1, 2), 8, 4, 1), ((12, 3, 1, 1), 150, 4, 0)])
+def test_rotary_positions_in_two_batches(ring, heads, n_pairs, rest):
+    """More pairs than 2 GB of converted limbs (N = 2^17, 17 limbs: 30), and more than 512: single heads of the call against the same heads alone, a pair of the last against
+    the oracle."""
+    p, orc, ctx = world(*ring)
+    level = p.num_q - 1
+    x = device_residues(1, p, level + 1, heads, 2 * n_pairs + rest, 2)
+    cos, sin = device_residues(2, p, level + 1, n_pairs), device_residues(3, p, level + 1, n_pairs)
+    got = hx.he_rope_axes(ctx, level, x, cos, sin, inverse=True)
+    for h in (0, heads // 2 - 1, heads // 2, heads - 2, heads - 1):
+        assert torch.equal(got[h:h + 1], hx.he_rope_axes(ctx, level, x[h:h + 1], cos, sin, inverse=True)), h
+    want = orc.rope_axes(hx.to_host(x[heads - 1, [0, n_pairs]]), level, hx.to_host(cos[:1]), hx.to_host(sin[:1]), inverse=True)
+    assert np.array_equal(hx.to_host(got[heads - 1, [0, n_pairs]]), np.array(want))
+
+
 # ------------------------------------------------------------------------------------------ together, streams, graphs, refusals
 def block_calls(ctx, level, x, w, tab, rlk, k, ws):
     h = hx.he_norm_gate(ctx, level, x, k[0], k[1], k[2], k[3:], rlk, ws=ws)
