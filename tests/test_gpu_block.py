@@ -99,6 +99,12 @@ def test_grouped_product_where_the_kernels_change(c_in, c_out, dtype):
     linear_case((12, 3, 1, 2, 50), 1, (1,), c_in, c_out, dtype, True, True, (1 << 64) - 1, c_out, extremes=True)
 
 
+@pytest.mark.parametrize("log_n", [5, 6, 7])
+@pytest.mark.parametrize("c_in", [20, 100, 250])
+def test_grouped_product_on_rings_of_about_one_workgroup(log_n, c_in):
+    linear_case((log_n, 4, 2, 2, 20), 3, (1, 2), c_in, 18, np.int16, True, False, 12345, c_in)
+
+
 def test_grouped_product_of_a_large_ring():
     linear_case((16, 3, 1, 1, 50), 2, (1, 1), 9, 10, np.int32, True, False, 1 << 20, 4, strided=True)
 
