@@ -181,12 +181,21 @@ def empty(*shape) -> torch.Tensor:
     return torch.empty(*shape, dtype=torch.int64, device=_expect_device)
 
 
-def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
+_WORDS = (torch.int64, torch.uint64)
+
+
+def _ptr(t: Optional[torch.Tensor], types=(*_WORDS, torch.float64)) -> Optional[int]:
+    """Address of a contiguous tensor whose elements are eight bytes each: the callers count words, and the library reads and writes words."""
     if t is None:
         return None
-    if t.device.type != _expect_device or t.dtype not in (torch.int64, torch.uint64, torch.uint8, torch.float64) or not t.is_contiguous():
-        raise ValueError(f"need a contiguous int64 (float64 for the self-test hook) tensor on {_expect_device}")
+    if t.device.type != _expect_device or t.dtype not in types or not t.is_contiguous():
+        raise ValueError(f"need a contiguous tensor on {_expect_device} of one of the types {', '.join(str(d) for d in types)}")
     return t.data_ptr()
+
+
+def _raw_ptr(t: torch.Tensor) -> int:
+    """The same where bytes are counted (workspaces) or nothing is (keys)."""
+    return _ptr(t, (*_WORDS, torch.uint8, torch.float64))
 
 
 def _stream(stream) -> Optional[int]:
@@ -209,7 +218,7 @@ class Key:
         self.galois_elt = galois_elt
         self._ctx = ctx
         h = C.c_void_p()
-        ctx._check(_lib.ckks_key_load(ctx.handle, _ptr(tensor), galois_elt, C.byref(h)))
+        ctx._check(_lib.ckks_key_load(ctx.handle, _raw_ptr(tensor), galois_elt, C.byref(h)))
         self.handle = h
 
     def __del__(self):
@@ -298,7 +307,7 @@ def ckks_keyswitch(ctx: Context, c: torch.Tensor, level: int, key: Key, out: Opt
     if out is None:
         out = empty(2, level + 1, ctx.N)
     ws = _ws(ctx, ws, ckks_workspace_bytes(ctx, CKKS_OP_KEYSWITCH, level))
-    ctx._check(_lib.ckks_keyswitch(ctx.handle, _ptr(c), level, key.handle if key else None, _ptr(out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+    ctx._check(_lib.ckks_keyswitch(ctx.handle, _ptr(c), level, key.handle if key else None, _ptr(out), _raw_ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
     return out
 
 
@@ -317,7 +326,7 @@ def ckks_rotate_hoisted(ctx: Context, ct: torch.Tensor, level: int, offsets: Seq
     offs = (C.c_int32 * n)(*[int(r) for r in offsets])
     ks = _ptr_array([k.handle.value if k is not None else None for k in keys])
     os_ = _ptr_array([_ptr(o) for o in outs])
-    ctx._check(_lib.ckks_rotate_hoisted(ctx.handle, _ptr(ct), level, offs, n, ks, os_, int(bool(hoisted)), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+    ctx._check(_lib.ckks_rotate_hoisted(ctx.handle, _ptr(ct), level, offs, n, ks, os_, int(bool(hoisted)), _raw_ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
     return outs
 
 
@@ -348,7 +357,7 @@ def ckks_rescale(ctx: Context, ct: torch.Tensor, level: int, out: Optional[torch
     if out is None:
         out = empty(2, max(level, 1), ctx.N)
     ws = _ws(ctx, ws, ckks_workspace_bytes(ctx, CKKS_OP_RESCALE, level))
-    ctx._check(_lib.ckks_rescale(ctx.handle, _ptr(ct), level, _ptr(out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+    ctx._check(_lib.ckks_rescale(ctx.handle, _ptr(ct), level, _ptr(out), _raw_ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
     return out
 
 
@@ -367,7 +376,7 @@ def ckks_ctct_mul_relin(ctx: Context, a: torch.Tensor, b: torch.Tensor, level: i
     if out is None:
         out = empty(2, level + 1, ctx.N)
     ws = _ws(ctx, ws, ckks_workspace_bytes(ctx, CKKS_OP_CTCT_MUL_RELIN, level))
-    ctx._check(_lib.ckks_ctct_mul_relin(ctx.handle, _ptr(a), _ptr(b), level, rlk.handle if rlk else None, _ptr(out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+    ctx._check(_lib.ckks_ctct_mul_relin(ctx.handle, _ptr(a), _ptr(b), level, rlk.handle if rlk else None, _ptr(out), _raw_ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
     return out
 
 
@@ -453,7 +462,7 @@ def he_conv_batched(ctx: Context, height: int, width: int, batch: int, level: in
     ia = _ptr_array([_ptr(t) for t in ins])
     ka = _ptr_array([k.handle.value if k is not None else None for k in rot_keys])
     oa = _ptr_array([_ptr(o) for o in outs])
-    ctx._check(_lib.he_conv_batched(ctx.handle, C.byref(d), ia, ka, _ptr(tap_masks), _ptr(w_res), oa, _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+    ctx._check(_lib.he_conv_batched(ctx.handle, C.byref(d), ia, ka, _ptr(tap_masks), _ptr(w_res), oa, _raw_ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
     return outs
 
 
@@ -477,7 +486,7 @@ def he_poly_act_deg7(ctx: Context, xs: Sequence[torch.Tensor], level: int, k: Se
     ka = (C.c_int64 * 4)(*[int(v) for v in k])
     xa = _ptr_array([_ptr(x) for x in xs])
     oa = _ptr_array([_ptr(o) for o in outs])
-    ctx._check(_lib.he_poly_act_deg7(ctx.handle, xa, n, level, ka, rlk.handle if rlk else None, int(bool(merged)), oa, _ptr(ws),
+    ctx._check(_lib.he_poly_act_deg7(ctx.handle, xa, n, level, ka, rlk.handle if rlk else None, int(bool(merged)), oa, _raw_ptr(ws),
                                      ws.numel() * ws.element_size(), _stream(stream)))
     return outs
 
@@ -506,7 +515,7 @@ def he_accumulator_merge(ctx: Context, cts: Sequence[torch.Tensor], level: int, 
     ws = _ws(ctx, ws, he_accumulator_workspace_bytes(ctx, level, g))
     ca = _ptr_array([_ptr(t) for t in cts])
     ka = _ptr_array([k.handle.value if k is not None else None for k in keys])
-    ctx._check(_lib.he_accumulator_merge(ctx.handle, ca, g, level, sts, _ptr(mask), ka, _ptr(out), _ptr(ws),
+    ctx._check(_lib.he_accumulator_merge(ctx.handle, ca, g, level, sts, _ptr(mask), ka, _ptr(out), _raw_ptr(ws),
                                          ws.numel() * ws.element_size(), _stream(stream)))
     return out
 
@@ -572,7 +581,7 @@ def he_relayout_two_rotations(ctx: Context, cts: Sequence[torch.Tensor], level: 
     i32 = lambda v: (C.c_int32 * len(v))(*[int(x) for x in v])
     ctx._check(_lib.he_relayout_two_rotations(ctx.handle, _ptr_array([_ptr(t) for t in cts]), n_ct, level, i32(lo), n_lo, arr(lo_keys),
                                               i32(hi), n_hi, arr(hi_keys), _ptr_array([_ptr(m) for row in masks for m in row]), schedule,
-                                              _ptr_array([_ptr(t) for t in outs]), _ptr(ws), ws.numel() * ws.element_size(),
+                                              _ptr_array([_ptr(t) for t in outs]), _raw_ptr(ws), ws.numel() * ws.element_size(),
                                               _stream(stream)))
     return list(outs)
 
@@ -609,7 +618,7 @@ def he_fc_batched(ctx: Context, ct: torch.Tensor, level: int, d_in: int, d_out: 
     arr = lambda ks: _ptr_array([k.handle.value if k is not None else None for k in ks])
     ctx._check(_lib.he_fc_batched(ctx.handle, C.byref(_FcDesc(d_in, d_out, batch, level, base)), _ptr(ct), _ptr(w_enc), arr(sum_keys),
                                   arr(merge_keys), _ptr(merge_mask), _ptr(place_masks), arr(lo_keys), arr(hi_keys), _ptr(bias),
-                                  _ptr(out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+                                  _ptr(out), _raw_ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
     return out
 
 
@@ -621,7 +630,7 @@ def _ct_array(ctx: Context, t: torch.Tensor, n: int, limbs: int, what: str, plai
     """A tensor [..., 2, limbs or more, N] (plain: [..., limbs or more, N]) of n ciphertexts as the library takes it: limbs N apart, the ciphertexts at
     equal distances; it may be a view into a larger tensor."""
     tail = 2 if plain else 3
-    if t.device.type != _expect_device or t.dtype not in (torch.int64, torch.uint64):
+    if t.device.type != _expect_device or t.dtype not in _WORDS:
         raise ValueError(f"{what}: need an int64 tensor on {_expect_device}")
     if t.dim() < tail or t.shape[-1] != ctx.N or t.shape[-2] < limbs or (not plain and t.shape[-3] != 2) or math.prod(t.shape[:-tail]) != n:
         raise ValueError(f"{what}: need {n} {'plaintexts [limbs][N]' if plain else 'ciphertexts [2][limbs][N]'} of at least {limbs} limbs, got {tuple(t.shape)}")
@@ -679,7 +688,7 @@ def he_linear_grouped(ctx: Context, level: int, group_rows: Sequence[int], x: to
     out = _out(ctx, out, total, c_out, 2, level, ctx.N)
     arr = _ct_array(ctx, x, total * c_in, level + 1, "x")
     ws = ctx.workspace(int(_lib.he_linear_workspace_bytes(ctx.handle, C.byref(d), rows))) if ws is None else ws
-    ctx._check(_lib.he_linear_grouped(ctx.handle, C.byref(d), rows, C.byref(arr), w.data_ptr(), _ptr(bias), _ptr(out), _ptr(ws),
+    ctx._check(_lib.he_linear_grouped(ctx.handle, C.byref(d), rows, C.byref(arr), w.data_ptr(), _ptr(bias, _WORDS), _ptr(out, _WORDS), _raw_ptr(ws),
                                       ws.numel() * ws.element_size(), _stream(stream)))
     return out
 
@@ -700,8 +709,8 @@ def he_rope_axes(ctx: Context, level: int, x: torch.Tensor, cos: torch.Tensor, s
     out = _out(ctx, out, heads, head_dim, 2, level, ctx.N)
     arr = _ct_array(ctx, x, heads * head_dim, level + 1, "x")
     ws = ctx.workspace(int(_lib.he_rope_workspace_bytes(ctx.handle, C.byref(d)))) if ws is None else ws
-    ctx._check(_lib.he_rope_axes(ctx.handle, C.byref(d), C.byref(arr), _ptr(cos), _ptr(sin), _ptr(out), _ptr(ws), ws.numel() * ws.element_size(),
-                                 _stream(stream)))
+    ctx._check(_lib.he_rope_axes(ctx.handle, C.byref(d), C.byref(arr), _ptr(cos, _WORDS), _ptr(sin, _WORDS), _ptr(out, _WORDS), _raw_ptr(ws),
+                                 ws.numel() * ws.element_size(), _stream(stream)))
     return out
 
 
@@ -731,7 +740,7 @@ def he_norm_gate(ctx: Context, level: int, x: torch.Tensor, k_eps: int, k_slope:
     ra = _ct_array(ctx, residual, channels, max(last, 0) + 1, "residual") if residual is not None else None
     ws = ctx.workspace(int(_lib.he_norm_workspace_bytes(ctx.handle, C.byref(d)))) if ws is None else ws
     ctx._check(_lib.he_norm_gate(ctx.handle, C.byref(d), kn, C.byref(xa), C.byref(ga) if ga else None, C.byref(ra) if ra else None,
-                                 rlk.handle if rlk else None, _ptr(out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+                                 rlk.handle if rlk else None, _ptr(out, _WORDS), _raw_ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
     return out
 
 
