@@ -9,6 +9,7 @@
 #include <new>
 #include <vector>
 
+#include "ctarray.h"
 #include "ctx.h"
 
 namespace {
@@ -2035,16 +2036,9 @@ int he_poly_act_deg7(const ckks_ctx* c, const uint64_t* const* h_d_x, uint32_t n
 }
 
 // ---- a transformer block's operators ---------------------------------------------------------------------
-// Checks of a vector of n ciphertexts of which `limbs` limbs of n_comp components are read: what the kernels' 16-byte loads and indexes assume.
 static int check_array(const ckks_ctx* c, const he_ct_array* a, size_t n, u32 limbs, u32 n_comp) {
-    if (!a || !a->d) return set_err(c, CKKS_ERR_INVALID_ARG, "null ciphertext array");
-    const u64 one = (u64)limbs * c->N, most = (u64)1 << 40;  // 2^40 words: no product of a stride and a count overflows
-    if (((uintptr_t)a->d & 15) || (a->ct_stride & 1) || (n_comp > 1 && (a->comp_stride & 1)))
-        return set_err(c, CKKS_ERR_INVALID_ARG, "ciphertext array: not aligned to 16 bytes, or an odd stride");
-    if (a->ct_stride > most || (n_comp > 1 && a->comp_stride > most)) return set_err(c, CKKS_ERR_INVALID_ARG, "ciphertext array: stride out of range");
-    if (n_comp > 1 && a->comp_stride < one) return set_err(c, CKKS_ERR_INVALID_ARG, "ciphertext array: components overlap");
-    if (n > 1 && a->ct_stride != 0 && a->ct_stride < (n_comp > 1 ? a->comp_stride : 0) + one) return set_err(c, CKKS_ERR_INVALID_ARG, "ciphertext array: ciphertexts overlap");
-    return CKKS_OK;
+    const char* fault = ct_array_fault(a, n, limbs, n_comp, c->N);
+    return fault ? set_err(c, CKKS_ERR_INVALID_ARG, fault) : CKKS_OK;
 }
 
 static LimbScalars limb_scalars(const ckks_ctx* c, u32 level, int64_t k) {
