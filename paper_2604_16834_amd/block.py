@@ -21,10 +21,13 @@ class QuantisedWeights(NamedTuple):
 
 def quantise_weights(weights, q_level: int, bits: int = 32, gain: float = 1.0) -> QuantisedWeights:
     """Weights rounded to integers of 8, 16 or 32 bits, and the multiplier round(step * q_level * gain): the product's outputs have `gain` times the scale of its
-    inputs but for the rounding, exactly what ``linear_scale`` gives."""
+    inputs but for the rounding (the multiplier is one at least: where step * q_level * gain is below that, as with short moduli, the scale grows by more), exactly
+    what ``linear_scale`` gives."""
     w = np.asarray(weights, dtype=np.float64)
     if bits not in (8, 16, 32):
         raise ValueError("bits must be 8, 16 or 32")
+    if not 0.0 < gain < math.inf:
+        raise ValueError("gain must be positive and finite")
     top = float(np.abs(w).max()) if w.size else 0.0
     if not math.isfinite(top):
         raise ValueError("weights must be finite")

@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import paper_2604_16834_amd as hx
+from paper_2604_16834_amd.block import linear_scale, quantise_weights
 
 N, LEVEL = 16, 3
 
@@ -89,3 +90,18 @@ def test_operands_of_other_calls_have_eight_byte_elements(library):
     with pytest.raises(ValueError):
         hx.ckks_rescale(ctx, ct.to(torch.uint8), LEVEL)
     assert library.calls == ["ckks_rescale"]
+
+
+@pytest.mark.parametrize("gain", [0.0, -1.0, float("nan"), float("inf"), float("-inf")])
+def test_a_gain_has_to_be_positive_and_finite(gain):
+    """A negative or zero gain would leave the multiplier at one: outputs at a scale far below the noise, and no error."""
+    with pytest.raises(ValueError):
+        quantise_weights([[0.5, -0.25]], (1 << 50) - 27, 16, gain=gain)
+
+
+def test_a_multiplier_is_at_least_one_and_its_scale_is_told():
+    """Where step * q_level * gain is below one the scale grows instead; linear_scale follows the multiplier that is used."""
+    q = (1 << 20) - 3
+    qw = quantise_weights([[1.0, -0.5]], q, 32)
+    assert qw.multiplier == 1 and qw.step * q < 0.5
+    assert linear_scale(2.0 ** 30, qw, q) == 2.0 ** 30 / qw.step / q
