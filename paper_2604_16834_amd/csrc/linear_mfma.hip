@@ -12,9 +12,10 @@
 // (f64m_dot_w): 45 double-precision operations an output, the multiplier included.
 //
 // A workgroup owns 64 columns (up to 64 channels) or 32 of one row, component and limb: it reads them once, for all channels, turns them into digits in LDS, and its
-// waves take units of 16 outputs x 16 columns in turn, so X streams from HBM exactly once for any number of outputs.  Such a unit's diagonals are 28 to 40 registers, and
+// waves take units of 16 outputs x 16 columns in turn: X is read once for all outputs, unless the columns alone leave the chip short of workgroups
+// (fewer than 1024: the outputs are then split over several, each of which reads and converts them).  Such a unit's diagonals are 28 to 40 registers, and
 // four waves per SIMD hide each other's loads, products and folds.  Bound by HBM (a column is 8 (c_in + 2 c_out) bytes with what is added to, against c_in c_out 7 DW
-// digit products): 64 -> 64 channels, 8-bit weights, three rows of 23 limbs at N = 2^16 3.03 ms, 4.6 TB/s; 256 -> 192, 32-bit weights, two rows of 12 limbs 5.7 ms, 2.8 TB/s.
+// digit products): 64 -> 64 channels, 8-bit weights, three rows of 23 limbs at N = 2^16 3.07 ms, 4.5 TB/s; 256 -> 192, 32-bit weights, two rows of 12 limbs 5.87 ms, 2.7 TB/s.
 // Tried and slower: units of 32 x 32 (160 registers of diagonals, two waves per SIMD: 3.25 and 6.5 ms, the matrix pipe 30 % and the vector units 34 % busy, the two
 // workgroups of a CU load, multiply and fold in step); one persistent workgroup of eight waves per CU, two of which read and convert the next tile while six multiply
 // (6.9 to 9 ms in the second case: too few loads in flight); the next step's weights requested a step ahead (2 % slower: registers); what is added to requested behind
@@ -207,7 +208,10 @@ __global__ __launch_bounds__(THREADS, 4) void linear_mfma_kernel(LinearMfmaArgs 
 
 // The matrix-core kernel takes moduli below 2^50, whole column tiles, and sums that fill its tiles (64 channels x 16 outputs): a chain of the vector kernel holds 8
 // channels and 8 outputs.  Vector / matrix kernel in us, four rows of 10 limbs at N = 2^14, 8-bit weights: 8 -> 24 channels 312 / 307, 12 -> 8 131 / 150, 16 -> 24
-// 399 / 311, 12 -> 2 64 / 100, 40 -> 1 128 / 129, 40 -> 3 219 / 152.
+// 399 / 311, 12 -> 2 64 / 100, 40 -> 1 128 / 129, 40 -> 3 219 / 152.  Whole calls with up to eight channels and many outputs, 8- and 32-bit weights, vector (the same for
+// both) / matrix, matrix: 2 -> 24 250 / 286, 315, 2 -> 192 1940 / 2017, 2168, 4 -> 24 269 / 290, 321, 4 -> 192 2105 / 2013, 2178, 8 -> 24 317 / 296, 335, 8 -> 192 2380 / 2019,
+// 2181; one row of 24 limbs at 2^16: 4 -> 192 5310 / 4986, 5373, 8 -> 192 6200 / 4991, 5385.  So up to four channels the rule is the faster side or within 7 % of it;
+// at eight channels and more than some 40 outputs the matrix kernel would be up to 24 % faster.
 bool linear_mfma_applies(const ckks_ctx* c, u32 c_in, u32 c_out) {
     if (!c->small_q || c->N < 64) return false;
     return c_in <= 16 ? c_in > 8 && c_out > 8 : c_in > 32 || c_out > 2;

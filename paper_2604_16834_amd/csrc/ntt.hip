@@ -800,7 +800,8 @@ __device__ __forceinline__ void fwd_lo_rounds(double (&v)[8], double* lds0, doub
 // for two results that share operands and the slice's twiddles, one transformed after the other:
 //   VEC_TURN: the pair z = z0 + .., (a, b), of channels, one component: v = a C - b S and a S + b C (batch items 4 z + comp, 4 z + 2 + comp)
 //   VEC_GATE: the two components of ciphertext z: v = G x_0 and G x_1 (batch items 2 z, 2 z + 1)
-// Residues below 2^50.  Bound by HBM: converted limbs, operands and results once each, 1.05 ms for 64 channels of 23 limbs at N = 2^16 (4.2 TB/s).  A workgroup per result
+// Residues below 2^50.  Bound by HBM: converted limbs, operands and results once each, 1.05 to 1.11 ms for 64 channels of 23 limbs at N = 2^16 (4.35 TB/s
+// at the latter).  A workgroup per result
 // took 1.25 ms: its operands and twiddles, seven times the bytes of a result, came from the L2 cache for each.  With the operands requested in front of the second
 // transform (180 registers, two waves per SIMD instead of four) 1.15 ms.
 template <VecMode MODE>
