@@ -106,7 +106,9 @@ int ckks_ntt_inv(const ckks_ctx* ctx, uint64_t* d_polys, const uint32_t* h_modul
                  uint32_t n_limbs, uint32_t batch, void* stream);
 
 /* Wraps a caller-owned switching key (no copy).  galois_elt = 5^r mod 2N for the key of a rotation
- * by r slots, 0 for the relinearisation key (s^2 -> s). */
+ * by r slots (sigma_g(s) -> s), 0 for the relinearisation key (s^2 -> s), CKKS_KEY_CROSS | g for the cross key of a
+ * rotation (s sigma_g(s) -> s), which the products with a rotated operand take (he_scan_gated). */
+#define CKKS_KEY_CROSS 0x80000000u
 int ckks_key_load(const ckks_ctx* ctx, const uint64_t* d_key, uint32_t galois_elt, ckks_key** out_key);
 void ckks_key_free(ckks_key* key);
 
@@ -394,6 +396,89 @@ typedef struct he_norm_desc {
 size_t he_norm_workspace_bytes(const ckks_ctx* ctx, const he_norm_desc* desc);
 int he_norm_gate(const ckks_ctx* ctx, const he_norm_desc* desc, const int64_t* h_k_newton, const he_ct_array* x, const he_ct_array* gate,
                  const he_ct_array* residual, const ckks_key* rlk, uint64_t* d_out, void* d_ws, size_t ws_bytes, void* stream);
+
+/* ---- A recurrent block's operators on the same packing, forward and backward: the slots are the tokens of a batch of sequences, one sequence after the
+ * other, of any lengths (not from the paper, as above).  What mixes positions are rotations.  All of them are made of one product, of a ciphertext with a
+ * ROTATED one: a = (a0, a1), h = (h0, h1) give, without rotating h first,
+ *   a (.) Rot(h, r) = a0 sigma(h0) + a1 sigma(h0) s + a0 sigma(h1) sigma(s) + a1 sigma(h1) s sigma(s),  sigma = sigma_g, g = 5^r,
+ * so that the last two parts are brought under s by two key switches, with the rotation's key and with its cross key (CKKS_KEY_CROSS), added up on
+ * the extended basis with P times the first two, and divided by P q once: one division and one rounding, where a rotation and a product take two. */
+
+/* Gated linear recurrence over the slots, h_t = a_t h_{t-1} + x_t with encrypted gates a, as a scan in `steps` doublings:
+ *   for s = 0 .. steps - 1, at level - s:   h <- Rescale(a (.) Rot(h, -2^s) + h_k[s] h),   a <- Rescale(a (.) Rot(a, -2^s))
+ * starting from h = x, which gives every slot the sum over its last 2^steps positions.  A gate that is zero at the first token of every sequence keeps the
+ * sequences apart, whatever their lengths (slot 0 follows the last one), so steps = ceil(log2(longest sequence)); padding slots have gate and x zero.
+ * heads gates serve channels / heads channels each: channel c's is c / (channels / heads).  h_k[s] is the gate's scale at that step, rounded
+ * (scan_constants in block.py): with gates at the scale of q_level scales stay.  A plaintext gate is the ciphertext (its encoding, 0).
+ * reverse != 0: h_t = a_t h_{t+1} + x_t, rotations by +2^s, gates zero at the last tokens.
+ * rot_keys[s], cross_keys[s]: the two keys of step s's rotation.  x, gate: ciphertexts of limbs 0 .. level; d_out uint64[channels][2][level+1-steps][N];
+ * 1 <= steps <= level, 2^steps <= N/2 (a sequence of one token is its own scan). */
+typedef struct he_scan_desc {
+    uint32_t channels, heads, level;
+    uint32_t steps;   /* not read by he_scan_step */
+    uint32_t reverse; /* not read by he_scan_step */
+} he_scan_desc;
+size_t he_scan_workspace_bytes(const ckks_ctx* ctx, const he_scan_desc* desc);
+int he_scan_gated(const ckks_ctx* ctx, const he_scan_desc* desc, const int64_t* h_k, const he_ct_array* x, const he_ct_array* gate, const ckks_key* const* rot_keys,
+                  const ckks_key* const* cross_keys, uint64_t* d_out, void* d_ws, size_t ws_bytes, void* stream);
+
+/* Its backward pass: grad = the gradient with respect to the outputs, desc as in the forward call (its reverse too),
+ *   b = Rot(a, 1);  dx_t = grad_t + b_t dx_{t+1} by the scan in the other direction;  dgate = Rescale(sum of a head's channels: dx (.) Rot(h, -1))
+ * (reverse: all rotations the other way).  rot_keys[s], cross_keys[s] are those of the rotations by +2^s, back_rot, back_cross those of -1.  states: the forward
+ * call's outputs, of which limbs 0 .. level-steps are read (the gradient may start at another level than the forward pass: gate has limbs 0 .. level).
+ * d_dx uint64[channels][2][level+1-steps][N], d_dgate uint64[heads][2][level-steps][N] or NULL (gates that are not learned; states and the two keys of -1 are
+ * not read then).  At a sequence's first token dgate holds dx times the state in the slot before, another sequence's: nothing flows through a gate that is
+ * zero by construction, and a caller's own backward pass through that zero drops it.  steps <= level, one less with d_dgate. */
+size_t he_scan_backward_workspace_bytes(const ckks_ctx* ctx, const he_scan_desc* desc);
+int he_scan_gated_backward(const ckks_ctx* ctx, const he_scan_desc* desc, const int64_t* h_k, const he_ct_array* grad, const he_ct_array* gate, const he_ct_array* states,
+                           const ckks_key* const* rot_keys, const ckks_key* const* cross_keys, const ckks_key* back_rot, const ckks_key* back_cross, uint64_t* d_dx,
+                           uint64_t* d_dgate, void* d_ws, size_t ws_bytes, void* stream);
+
+/* One step of the recurrence, the form for single tokens: out_c = Rescale(a (.) Rot(h_c, r) + k x_c), one level lower.
+ * rot_key NULL and cross_key the relinearisation key: r = 0, a stream's next token replaces the one before in its slot.  Otherwise r is the keys' rotation: -1 puts the
+ * next token in the next slot, as he_scan_gated packs them.  gate: `heads` ciphertexts, state, x: `channels` (x NULL or its pointer NULL: no addend), limbs 0 .. level of all,
+ * level >= 1; d_out uint64[channels][2][level][N]. */
+size_t he_scan_step_workspace_bytes(const ckks_ctx* ctx, const he_scan_desc* desc);
+int he_scan_step(const ckks_ctx* ctx, const he_scan_desc* desc, int64_t k, const he_ct_array* gate, const he_ct_array* state, const he_ct_array* x, const ckks_key* rot_key,
+                 const ckks_key* cross_key, uint64_t* d_out, void* d_ws, size_t ws_bytes, void* stream);
+
+/* Layer norm over the C channels of every slot, with gain and bias as they are after a training step, encrypted (the same value in every slot):
+ *   S = sum_c x_c;  v = Rescale(Relin(C sum_c x_c x_c - S S)) + k_eps                 C^2 times the variance, one relinearisation; level-1
+ *   r = Rescale(k_slope * v) + k_start, then `iterations` Newton steps as in he_norm_gate     level-2-2*iterations = m
+ *   norm_c = Rescale(Relin((C x_c - S) r))                                                m-1
+ *   out_c = Rescale(Relin(gain_c norm_c) + k_bias * bias_c)                               m-2
+ * The integers are those of layer_norm_constants (block.py).  A gain and bias in the clear belong in the weights of the product behind the norm.
+ * x: limbs 0 .. level, level >= 3 + 2*iterations (4 + with a gain); gain, bias (bias NULL or its pointer NULL: none; no bias without a gain): limbs 0 .. m-1.
+ * d_norm uint64[C][2][m][N]; d_inv uint64[2][m+1][N] (r, for the backward pass) or NULL; d_out uint64[C][2][m-1][N], NULL if and only if there is no gain. */
+typedef struct he_layer_norm_desc {
+    uint32_t channels, level, iterations;
+    uint32_t affine; /* whether there is a gain */
+    int64_t k_eps, k_slope, k_start, k_bias;
+} he_layer_norm_desc;
+size_t he_layer_norm_workspace_bytes(const ckks_ctx* ctx, const he_layer_norm_desc* desc);
+int he_layer_norm(const ckks_ctx* ctx, const he_layer_norm_desc* desc, const int64_t* h_k_newton, const he_ct_array* x, const he_ct_array* gain, const he_ct_array* bias,
+                  const ckks_key* rlk, uint64_t* d_norm, uint64_t* d_inv, uint64_t* d_out, void* d_ws, size_t ws_bytes, void* stream);
+
+/* Its backward pass.  grad = the gradient with respect to out (without a gain: to norm), norm and inv = the forward call's d_norm and d_inv:
+ *   g_c = grad_c,  or Rescale(Relin(gain_c grad_c)), a level lower;  b = its level
+ *   T = sum_c g_c;  u = Rescale(Relin(sum_c g_c norm_c));  t = Rescale(Relin(inv u))                          b-1, b-2
+ *   dx_c = Rescale(Relin(inv k_grad (C g_c - T) + k_norm t norm_c))                                           b-3
+ *   dgain_c = Sum(Rescale(Relin(grad_c norm_c))),  dbias_c = Sum(grad_c)                                      level-1
+ * k_norm has the sign that makes it C inv (g - mean g - norm mean(g norm)) (layer_norm_grad_constants).  Sum adds up slots in n_stages stages: z <- z + the sum of its rotations
+ * by the h_stage_rots[i] keys of stage i, with one decomposition and one division by P for all of them; sum_keys holds the stages' keys one after the other.  One rotation a stage
+ * (1, 2, 4, ..) doubles what is summed, three (1, 2, 3; 4, 8, 12; ..) give four times; n_stages = 0: the gradients slot by slot.
+ * Limbs read: grad, gain, norm 0 .. level, inv 0 .. b-1; level >= 3, 4 with a gain.  d_dx uint64[C][2][b-2][N]; d_dgain, d_dbias uint64[C][2][level][N], or NULL: not wanted. */
+#define HE_SUM_MAX_STAGES 64
+typedef struct he_layer_norm_grad_desc {
+    uint32_t channels, level;
+    uint32_t affine; /* whether there is a gain */
+    uint32_t n_stages;
+    int64_t k_grad, k_norm;
+} he_layer_norm_grad_desc;
+size_t he_layer_norm_backward_workspace_bytes(const ckks_ctx* ctx, const he_layer_norm_grad_desc* desc);
+int he_layer_norm_backward(const ckks_ctx* ctx, const he_layer_norm_grad_desc* desc, const he_ct_array* grad, const he_ct_array* norm, const he_ct_array* inv, const he_ct_array* gain,
+                           const ckks_key* rlk, const uint32_t* h_stage_rots, const ckks_key* const* sum_keys, uint64_t* d_dx, uint64_t* d_dgain, uint64_t* d_dbias, void* d_ws,
+                           size_t ws_bytes, void* stream);
 
 /* Self-test hook (not part of the paper's method): evaluates on the GPU the routines of the double-precision modular
  * arithmetic that the transforms, basis conversions and fused inner products are made of, for moduli q < 2^50, on

@@ -889,6 +889,131 @@ class Oracle:
             out.append(self.ctct_mul_relin_rescale(self.drop_to_level(t, m), r, rlk, m, addend=add))
         return out
 
+    # -------------------------------------------------------- a recurrent block's operators
+    def gen_cross_key(self, s_ntt: np.ndarray, offset: int, seed: int) -> np.ndarray:
+        """Key switching from s sigma_g(s) to s, g = 5^offset."""
+        idx = list(range(self.M))
+        return self._gen_switch_key(s_ntt, self.mul(s_ntt, self.automorph_ntt(s_ntt, self.galois(offset)), idx), seed)
+
+    def _switched(self, polys, keys, d0, d1, level: int) -> np.ndarray:
+        """((d0, d1) + the key switches of the polynomials) / q_level, one division by P q_level."""
+        L1 = level + 1
+        v = None
+        for poly, key in zip(polys, keys):
+            inner = self.key_inner(self.modup(poly, level), key, level)
+            v = inner if v is None else self.add_ext(v, inner, level)
+        Pres = self.special_product_residues(level)[:L1]
+        out = []
+        for comp, dpart in enumerate((d0, d1)):
+            vc = v[comp].copy()
+            vc[:L1] = self.add(vc[:L1], self.scalar_mul(dpart, Pres, level), level)
+            out.append(self.moddown_rescale(vc, level))
+        return np.stack(out)
+
+    def _turned_terms(self, a, h, level: int, offset: int):
+        """a0 sigma(h0), a1 sigma(h0), a0 sigma(h1), a1 sigma(h1)."""
+        idx, g = list(range(level + 1)), self.galois(offset)
+        a, h = self.drop_to_level(a, level), self.drop_to_level(h, level)
+        h = [self.automorph_ntt(h[k], g) for k in range(2)]
+        return [self.mul(a[i], h[j], idx) for i, j in ((0, 0), (1, 0), (0, 1), (1, 1))]
+
+    def turned_product(self, a, h, level: int, offset: int, rot_key, cross_key, k: int = 0, x=None) -> np.ndarray:
+        """Rescale(a (.) Rot(h, offset) + k x)."""
+        d0, d1, u, v = self._turned_terms(a, h, level, offset)
+        if x is not None:
+            kx = self.scalar_mul(self.drop_to_level(x, level), self.scalar_residues(k, level), level)
+            d0, d1 = self.add(d0, kx[0], level), self.add(d1, kx[1], level)
+        return self._switched((u, v), (rot_key, cross_key), d0, d1, level)
+
+    def scan_gated(self, x, gates, level: int, k: Sequence[int], rot_keys, cross_keys, sign: int = -1) -> List[np.ndarray]:
+        """x: channel ciphertexts, gates: one per len(x) / len(gates) channels; step s rotates by sign * 2^s with rot_keys[s], cross_keys[s]."""
+        x, gates = list(x), list(gates)
+        per = len(x) // len(gates)
+        for s, ks in enumerate(k):
+            off, lv = sign * (1 << s), level - s
+            x, gates = ([self.turned_product(gates[c // per], x[c], lv, off, rot_keys[s], cross_keys[s], ks, x[c]) for c in range(len(x))],
+                        [self.turned_product(a, a, lv, off, rot_keys[s], cross_keys[s]) for a in gates] if s + 1 < len(k) else [])
+        return x
+
+    def scan_gated_backward(self, grad, gates, states, level: int, k: Sequence[int], rot_keys, cross_keys, back_rot, back_cross, sign: int = 1):
+        """(dx, dgate); step s rotates by sign * 2^s."""
+        turned = [self.rotate(self.drop_to_level(a, level), level, sign, rot_keys[0], hoisted=False) for a in gates]
+        dx = self.scan_gated(grad, turned, level, k, rot_keys, cross_keys, sign)
+        last, per, dgate = level - len(k), len(dx) // len(turned), []
+        for h in range(len(turned) if states is not None else 0):
+            total = None
+            for c in range(h * per, (h + 1) * per):
+                terms = self._turned_terms(dx[c], states[c], last, -sign)
+                total = terms if total is None else [self.add(s, t, last) for s, t in zip(total, terms)]
+            dgate.append(self._switched(total[2:], (back_rot, back_cross), total[0], total[1], last))
+        return dx, dgate
+
+    def layer_norm(self, x, level: int, k_eps: int, k_slope: int, k_start: int, k_newton: Sequence[int], rlk, gain=None, bias=None, k_bias: int = 0):
+        """(norm, inv, out): channel ciphertexts x; gain, bias: ciphertexts or None.  The variance is the sum over channels of the centred channels' squares, divided by
+        C where C^2 var is written as C sum x^2 - (sum x)^2: here the latter, term by term."""
+        C_, idx = len(x), list(range(level + 1))
+        total = x[0]
+        for ct in x[1:]:
+            total = self.add(total, ct, level)
+        times = lambda poly, k, lv: self.scalar_mul(poly, self.scalar_residues(k, lv), lv)  # noqa: E731
+        d = []
+        for i, j, twice in ((0, 0, 1), (0, 1, 2), (1, 1, 1)):
+            acc = times(self.mul(total[i], total[j], idx), -1, level)
+            for ct in x:
+                acc = self.add(acc, times(self.mul(ct[i], ct[j], idx), C_, level), level)
+            d.append(times(acc, twice, level))
+        s = self.add_constant(self.relin_rescale(*d, rlk, level), k_eps, level - 1)
+        scaled = lambda ct, k, lv: times(self.drop_to_level(ct, lv), k, lv)  # noqa: E731
+        r, m = self.add_constant(self.rescale(scaled(s, k_slope, level - 1), level - 1), k_start, level - 2), level - 2
+        for k in k_newton:
+            u = self.ctct_mul_relin_rescale(r, r, rlk, m)
+            w = self.ctct_mul_relin_rescale(self.drop_to_level(s, m), r, rlk, m)
+            r, m = self.ctct_mul_relin_rescale(u, w, rlk, m - 1, addend=scaled(r, k, m - 1)), m - 2
+        minus = scaled(total, -1, m)
+        norm = [self.ctct_mul_relin_rescale(self.add(scaled(ct, C_, m), minus, m), r, rlk, m) for ct in x]
+        out = None
+        if gain is not None:
+            out = [self.ctct_mul_relin_rescale(self.drop_to_level(gain[c], m - 1), norm[c], rlk, m - 1, addend=scaled(bias[c], k_bias, m - 1) if bias is not None else None)
+                   for c in range(C_)]
+        return norm, r, out
+
+    def slot_sum(self, z, level: int, offsets: Sequence[int], keys) -> np.ndarray:
+        """z + the sum of its rotations, divided by P once."""
+        v, digits = None, self.modup(z[1], level)
+        for off, key in zip(offsets, keys):
+            ext = self.aligned_ext(z, level, off, key, digits)
+            v = ext if v is None else self.add_ext(v, ext, level)
+        return self.add(z, np.stack([self.moddown(v[k], level) for k in range(2)]), level)
+
+    def layer_norm_backward(self, grad, norm, inv, level: int, k_grad: int, k_norm: int, rlk, gain=None, stages=()):
+        """(dx, dgain, dbias); stages: (offsets, keys) of each stage of the sums over slots."""
+        C_, g, b = len(grad), [self.drop_to_level(ct, level) for ct in grad], level
+        if gain is not None:
+            g, b = [self.ctct_mul_relin_rescale(self.drop_to_level(gain[c], level), g[c], rlk, level) for c in range(C_)], level - 1
+        times = lambda poly, k, lv: self.scalar_mul(poly, self.scalar_residues(k, lv), lv)  # noqa: E731
+        drop = self.drop_to_level
+        total, terms = drop(g[0], b - 2), None
+        for ct in g[1:]:
+            total = self.add(total, drop(ct, b - 2), b - 2)
+
+        def tensor(p, q, lv):
+            idx, p, q = list(range(lv + 1)), drop(p, lv), drop(q, lv)
+            return [self.mul(p[0], q[0], idx), self.add(self.mul(p[0], q[1], idx), self.mul(p[1], q[0], idx), lv), self.mul(p[1], q[1], idx)]
+
+        for c in range(C_):
+            t = tensor(g[c], norm[c], b)
+            terms = t if terms is None else [self.add(s, v, b) for s, v in zip(terms, t)]
+        u = self.relin_rescale(*terms, rlk, b)
+        t = self.ctct_mul_relin_rescale(drop(inv, b - 1), u, rlk, b - 1)
+        m, dx = b - 2, []
+        for c in range(C_):
+            centred = times(self.add(times(drop(g[c], m), C_, m), times(total, -1, m), m), k_grad, m)
+            dx.append(self.relin_rescale(*[self.add(p, q, m) for p, q in zip(tensor(inv, centred, m), tensor(times(t, k_norm, m), norm[c], m))], rlk, m))
+        sums = [self.ctct_mul_relin_rescale(drop(grad[c], level), drop(norm[c], level), rlk, level) for c in range(C_)] + [drop(ct, level - 1) for ct in grad]
+        for offsets, keys in stages:
+            sums = [self.slot_sum(z, level - 1, offsets, keys) for z in sums]
+        return dx, sums[:C_], sums[C_:]
+
     # ------------------------------------------------------------------ fully connected layer
     @staticmethod
     def fc_shifts(d_in: int, d_out: int, batch: int, base: int):

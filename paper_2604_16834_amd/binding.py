@@ -46,6 +46,8 @@ HE_GATE_NONE = 0
 HE_GATE_PLAIN = 1
 HE_GATE_CIPHER = 2
 HE_NORM_MAX_ITERATIONS = 16
+CKKS_KEY_CROSS = 0x80000000
+HE_SUM_MAX_STAGES = 64
 
 EXPORTS = (
     "ckks_ctx_create", "ckks_ctx_destroy", "ckks_last_error_string", "ckks_workspace_bytes",
@@ -55,6 +57,8 @@ EXPORTS = (
     "he_accumulator_workspace_bytes", "he_accumulator_merge", "he_fc_workspace_bytes", "he_fc_batched",
     "he_relayout_workspace_bytes", "he_relayout_two_rotations", "ckks_key_expand_a", "ckks_keyset_stage", "ckks_ctx_set_overlap",
     "he_linear_workspace_bytes", "he_linear_grouped", "he_rope_workspace_bytes", "he_rope_axes", "he_norm_workspace_bytes", "he_norm_gate",
+    "he_scan_workspace_bytes", "he_scan_gated", "he_scan_backward_workspace_bytes", "he_scan_gated_backward", "he_scan_step_workspace_bytes", "he_scan_step",
+    "he_layer_norm_workspace_bytes", "he_layer_norm", "he_layer_norm_backward_workspace_bytes", "he_layer_norm_backward",
     "ckks_prof_kernel_count", "ckks_prof_kernel_name", "ckks_prof_begin", "ckks_prof_end",
 )
 
@@ -98,6 +102,20 @@ class _RopeDesc(C.Structure):
 class _NormDesc(C.Structure):
     _fields_ = [("channels", C.c_uint32), ("level", C.c_uint32), ("iterations", C.c_uint32), ("gate", C.c_uint32), ("k_eps", C.c_int64),
                 ("k_slope", C.c_int64), ("k_start", C.c_int64), ("k_residual", C.c_int64)]
+
+
+class _ScanDesc(C.Structure):
+    _fields_ = [("channels", C.c_uint32), ("heads", C.c_uint32), ("level", C.c_uint32), ("steps", C.c_uint32), ("reverse", C.c_uint32)]
+
+
+class _LayerNormDesc(C.Structure):
+    _fields_ = [("channels", C.c_uint32), ("level", C.c_uint32), ("iterations", C.c_uint32), ("affine", C.c_uint32), ("k_eps", C.c_int64),
+                ("k_slope", C.c_int64), ("k_start", C.c_int64), ("k_bias", C.c_int64)]
+
+
+class _LayerNormGradDesc(C.Structure):
+    _fields_ = [("channels", C.c_uint32), ("level", C.c_uint32), ("affine", C.c_uint32), ("n_stages", C.c_uint32), ("k_grad", C.c_int64),
+                ("k_norm", C.c_int64)]
 
 
 def _bind(path: str):
@@ -155,6 +173,16 @@ def _bind(path: str):
     lib.he_norm_workspace_bytes.argtypes = [vp, C.POINTER(_NormDesc)]
     lib.he_norm_workspace_bytes.restype = sz
     lib.he_norm_gate.argtypes = [vp, C.POINTER(_NormDesc), C.POINTER(C.c_int64), arr, arr, arr, vp, vp, vp, sz, vp]
+    keys, i64p = C.POINTER(vp), C.POINTER(C.c_int64)
+    for f, d in ((lib.he_scan_workspace_bytes, _ScanDesc), (lib.he_scan_backward_workspace_bytes, _ScanDesc), (lib.he_scan_step_workspace_bytes, _ScanDesc),
+                 (lib.he_layer_norm_workspace_bytes, _LayerNormDesc), (lib.he_layer_norm_backward_workspace_bytes, _LayerNormGradDesc)):
+        f.argtypes = [vp, C.POINTER(d)]
+        f.restype = sz
+    lib.he_scan_gated.argtypes = [vp, C.POINTER(_ScanDesc), i64p, arr, arr, keys, keys, vp, vp, sz, vp]
+    lib.he_scan_gated_backward.argtypes = [vp, C.POINTER(_ScanDesc), i64p, arr, arr, arr, keys, keys, vp, vp, vp, vp, vp, sz, vp]
+    lib.he_scan_step.argtypes = [vp, C.POINTER(_ScanDesc), C.c_int64, arr, arr, arr, vp, vp, vp, vp, sz, vp]
+    lib.he_layer_norm.argtypes = [vp, C.POINTER(_LayerNormDesc), i64p, arr, arr, arr, vp, vp, vp, vp, vp, sz, vp]
+    lib.he_layer_norm_backward.argtypes = [vp, C.POINTER(_LayerNormGradDesc), arr, arr, arr, arr, vp, C.POINTER(u32), keys, vp, vp, vp, vp, sz, vp]
     lib.ckks_prof_kernel_count.restype = u32
     lib.ckks_prof_kernel_name.argtypes = [u32]
     lib.ckks_prof_kernel_name.restype = C.c_char_p
@@ -742,6 +770,164 @@ def he_norm_gate(ctx: Context, level: int, x: torch.Tensor, k_eps: int, k_slope:
     ctx._check(_lib.he_norm_gate(ctx.handle, C.byref(d), kn, C.byref(xa), C.byref(ga) if ga else None, C.byref(ra) if ra else None,
                                  rlk.handle if rlk else None, _ptr(out, _WORDS), _raw_ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
     return out
+
+
+# ------------------------------------------------------------------ a recurrent block's operators
+def _key_handles(keys: Sequence["Key"]):
+    if any(k is None for k in keys):
+        raise ValueError("a key is missing")
+    return (C.c_void_p * max(len(keys), 1))(*[k.handle.value if k.handle is not None else None for k in keys])
+
+
+def _int64(*values) -> List[int]:
+    out = [int(v) for v in values]
+    if any(not -(1 << 63) <= v < 1 << 63 for v in out):
+        raise ValueError("the constants must be 64-bit signed integers")
+    return out
+
+
+def _wanted(ctx: Context, given: Optional[torch.Tensor], *shape) -> torch.Tensor:
+    """An output given or made; its size is the caller's to get right, as the library counts its words from the descriptor."""
+    return _out(ctx, given, *shape) if given is None or min(shape) > 0 else given
+
+
+def _scan_desc(ctx: Context, level: int, channels: int, heads: int, steps: int, reverse: bool = False) -> _ScanDesc:
+    return _ScanDesc(channels, heads, level, steps, int(bool(reverse)))
+
+
+def _scan_args(x: torch.Tensor, gate: torch.Tensor, k: Sequence[int], rot_keys, cross_keys, what: str):
+    if x.dim() != 4 or gate.dim() != 4:
+        raise ValueError(f"need {what} [channels][2][limbs][N] and gate [heads][2][limbs][N]")
+    steps = len(k)
+    if len(rot_keys) != steps or len(cross_keys) != steps:
+        raise ValueError("need a constant, a rotation key and a cross key for every step")
+    return x.shape[0], gate.shape[0], steps, (C.c_int64 * max(steps, 1))(*_int64(*k))
+
+
+def he_scan_workspace_bytes(ctx: Context, level: int, channels: int, heads: int, steps: int) -> int:
+    return int(_lib.he_scan_workspace_bytes(ctx.handle, C.byref(_scan_desc(ctx, level, channels, heads, steps))))
+
+
+def he_scan_gated(ctx: Context, level: int, x: torch.Tensor, gate: torch.Tensor, k: Sequence[int], rot_keys: Sequence[Key], cross_keys: Sequence[Key],
+                  reverse: bool = False, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """h_t = a_t h_{t-1} + x_t over the slots.  x: [channels][2][level+1 or more][N]; gate: [heads][2][level+1 or more][N], zero at every sequence's first token;
+    k: one integer a step (``scan_constants`` in ``block.py``), as many steps as doublings; rot_keys[s], cross_keys[s]: keys of the rotation by -2^s (reverse: +2^s), the
+    latter loaded with CKKS_KEY_CROSS.  Returns [channels][2][level+1-steps][N]."""
+    channels, heads, steps, ks = _scan_args(x, gate, k, rot_keys, cross_keys, "x")
+    d = _scan_desc(ctx, level, channels, heads, steps, reverse)
+    out = _wanted(ctx, out, channels, 2, level + 1 - steps, ctx.N)
+    xa, ga = _ct_array(ctx, x, channels, level + 1, "x"), _ct_array(ctx, gate, heads, level + 1, "gate")
+    ws = ctx.workspace(int(_lib.he_scan_workspace_bytes(ctx.handle, C.byref(d)))) if ws is None else ws
+    ctx._check(_lib.he_scan_gated(ctx.handle, C.byref(d), ks, C.byref(xa), C.byref(ga), _key_handles(rot_keys), _key_handles(cross_keys), _ptr(out, _WORDS), _raw_ptr(ws),
+                                  ws.numel() * ws.element_size(), _stream(stream)))
+    return out
+
+
+def he_scan_backward_workspace_bytes(ctx: Context, level: int, channels: int, heads: int, steps: int) -> int:
+    return int(_lib.he_scan_backward_workspace_bytes(ctx.handle, C.byref(_scan_desc(ctx, level, channels, heads, steps))))
+
+
+def he_scan_gated_backward(ctx: Context, level: int, grad: torch.Tensor, gate: torch.Tensor, states: Optional[torch.Tensor], k: Sequence[int], rot_keys: Sequence[Key],
+                           cross_keys: Sequence[Key], back_rot: Optional[Key] = None, back_cross: Optional[Key] = None, reverse: bool = False, want_gate: bool = True,
+                           dx: Optional[torch.Tensor] = None, dgate: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """The gradients of ``he_scan_gated`` with respect to x and the gates.  grad, gate at ``level``; states: the forward call's outputs, [channels][2][level+1-steps or
+    more][N]; rot_keys[s], cross_keys[s]: keys of the rotations the other way, +2^s (reverse: -2^s), back_rot, back_cross: those of -1 (reverse: +1).
+    want_gate = False: the gates are not learned; states and the last two keys may be None.  Returns (dx [channels][2][level+1-steps][N],
+    dgate [heads][2][level-steps][N] or None)."""
+    channels, heads, steps, ks = _scan_args(grad, gate, k, rot_keys, cross_keys, "grad")
+    d = _scan_desc(ctx, level, channels, heads, steps, reverse)
+    if want_gate and (states is None or back_rot is None or back_cross is None or states.dim() != 4):
+        raise ValueError("the gates' gradient needs states [channels][2][limbs][N] and the keys of the rotation back")
+    dx = _wanted(ctx, dx, channels, 2, level + 1 - steps, ctx.N)
+    dgate = _wanted(ctx, dgate, heads, 2, level - steps, ctx.N) if want_gate else None
+    xa, ga = _ct_array(ctx, grad, channels, level + 1, "grad"), _ct_array(ctx, gate, heads, level + 1, "gate")
+    sa = _ct_array(ctx, states, channels, max(level + 1 - steps, 1), "states") if want_gate else None
+    ws = ctx.workspace(int(_lib.he_scan_backward_workspace_bytes(ctx.handle, C.byref(d)))) if ws is None else ws
+    ctx._check(_lib.he_scan_gated_backward(ctx.handle, C.byref(d), ks, C.byref(xa), C.byref(ga), C.byref(sa) if sa else None, _key_handles(rot_keys), _key_handles(cross_keys),
+                                           back_rot.handle if back_rot else None, back_cross.handle if back_cross else None, _ptr(dx, _WORDS), _ptr(dgate, _WORDS),
+                                           _raw_ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+    return dx, dgate
+
+
+def he_scan_step_workspace_bytes(ctx: Context, level: int, channels: int, heads: int) -> int:
+    return int(_lib.he_scan_step_workspace_bytes(ctx.handle, C.byref(_scan_desc(ctx, level, channels, heads, 1))))
+
+
+def he_scan_step(ctx: Context, level: int, gate: torch.Tensor, state: torch.Tensor, cross_key: Key, rot_key: Optional[Key] = None, x: Optional[torch.Tensor] = None,
+                 k: int = 0, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """One step, the form for single tokens: Rescale(gate (.) Rot(state, r) + k x).  gate: [heads][2][level+1 or more][N]; state, x: [channels][2][level+1 or more][N], x None
+    for no addend.  rot_key None: r = 0 and cross_key is the relinearisation key; otherwise the two keys of the rotation.  Returns [channels][2][level][N]."""
+    if gate.dim() != 4 or state.dim() != 4 or (x is not None and x.dim() != 4):
+        raise ValueError("need gate [heads][2][limbs][N] and state, x [channels][2][limbs][N]")
+    channels, heads = state.shape[0], gate.shape[0]
+    d = _scan_desc(ctx, level, channels, heads, 1)
+    out = _wanted(ctx, out, channels, 2, level, ctx.N)
+    ga, sa = _ct_array(ctx, gate, heads, level + 1, "gate"), _ct_array(ctx, state, channels, level + 1, "state")
+    xa = _ct_array(ctx, x, channels, level + 1, "x") if x is not None else None
+    ws = ctx.workspace(int(_lib.he_scan_step_workspace_bytes(ctx.handle, C.byref(d)))) if ws is None else ws
+    ctx._check(_lib.he_scan_step(ctx.handle, C.byref(d), _int64(k)[0], C.byref(ga), C.byref(sa), C.byref(xa) if xa else None, rot_key.handle if rot_key else None,
+                                 cross_key.handle if cross_key else None, _ptr(out, _WORDS), _raw_ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+    return out
+
+
+def he_layer_norm_workspace_bytes(ctx: Context, level: int, channels: int, iterations: int, affine: bool = False) -> int:
+    return int(_lib.he_layer_norm_workspace_bytes(ctx.handle, C.byref(_LayerNormDesc(channels, level, iterations, int(bool(affine)), 0, 0, 0, 0))))
+
+
+def he_layer_norm(ctx: Context, level: int, x: torch.Tensor, k_eps: int, k_slope: int, k_start: int, k_newton: Sequence[int], rlk: Key, gain: Optional[torch.Tensor] = None,
+                  bias: Optional[torch.Tensor] = None, k_bias: int = 0, norm: Optional[torch.Tensor] = None, inv: Optional[torch.Tensor] = None,
+                  out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """Layer norm over the channels of every slot.  x: [channels][2][level+1 or more][N]; gain, bias: None or ciphertexts [channels][2][m or more][N],
+    m = level-2-2*iterations; the integers as ``layer_norm_constants`` in ``block.py`` gives them.  Returns (norm [channels][2][m][N], inv [2][m+1][N],
+    out [channels][2][m-1][N] or, without a gain, None): norm and inv are what the backward pass takes."""
+    if x.dim() != 4:
+        raise ValueError("need x [channels][2][limbs][N]")
+    if gain is None and (bias is not None or out is not None):
+        raise ValueError("a bias, or an output with gain and bias, needs a gain")
+    channels, its = x.shape[0], len(k_newton)
+    consts = _int64(k_eps, k_slope, k_start, k_bias)
+    kn = (C.c_int64 * max(its, 1))(*_int64(*k_newton))
+    m = level - 2 - 2 * its
+    d = _LayerNormDesc(channels, level, its, int(gain is not None), *consts)
+    norm, inv = _wanted(ctx, norm, channels, 2, m, ctx.N), _wanted(ctx, inv, 2, m + 1, ctx.N)
+    out = _wanted(ctx, out, channels, 2, m - 1, ctx.N) if gain is not None else None
+    xa = _ct_array(ctx, x, channels, level + 1, "x")
+    ga = _ct_array(ctx, gain, channels, max(m, 1), "gain") if gain is not None else None
+    ba = _ct_array(ctx, bias, channels, max(m, 1), "bias") if bias is not None else None
+    ws = ctx.workspace(int(_lib.he_layer_norm_workspace_bytes(ctx.handle, C.byref(d)))) if ws is None else ws
+    ctx._check(_lib.he_layer_norm(ctx.handle, C.byref(d), kn, C.byref(xa), C.byref(ga) if ga else None, C.byref(ba) if ba else None, rlk.handle if rlk else None,
+                                  _ptr(norm, _WORDS), _ptr(inv, _WORDS), _ptr(out, _WORDS), _raw_ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+    return norm, inv, out
+
+
+def he_layer_norm_backward_workspace_bytes(ctx: Context, level: int, channels: int, affine: bool = False, stages: int = 1) -> int:
+    return int(_lib.he_layer_norm_backward_workspace_bytes(ctx.handle, C.byref(_LayerNormGradDesc(channels, level, int(bool(affine)), stages, 0, 0))))
+
+
+def he_layer_norm_backward(ctx: Context, level: int, grad: torch.Tensor, norm: torch.Tensor, inv: torch.Tensor, k_grad: int, k_norm: int, rlk: Key,
+                           gain: Optional[torch.Tensor] = None, sum_keys: Sequence[Sequence[Key]] = (), want_gain: bool = True, want_bias: bool = True,
+                           dx: Optional[torch.Tensor] = None, dgain: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None,
+                           ws: Optional[torch.Tensor] = None, stream=None):
+    """The gradients of ``he_layer_norm``.  grad, norm and gain (None where the forward call had none): [channels][2][level+1 or more][N]; inv: [2][level+1 or more][N] (a
+    limb less is read, two with a gain); sum_keys: for each stage of the sums over slots the keys of its rotations; none: the gradients of gain and bias stay slot by slot.
+    Returns (dx [channels][2][level-2][N], with a gain one limb less, dgain, dbias [channels][2][level][N] each, or None where not wanted)."""
+    if grad.dim() != 4 or norm.dim() != 4 or inv.dim() != 3 or (gain is not None and gain.dim() != 4):
+        raise ValueError("need grad, norm, gain [channels][2][limbs][N] and inv [2][limbs][N]")
+    channels, affine = grad.shape[0], int(gain is not None)
+    stages = [list(row) for row in sum_keys]
+    d = _LayerNormGradDesc(channels, level, affine, len(stages), *_int64(k_grad, k_norm))
+    dx = _wanted(ctx, dx, channels, 2, level - 2 - affine, ctx.N)
+    dgain = _wanted(ctx, dgain, channels, 2, level, ctx.N) if want_gain else None
+    dbias = _wanted(ctx, dbias, channels, 2, level, ctx.N) if want_bias else None
+    da, na = _ct_array(ctx, grad, channels, level + 1, "grad"), _ct_array(ctx, norm, channels, level + 1, "norm")
+    ia = _ct_array(ctx, inv, 1, max(level - affine, 1), "inv")
+    ga = _ct_array(ctx, gain, channels, level + 1, "gain") if affine else None
+    ws = ctx.workspace(int(_lib.he_layer_norm_backward_workspace_bytes(ctx.handle, C.byref(d)))) if ws is None else ws
+    rots = (C.c_uint32 * max(len(stages), 1))(*[len(row) for row in stages])
+    ctx._check(_lib.he_layer_norm_backward(ctx.handle, C.byref(d), C.byref(da), C.byref(na), C.byref(ia), C.byref(ga) if ga else None, rlk.handle if rlk else None, rots,
+                                           _key_handles([key for row in stages for key in row]), _ptr(dx, _WORDS), _ptr(dgain, _WORDS), _ptr(dbias, _WORDS), _raw_ptr(ws),
+                                           ws.numel() * ws.element_size(), _stream(stream)))
+    return dx, dgain, dbias
 
 
 def ckks_prof_kernel_names() -> List[str]:

@@ -1,5 +1,6 @@
-"""Host-side constants of a transformer block's operators (``he_linear_grouped``, ``he_rope_axes``, ``he_norm_gate``): integers and
-angles that a program computes once, with the scales it has to track.  Nothing here touches ciphertexts or the GPU."""
+"""Host-side constants of a transformer block's operators (``he_linear_grouped``, ``he_rope_axes``, ``he_norm_gate``) and of a recurrent
+block's (``he_scan_gated``, ``he_layer_norm`` and their backward passes): integers and angles that a program computes once, with the
+scales it has to track.  Nothing here touches ciphertexts or the GPU."""
 from __future__ import annotations
 
 import math
@@ -87,21 +88,23 @@ class NormConstants(NamedTuple):
     relative_error: float    # of 1 / sqrt after the last iteration, at most, for mean squares inside the interval
 
 
-def norm_constants(moduli: Sequence[int], level: int, channels: int, scale: float, interval: Tuple[float, float], iterations: int, eps: float = 0.0,
-                   gate_scale: Optional[float] = None, residual: Optional[Tuple[float, float]] = None) -> NormConstants:
-    """The integers of ``he_norm_gate`` for inputs at ``scale`` (close to the moduli: the mean square has the scale channels * scale^2 /
-    q_level) whose mean squares plus eps lie in ``interval``; gate_scale: the gate's scale; residual: (factor, scale) of the residual.
+class _InverseRoot(NamedTuple):
+    k_eps: int
+    k_slope: int
+    k_start: int
+    k_newton: Tuple[int, ...]
+    level: int
+    scale: float
+    relative_error: float
 
-    The first guess is the line a (1 - b v) whose error against 1 / sqrt(v) is the same at both ends and in the middle; a Newton step turns
-    r sqrt(v) = 1 + e into 1 - (3 + e) e^2 / 2, so the first step's worst error is at e > 0 and all later ones come from below.  The scale of r is the one that a step leaves as it is: twice the scale of
-    u * w, r^2 and s r each divided by one modulus, the product by another."""
+
+def _inverse_root(q: Sequence[float], level: int, s_scale: float, interval: Tuple[float, float], iterations: int, eps: float) -> _InverseRoot:
+    """The guess and the Newton steps of 1 / sqrt(v) for v at ``s_scale``, level - 1 (see ``norm_constants``)."""
     lo, hi = interval
     if not 0 < lo < hi:
         raise ValueError("need 0 < lo < hi")
     if iterations < 0 or level < 3 + 2 * iterations:
         raise ValueError("need level >= 3 + 2 * iterations")
-    q = [float(int(m)) for m in moduli]
-    s_scale = channels * scale * scale / q[level]
     sign = -1 if iterations % 2 else 1
     # the line
     b = (math.sqrt(hi) - math.sqrt(lo)) / (hi ** 1.5 - lo ** 1.5)
@@ -118,9 +121,131 @@ def norm_constants(moduli: Sequence[int], level: int, channels: int, scale: floa
         newton.append(round(-1.5 * product / r_scale))
         r_scale = product / q[m - 1]
         m -= 2
+    return _InverseRoot(k_eps, k_slope, k_start, tuple(newton), m, r_scale, error)
+
+
+def _check_int64(*values: int) -> None:
+    if any(not -(1 << 63) < k < 1 << 63 for k in values):
+        raise ValueError("a constant passes 63 bits: the inputs' scale is too far from the moduli")
+
+
+def norm_constants(moduli: Sequence[int], level: int, channels: int, scale: float, interval: Tuple[float, float], iterations: int, eps: float = 0.0,
+                   gate_scale: Optional[float] = None, residual: Optional[Tuple[float, float]] = None) -> NormConstants:
+    """The integers of ``he_norm_gate`` for inputs at ``scale`` (close to the moduli: the mean square has the scale channels * scale^2 /
+    q_level) whose mean squares plus eps lie in ``interval``; gate_scale: the gate's scale; residual: (factor, scale) of the residual.
+
+    The first guess is the line a (1 - b v) whose error against 1 / sqrt(v) is the same at both ends and in the middle; a Newton step turns
+    r sqrt(v) = 1 + e into 1 - (3 + e) e^2 / 2, so the first step's worst error is at e > 0 and all later ones come from below.  The scale of r is the one that a step leaves as it is: twice the scale of
+    u * w, r^2 and s r each divided by one modulus, the product by another."""
+    q = [float(int(m)) for m in moduli]
+    r = _inverse_root(q, level, channels * scale * scale / q[level], interval, iterations, eps)
     t_scale = scale if gate_scale is None else scale * gate_scale / q[level]
-    k_residual = round(residual[0] * t_scale * r_scale / residual[1]) if residual else 0
-    for k in (k_eps, k_slope, k_start, k_residual, *newton):
-        if abs(k) >= 1 << 63:
-            raise ValueError("a constant passes 63 bits: the inputs' scale is too far from the moduli")
-    return NormConstants(k_eps, k_slope, k_start, tuple(newton), k_residual, m - 1, t_scale * r_scale / q[m], error)
+    k_residual = round(residual[0] * t_scale * r.scale / residual[1]) if residual else 0
+    _check_int64(r.k_eps, r.k_slope, r.k_start, k_residual, *r.k_newton)
+    return NormConstants(r.k_eps, r.k_slope, r.k_start, r.k_newton, k_residual, r.level - 1, t_scale * r.scale / q[r.level], r.relative_error)
+
+
+# ------------------------------------------------------------------------------------------ layer norm
+class LayerNormConstants(NamedTuple):
+    k_eps: int
+    k_slope: int
+    k_start: int
+    k_newton: Tuple[int, ...]
+    k_bias: int
+    norm_level: int          # of the normalised channels; inv is one level above, the output with gain and bias one below
+    norm_scale: float
+    inv_scale: float
+    out_scale: float         # with a gain; norm_scale without
+    relative_error: float    # of 1 / sqrt after the last iteration, at most, for variances inside the interval
+
+
+def layer_norm_constants(moduli: Sequence[int], level: int, channels: int, scale: float, interval: Tuple[float, float], iterations: int, eps: float = 0.0,
+                         gain_scale: Optional[float] = None, bias_scale: Optional[float] = None) -> LayerNormConstants:
+    """The integers of ``he_layer_norm`` for inputs at ``scale`` whose variances over the channels plus eps lie in ``interval``: what the Newton chain works on is channels^2
+    times the variance, at the scale channels^2 scale^2 / q_level; the centred channels have channels times the inputs' scale."""
+    q = [float(int(m)) for m in moduli]
+    if gain_scale is not None and level < 4 + 2 * iterations:
+        raise ValueError("a gain needs one more level")
+    r = _inverse_root(q, level, channels * channels * scale * scale / q[level], interval, iterations, eps)
+    norm_scale, m = channels * scale * r.scale / q[r.level], r.level - 1
+    k_bias = round(gain_scale * norm_scale / bias_scale) if gain_scale is not None and bias_scale is not None else 0
+    _check_int64(r.k_eps, r.k_slope, r.k_start, k_bias, *r.k_newton)
+    return LayerNormConstants(r.k_eps, r.k_slope, r.k_start, r.k_newton, k_bias, m, norm_scale, r.scale, norm_scale if gain_scale is None else gain_scale * norm_scale / q[m],
+                              r.relative_error)
+
+
+class LayerNormGradConstants(NamedTuple):
+    k_grad: int
+    k_norm: int
+    dx_level: int
+    dx_scale: float
+    dgain_scale: float       # dgain and dbias are at level - 1
+    dbias_scale: float
+
+
+def layer_norm_grad_constants(moduli: Sequence[int], level: int, channels: int, grad_scale: float, norm_scale: float, inv_scale: float, gain_scale: Optional[float] = None,
+                              bits: int = 16) -> LayerNormGradConstants:
+    """The integers of ``he_layer_norm_backward`` for a gradient at ``grad_scale``: k_norm / k_grad is minus the ratio of the scales of the two terms of
+    channels * dx, to within 2^-(bits + 1), as both are at least 2^bits; dx's scale holds the factors channels and k_grad."""
+    q = [float(int(m)) for m in moduli]
+    if level < (3 if gain_scale is None else 4):
+        raise ValueError("need level >= 3, 4 with a gain")
+    b = level if gain_scale is None else level - 1
+    g_scale = grad_scale if gain_scale is None else gain_scale * grad_scale / q[level]
+    t_scale = inv_scale * (g_scale * norm_scale / q[b]) / q[b - 1]
+    ratio = inv_scale * g_scale / (t_scale * norm_scale)
+    k_grad = max(1, math.ceil(2.0 ** bits * max(1.0, 1.0 / ratio)))
+    k_norm = -round(k_grad * ratio)
+    _check_int64(k_grad, k_norm)
+    return LayerNormGradConstants(k_grad, k_norm, b - 3, channels * k_grad * inv_scale * g_scale / q[b - 2], grad_scale * norm_scale / q[level], grad_scale)
+
+
+# ------------------------------------------------------------------------------------------ gated recurrence
+class ScanConstants(NamedTuple):
+    k: Tuple[int, ...]       # one integer a step
+    out_level: int
+    out_scale: float
+
+
+def scan_steps(longest: int) -> int:
+    """Doublings of a scan over sequences of at most ``longest`` tokens (one at least: the call has no scan without a step)."""
+    if longest < 1:
+        raise ValueError("a sequence has at least one token")
+    return max(1, (longest - 1).bit_length())
+
+
+def scan_gate_mask(lengths: Sequence[int], slots: int, reverse: bool = False) -> np.ndarray:
+    """[slots]: 0 where a gate has to be zero, the first token (reverse: the last) of every sequence and the padding behind the last one; 1 elsewhere."""
+    lengths = [int(n) for n in lengths]
+    if any(n < 0 for n in lengths) or sum(lengths) > slots:
+        raise ValueError("the sequences do not fit the slots")
+    mask, start = np.zeros(slots), 0
+    for n in lengths:
+        if reverse:
+            mask[start:start + max(n - 1, 0)] = 1.0
+        else:
+            mask[start + 1:start + n] = 1.0
+        start += n
+    return mask
+
+
+def scan_constants(moduli: Sequence[int], level: int, scale: float, gate_scale: float, steps: int) -> ScanConstants:
+    """The integers of ``he_scan_gated`` (and of its backward pass) for inputs at ``scale`` and gates at ``gate_scale``: at every step the gates' scale, rounded, as what is
+    carried on has to join a product with them.  Scales stay where gate_scale is close to the moduli."""
+    if not 1 <= steps <= level:
+        raise ValueError("need 1 <= steps <= level")
+    q, k = [float(int(m)) for m in moduli], []
+    for s in range(steps):
+        k.append(round(gate_scale))
+        scale, gate_scale = scale * gate_scale / q[level - s], gate_scale * gate_scale / q[level - s]
+    _check_int64(*k)
+    if min(k) < 1:
+        raise ValueError("the gates' scale falls below one")
+    return ScanConstants(tuple(k), level - steps, scale)
+
+
+def step_constant(moduli: Sequence[int], level: int, gate_scale: float, state_scale: float, x_scale: float) -> Tuple[int, float]:
+    """The integer of ``he_scan_step`` and the scale of its outputs."""
+    k = round(gate_scale * state_scale / x_scale)
+    _check_int64(k)
+    return k, gate_scale * state_scale / float(int(moduli[level]))

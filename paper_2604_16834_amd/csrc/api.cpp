@@ -1217,7 +1217,8 @@ int ckks_key_load(const ckks_ctx* c, const uint64_t* d_key, uint32_t galois_elt,
     if (!c) return CKKS_ERR_INVALID_ARG;
     if (!d_key || !out) return set_err(c, CKKS_ERR_INVALID_ARG, "null pointer");
     if (!c->dnum) return set_err(c, CKKS_ERR_UNSUPPORTED_PARAMS, "context has no key-switching digits");
-    if (galois_elt != 0 && ((galois_elt & 1) == 0 || galois_elt >= 2 * c->N)) return set_err(c, CKKS_ERR_INVALID_ARG, "Galois element must be odd and below 2N");
+    const u32 g = galois_elt & ~CKKS_KEY_CROSS;
+    if (galois_elt != 0 && ((g & 1) == 0 || g >= 2 * c->N)) return set_err(c, CKKS_ERR_INVALID_ARG, "Galois element must be odd and below 2N");
     ckks_key* k = new (std::nothrow) ckks_key;
     if (!k) return set_err(c, CKKS_ERR_INVALID_ARG, "out of host memory");
     k->d_key = (const u64*)d_key;
@@ -2291,6 +2292,73 @@ int he_rope_axes(const ckks_ctx* c, const he_rope_desc* d, const he_ct_array* in
     return CKKS_OK;
 }
 
+// k times q_lv: a constant k joins a quotient by B exactly as B k joins the dividend (it vanishes modulo every dropped limb), and the addends of the inner product
+// are multiplied by P already
+static LimbScalars times_limb(const ckks_ctx* c, int64_t k, u32 lv) {
+    LimbScalars v = limb_scalars(c, lv, k);
+    for (u32 i = 0; i <= lv; i++) v.v[i] = (u64)((unsigned __int128)v.v[i] * (c->mod[lv] % c->mod[i]) % c->mod[i]);
+    return v;
+}
+// The norms' inverse square root: s from the tensor product sq3 of `level` ([3][level + 1][N], the constant in it already), the linear first guess, Newton's iterations.
+// s, u, w [2][level][N]; ra, rb [2][level + 1][N] (swapped: the result is in ra).  Scratch: ws_inverse_root.
+static size_t ws_inverse_root(const ckks_ctx* c, u32 level, u32 iterations) {
+    const size_t N = c->N, L1 = level + 1;
+    size_t sub = ws_ks(c, level, 1, 1), t;
+    if ((t = ws_rescale(c, level - 1, 1)) > sub) sub = t;
+    if (iterations && (t = ws_ctct(c, level - 2, ntt_has_modup(c) ? 2 : 1) + (ntt_has_modup(c) ? 0 : blk(2 * L1 * N))) > sub) sub = t;
+    return sub;
+}
+static int run_inverse_root(const ckks_ctx* c, u32 level, u32 iterations, int64_t k_slope, int64_t k_start, const int64_t* h_k_newton, const u64* d_rlk, const u64* sq3, u64* s,
+                            u64* u, u64* w, u64*& ra, u64*& rb, Arena ar, hipStream_t st) {
+    const bool mac = ntt_has_modup(c);
+    const size_t N = c->N, L1 = level + 1;
+    int rc;
+    {
+        KsWs ws;
+        Arena sub = ar;
+        if (!carve_ks(c, level, 1, 1, sub, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
+        const u64 *d0 = sq3, *d1 = sq3 + L1 * N, *d2 = sq3 + 2 * L1 * N;
+        u64* v = ws.v;
+        if ((rc = run_modup(c, level, &d2, 1, ws, st))) return rc;
+        HIP_TRY(launch_key_inner_ext(c, level, dsrc(c, ws, 0), d_rlk, 1, &d0, &d1, nullptr, &v, 1, st));
+        const FinalItem item = {nullptr, nullptr, nullptr, s, 1, 0, nullptr};
+        if ((rc = run_moddown(c, level, ws, 1, &item, st, true))) return rc;
+    }
+    // the first guess
+    const size_t ss = (size_t)level * N;  // component stride of s
+    HIP_TRY(launch_affine(c, level - 1, s, ss, limb_scalars(c, level - 1, k_slope), times_limb(c, k_start, level - 1), rb, st));
+    const u64* prb = rb;
+    if ((rc = run_rescale(c, level - 1, &prb, ss, &ra, 1, ar, st))) return rc;
+    // r at level m
+    u32 m = level - 2;
+    for (u32 it = 0; it < iterations; it++, m -= 2) {
+        const size_t rs = (size_t)(m + 1) * N, us = (size_t)m * N;
+        const u64 *pr = ra, *ps = s, *pu = u, *pw = w;
+        Arena sub = ar;
+        if (mac) {  // r r and r s side by side
+            const u64 *pa[2] = {ra, ra}, *pb0[2] = {ra, s}, *pb1[2] = {ra + rs, s + ss};
+            u64* po[2] = {u, w};
+            KsWs ws;
+            if (!carve_ks(c, m, 2, 2, sub, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
+            if ((rc = run_product(c, m, pa, rs, pb0, pb1, d_rlk, po, 2, ws, st, true))) return rc;
+            const LimbScalars kn = limb_scalars(c, m - 1, h_k_newton[it]), zero = limb_scalars(c, m - 1, 0);
+            const LinAddend lin = {&pr, rs, kn.v, &pr, rs, zero.v};
+            if ((rc = run_ctct_merged(c, m - 1, &pu, us, &pw, us, nullptr, 0, d_rlk, &rb, 1, ar, st, &lin))) return rc;
+        } else {
+            u64* add = sub.take(2 * us);
+            if (!sub.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
+            if ((rc = run_ctct_merged(c, m, &pr, rs, &pr, rs, nullptr, 0, d_rlk, &u, 1, sub.rest(), st))) return rc;
+            if ((rc = run_ctct_merged(c, m, &pr, rs, &ps, ss, nullptr, 0, d_rlk, &w, 1, sub.rest(), st))) return rc;
+            HIP_TRY(launch_affine(c, m - 1, ra, rs, limb_scalars(c, m - 1, h_k_newton[it]), limb_scalars(c, m - 1, 0), add, st));
+            if ((rc = run_ctct_merged(c, m - 1, &pu, us, &pw, us, add, 0, d_rlk, &rb, 1, sub.rest(), st))) return rc;
+        }
+        u64* other = ra;
+        ra = rb;
+        rb = other;
+    }
+    return CKKS_OK;
+}
+
 static int norm_check(const ckks_ctx* c, const he_norm_desc* d) {
     if (!d) return set_err(c, CKKS_ERR_INVALID_ARG, "null descriptor");
     if (d->channels == 0 || d->channels > 65536) return set_err(c, CKKS_ERR_INVALID_ARG, "channels out of range (1 to 65536)");
@@ -2337,9 +2405,7 @@ static size_t ws_norm_lane(const ckks_ctx* c, const he_norm_desc* d) {
 }
 static size_t ws_norm(const ckks_ctx* c, const he_norm_desc* d, bool two) {
     const size_t N = c->N, L1 = d->level + 1, lane = ws_norm_lane(c, d);
-    size_t sub = ws_ks(c, d->level, 1, 1), t;  // the chain's
-    if ((t = ws_rescale(c, d->level - 1, 1)) > sub) sub = t;
-    if (d->iterations && (t = ws_ctct(c, d->level - 2, ntt_has_modup(c) ? 2 : 1) + (ntt_has_modup(c) ? 0 : blk(2 * L1 * N))) > sub) sub = t;
+    size_t sub = ws_inverse_root(c, d->level, d->iterations);  // the chain's
     if (lane > sub) sub = lane;
     return blk(3 * L1 * N) + 2 * blk(2 * L1 * N) + 3 * blk(2 * N * d->level) + (d->gate ? blk((size_t)norm_chunk(c, d) * 2 * norm_gated_limbs(c, d) * N) : 0) + sub +
            (two ? lane : 0);
@@ -2420,59 +2486,8 @@ int he_norm_gate(const ckks_ctx* c, const he_norm_desc* d, const int64_t* h_k_ne
     };
     // s and Newton's iterations
     auto run_chain = [&]() -> int {
-        int rc;
-        // a constant k joins a quotient by B exactly as B k joins the dividend (it vanishes modulo every dropped limb), and the addends of the
-        // inner product are multiplied by P already
-        auto times_limb = [&](int64_t k, u32 lv) {
-            LimbScalars v = limb_scalars(c, lv, k);
-            for (u32 i = 0; i <= lv; i++) v.v[i] = (u64)((unsigned __int128)v.v[i] * (c->mod[lv] % c->mod[i]) % c->mod[i]);
-            return v;
-        };
-        HIP_TRY(launch_square_sum(c, level, (const u64*)x->d, x->ct_stride, x->comp_stride, d->channels, times_limb(d->k_eps, level), sq3, st));
-        {
-            KsWs ws;
-            Arena sub = ar.rest();
-            if (!carve_ks(c, level, 1, 1, sub, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
-            const u64 *d0 = sq3, *d1 = sq3 + L1 * N, *d2 = sq3 + 2 * L1 * N;
-            u64* v = ws.v;
-            if ((rc = run_modup(c, level, &d2, 1, ws, st))) return rc;
-            HIP_TRY(launch_key_inner_ext(c, level, dsrc(c, ws, 0), rlk->d_key, 1, &d0, &d1, nullptr, &v, 1, st));
-            const FinalItem item = {nullptr, nullptr, nullptr, s, 1, 0, nullptr};
-            if ((rc = run_moddown(c, level, ws, 1, &item, st, true))) return rc;
-        }
-        // the first guess
-        const size_t ss = (size_t)level * N;  // component stride of s
-        HIP_TRY(launch_affine(c, level - 1, s, ss, limb_scalars(c, level - 1, d->k_slope), times_limb(d->k_start, level - 1), rb, st));
-        const u64* prb = rb;
-        if ((rc = run_rescale(c, level - 1, &prb, ss, &ra, 1, ar.rest(), st))) return rc;
-        // r at level m
-        u32 m = level - 2;
-        for (u32 it = 0; it < d->iterations; it++, m -= 2) {
-            const size_t rs = (size_t)(m + 1) * N, us = (size_t)m * N;
-            const u64 *pr = ra, *ps = s, *pu = u, *pw = w;
-            Arena sub = ar.rest();
-            if (mac) {  // r r and r s side by side
-                const u64 *pa[2] = {ra, ra}, *pb0[2] = {ra, s}, *pb1[2] = {ra + rs, s + ss};
-                u64* po[2] = {u, w};
-                KsWs ws;
-                if (!carve_ks(c, m, 2, 2, sub, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
-                if ((rc = run_product(c, m, pa, rs, pb0, pb1, rlk->d_key, po, 2, ws, st, true))) return rc;
-                const LimbScalars kn = limb_scalars(c, m - 1, h_k_newton[it]), zero = limb_scalars(c, m - 1, 0);
-                const LinAddend lin = {&pr, rs, kn.v, &pr, rs, zero.v};
-                if ((rc = run_ctct_merged(c, m - 1, &pu, us, &pw, us, nullptr, 0, rlk->d_key, &rb, 1, ar.rest(), st, &lin))) return rc;
-            } else {
-                u64* add = sub.take(2 * us);
-                if (!sub.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
-                if ((rc = run_ctct_merged(c, m, &pr, rs, &pr, rs, nullptr, 0, rlk->d_key, &u, 1, sub.rest(), st))) return rc;
-                if ((rc = run_ctct_merged(c, m, &pr, rs, &ps, ss, nullptr, 0, rlk->d_key, &w, 1, sub.rest(), st))) return rc;
-                HIP_TRY(launch_affine(c, m - 1, ra, rs, limb_scalars(c, m - 1, h_k_newton[it]), limb_scalars(c, m - 1, 0), add, st));
-                if ((rc = run_ctct_merged(c, m - 1, &pu, us, &pw, us, add, 0, rlk->d_key, &rb, 1, sub.rest(), st))) return rc;
-            }
-            u64* other = ra;
-            ra = rb;
-            rb = other;
-        }
-        return CKKS_OK;
+        HIP_TRY(launch_square_sum(c, level, (const u64*)x->d, x->ct_stride, x->comp_stride, d->channels, times_limb(c, d->k_eps, level), sq3, st));
+        return run_inverse_root(c, level, d->iterations, d->k_slope, d->k_start, h_k_newton, rlk->d_key, sq3, s, u, w, ra, rb, ar.rest(), st);
     };
     // the last products
     const size_t rs = (size_t)(last + 1) * N, out_ct = (size_t)2 * last * N;
@@ -2533,6 +2548,533 @@ int he_norm_gate(const ckks_ctx* c, const he_norm_desc* d, const int64_t* h_k_ne
             rc = run_last(c0, i0, end - i0 < nb ? end - i0 : nb, turns && (no & 1) ? aside : ar.rest(), turns && (no & 1) ? c->side : st);
         if (turns) rc = join(rc);
         if (rc) return rc;
+    }
+    return CKKS_OK;
+}
+
+// ---- a recurrent block's operators -----------------------------------------------------------------------
+// n products with a rotated operand, outs[b] = Rescale(a[b] (.) sigma_g(h[b]) + k x[b]) (x: null, or one addend each), level -> level - 1: two key switches, of a0 sigma(h1)
+// and of a1 sigma(h1), that share one division.  n <= turned_batch.
+static u32 turned_batch(const ckks_ctx* c) { return ks_batch(c) / 2; }
+static size_t ws_turned(const ckks_ctx* c, u32 level, u32 n) { return blk(4 * (size_t)n * (level + 1) * c->N) + ws_ks(c, level, 2 * n, 2 * n); }
+// terms [4][n][level + 1][N]: what launch_turned_terms gives
+static int run_turned_terms(const ckks_ctx* c, u32 level, u32 n, const u64* terms, const u64* d_rot, const u64* d_cross, u64* const* outs, Arena ar, hipStream_t st) {
+    const size_t poly = (size_t)(level + 1) * c->N;
+    KsWs ws;
+    if (!carve_ks(c, level, 2 * n, 2 * n, ar, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for products with rotated operands");
+    const u64 *polys[KS_MAX_BATCH], *add0[KS_MAX_BATCH], *add1[KS_MAX_BATCH];
+    u64* vs[KS_MAX_BATCH];
+    FinalItem items[KS_MAX_BATCH];
+    for (u32 b = 0; b < 2 * n; b++) {
+        polys[b] = terms + (2 * n + b) * poly;  // u of every item, then v of every item
+        vs[b] = ws.v + b * ws.v_b;
+    }
+    for (u32 b = 0; b < n; b++) {
+        add0[b] = terms + b * poly;
+        add1[b] = terms + (n + b) * poly;
+        items[b] = FinalItem{nullptr, nullptr, nullptr, outs[b], 1, 0, nullptr};
+    }
+    if (int rc = run_modup(c, level, polys, 2 * n, ws, st)) return rc;
+    HIP_TRY(launch_key_inner_ext(c, level, dsrc(c, ws, 0), d_rot, 1, add0, add1, nullptr, vs, n, st));
+    HIP_TRY(launch_key_inner_ext(c, level, dsrc(c, ws, n), d_cross, 1, nullptr, nullptr, nullptr, vs + n, n, st));
+    HIP_TRY(launch_add_ext(c, level, ws.v, ws.v + n * ws.v_b, 2 * n, st));
+    return run_moddown(c, level, ws, n, items, st, true);
+}
+static int run_turned(const ckks_ctx* c, u32 level, u32 n, const u64* const* a, size_t a_comp, const u64* const* h, size_t h_comp, u32 g, int64_t k, const u64* const* x, size_t x_comp,
+                      const u64* d_rot, const u64* d_cross, u64* const* outs, Arena ar, hipStream_t st) {
+    u64* terms = ar.take(4 * (size_t)n * (level + 1) * c->N);
+    if (!ar.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for products with rotated operands");
+    const u64* none[KS_MAX_BATCH] = {};
+    HIP_TRY(launch_turned_terms(c, level, ptr_list(a, n), a_comp, ptr_list(h, n), h_comp, ptr_list(x ? x : none, n), x_comp, limb_scalars(c, level, k), g, terms, n, st));
+    return run_turned_terms(c, level, n, terms, d_rot, d_cross, outs, ar.rest(), st);
+}
+
+static int scan_check(const ckks_ctx* c, const he_scan_desc* d, u32 deeper) {
+    if (!d) return set_err(c, CKKS_ERR_INVALID_ARG, "null descriptor");
+    if (d->channels == 0 || d->channels > 65536 || d->heads == 0 || d->channels % d->heads) return set_err(c, CKKS_ERR_INVALID_ARG, "need 1 to 65536 channels, a multiple of the heads");
+    if (!c->dnum) return set_err(c, CKKS_ERR_UNSUPPORTED_PARAMS, "context has no key-switching digits");
+    if (!level_ok(c, d->level)) return set_err(c, CKKS_ERR_LEVEL_MISMATCH, "level out of range");
+    if (d->steps == 0 || d->steps >= 32 || (1ull << d->steps) > c->N / 2) return set_err(c, CKKS_ERR_INVALID_ARG, "a scan needs at least one step and at most N/2 slots");
+    if (d->steps + deeper > d->level) return set_err(c, CKKS_ERR_LEVEL_MISMATCH, "a scan needs a level for every step");
+    return CKKS_OK;
+}
+static u32 scan_element(const ckks_ctx* c, const he_scan_desc* d, u32 s, bool forward) {
+    return ckks_galois_element(c, (forward == !d->reverse ? -1 : 1) * (int32_t)(1u << s));
+}
+static int check_turn_keys(const ckks_ctx* c, const ckks_key* rot, const ckks_key* cross, u32 g) {
+    if (!rot || !cross) return set_err(c, CKKS_ERR_NO_KEY, "a rotation's key or its cross key is missing");
+    if (rot->galois_elt != g || cross->galois_elt != (CKKS_KEY_CROSS | g)) return set_err(c, CKKS_ERR_NO_KEY, "a rotation's key or its cross key was made for another offset");
+    return CKKS_OK;
+}
+static u32 even_batch(u32 n, u32 most) { return (n + (n + most - 1) / most - 1) / ((n + most - 1) / most); }
+
+// the rows that a scan turns, gates before channels, in two buffers in turn
+static size_t scan_rows(const ckks_ctx* c, const he_scan_desc* d) { return ((size_t)d->heads + d->channels) * 2 * d->level * c->N; }
+// most rows of a step that go together: the last step has no gates, and its batches may be larger for it
+static u32 scan_batch(const ckks_ctx* c, const he_scan_desc* d) {
+    const u32 all = even_batch(d->heads + d->channels, turned_batch(c)), last = even_batch(d->channels, turned_batch(c));
+    return all > last ? all : last;
+}
+static size_t ws_scan(const ckks_ctx* c, const he_scan_desc* d) {
+    return (d->steps > 1 ? blk(scan_rows(c, d)) : 0) + (d->steps > 2 ? blk(scan_rows(c, d)) : 0) + ws_turned(c, d->level, scan_batch(c, d));
+}
+static int run_scan(const ckks_ctx* c, const he_scan_desc* d, bool forward, const int64_t* h_k, const he_ct_array& x, const he_ct_array& gate, const ckks_key* const* rot_keys,
+                    const ckks_key* const* cross_keys, u64* d_out, Arena ar, hipStream_t st) {
+    const size_t N = c->N;
+    const u32 per = d->channels / d->heads;
+    u64* buf[2] = {d->steps > 1 ? ar.take(scan_rows(c, d)) : nullptr, d->steps > 2 ? ar.take(scan_rows(c, d)) : nullptr};
+    if (!ar.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the scan");
+    he_ct_array hs = x, as = gate;
+    for (u32 s = 0; s < d->steps; s++) {
+        const u32 level = d->level - s, first = s + 1 < d->steps ? 0 : d->heads, rows = d->heads + d->channels;  // (nothing follows that would read the last step's gates)
+        const u32 nb = even_batch(rows - first, turned_batch(c)), g = scan_element(c, d, s, forward);
+        const size_t ct = (size_t)2 * level * N;  // of the step's results
+        u64* next = s + 1 < d->steps ? buf[s & 1] : d_out;  // from row `first` on
+        for (u32 r0 = first; r0 < rows; r0 += nb) {
+            const u32 n = rows - r0 < nb ? rows - r0 : nb;
+            const u64 *pa[KS_MAX_BATCH], *ph[KS_MAX_BATCH], *px[KS_MAX_BATCH];
+            u64* po[KS_MAX_BATCH];
+            // gates and channels of one batch differ in their strides while they are the caller's: components are then a batch's own
+            u32 m = n;
+            if (r0 < d->heads && r0 + n > d->heads && as.comp_stride != hs.comp_stride) m = d->heads - r0;
+            for (u32 done = 0; done < n; done += m, m = n - done) {
+                for (u32 b = 0; b < m; b++) {
+                    const u32 row = r0 + done + b, ch = row - d->heads;
+                    const bool is_gate = row < d->heads;
+                    pa[b] = (const u64*)as.d + (size_t)(is_gate ? row : ch / per) * as.ct_stride;
+                    ph[b] = is_gate ? pa[b] : (const u64*)hs.d + (size_t)ch * hs.ct_stride;
+                    px[b] = is_gate ? nullptr : ph[b];
+                    po[b] = next + (size_t)(row - first) * ct;
+                }
+                const size_t h_comp = r0 + done < d->heads ? as.comp_stride : hs.comp_stride;
+                if (int rc = run_turned(c, level, m, pa, as.comp_stride, ph, h_comp, g, h_k[s], px, h_comp, rot_keys[s]->d_key, cross_keys[s]->d_key, po, ar.rest(), st)) return rc;
+            }
+        }
+        as = he_ct_array{(const uint64_t*)next, ct, (size_t)level * N};
+        hs = he_ct_array{(const uint64_t*)(next + d->heads * ct), ct, (size_t)level * N};
+    }
+    return CKKS_OK;
+}
+
+size_t he_scan_workspace_bytes(const ckks_ctx* c, const he_scan_desc* d) {
+    if (!c || scan_check(c, d, 0)) return 0;
+    return ws_scan(c, d);
+}
+static int check_scan_keys(const ckks_ctx* c, const he_scan_desc* d, bool forward, const ckks_key* const* rot_keys, const ckks_key* const* cross_keys) {
+    if (!rot_keys || !cross_keys) return set_err(c, CKKS_ERR_NO_KEY, "no keys");
+    for (u32 s = 0; s < d->steps; s++)
+        if (int rc = check_turn_keys(c, rot_keys[s], cross_keys[s], scan_element(c, d, s, forward))) return rc;
+    return CKKS_OK;
+}
+int he_scan_gated(const ckks_ctx* c, const he_scan_desc* d, const int64_t* h_k, const he_ct_array* x, const he_ct_array* gate, const ckks_key* const* rot_keys,
+                  const ckks_key* const* cross_keys, uint64_t* d_out, void* d_ws, size_t ws_bytes, void* stream) {
+    if (!c) return CKKS_ERR_INVALID_ARG;
+    if (int rc = scan_check(c, d, 0)) return rc;
+    if (!d_out || !h_k) return set_err(c, CKKS_ERR_INVALID_ARG, "null pointer");
+    if ((uintptr_t)d_out & 15) return set_err(c, CKKS_ERR_INVALID_ARG, "output not aligned to 16 bytes");
+    if (int rc = check_scan_keys(c, d, true, rot_keys, cross_keys)) return rc;
+    if (int rc = check_array(c, x, d->channels, d->level + 1, 2)) return rc;
+    if (int rc = check_array(c, gate, d->heads, d->level + 1, 2)) return rc;
+    if (!d_ws || ws_bytes < ws_scan(c, d)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the scan");
+    return run_scan(c, d, true, h_k, *x, *gate, rot_keys, cross_keys, (u64*)d_out, Arena(d_ws, ws_bytes), (hipStream_t)stream);
+}
+
+static u32 scan_gates_batch(const ckks_ctx* c, const he_scan_desc* d) { return even_batch(d->heads, turned_batch(c)); }
+static size_t ws_scan_backward(const ckks_ctx* c, const he_scan_desc* d) {
+    const size_t N = c->N, L1 = d->level + 1, last = d->level - d->steps;
+    const u32 ng = scan_gates_batch(c, d);
+    size_t sub = blk((size_t)ng * 2 * L1 * N) + ws_rotate_unhoisted(c, d->level, ng), t;
+    if ((t = ws_scan(c, d)) > sub) sub = t;
+    if (last && (t = ws_turned(c, (u32)last, ng)) > sub) sub = t;
+    return blk((size_t)d->heads * 2 * L1 * N) + sub;
+}
+size_t he_scan_backward_workspace_bytes(const ckks_ctx* c, const he_scan_desc* d) {
+    if (!c || scan_check(c, d, 0)) return 0;
+    return ws_scan_backward(c, d);
+}
+int he_scan_gated_backward(const ckks_ctx* c, const he_scan_desc* d, const int64_t* h_k, const he_ct_array* grad, const he_ct_array* gate, const he_ct_array* states,
+                           const ckks_key* const* rot_keys, const ckks_key* const* cross_keys, const ckks_key* back_rot, const ckks_key* back_cross, uint64_t* d_dx, uint64_t* d_dgate,
+                           void* d_ws, size_t ws_bytes, void* stream) {
+    if (!c) return CKKS_ERR_INVALID_ARG;
+    if (int rc = scan_check(c, d, d_dgate ? 1 : 0)) return rc;
+    if (!d_dx || !h_k) return set_err(c, CKKS_ERR_INVALID_ARG, "null pointer");
+    if (((uintptr_t)d_dx | (uintptr_t)d_dgate) & 15) return set_err(c, CKKS_ERR_INVALID_ARG, "output not aligned to 16 bytes");
+    if (int rc = check_scan_keys(c, d, false, rot_keys, cross_keys)) return rc;
+    const u32 back = scan_element(c, d, 0, true), level = d->level, last = level - d->steps, per = d->channels / d->heads;
+    if (d_dgate)
+        if (int rc = check_turn_keys(c, back_rot, back_cross, back)) return rc;
+    if (int rc = check_array(c, grad, d->channels, level + 1, 2)) return rc;
+    if (int rc = check_array(c, gate, d->heads, level + 1, 2)) return rc;
+    if (d_dgate)
+        if (int rc = check_array(c, states, d->channels, last + 1, 2)) return rc;
+    if (!d_ws || ws_bytes < ws_scan_backward(c, d)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the scan's backward pass");
+    hipStream_t st = (hipStream_t)stream;
+    const size_t N = c->N, L1 = level + 1, ct = 2 * L1 * N;
+    const u32 ng = scan_gates_batch(c, d);
+    Arena ar(d_ws, ws_bytes);
+    u64* turned = ar.take((size_t)d->heads * ct);
+    if (!ar.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the scan's backward pass");
+    for (u32 g0 = 0; g0 < d->heads; g0 += ng) {  // the gates one position on
+        const u32 n = d->heads - g0 < ng ? d->heads - g0 : ng;
+        Arena sub = ar.rest();
+        u64* compact = sub.take((size_t)n * ct);
+        KsWs ws;
+        if (!carve_ks(c, level, n, n, sub, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the scan's backward pass");
+        const u64* src = (const u64*)gate->d + (size_t)g0 * gate->ct_stride;
+        if (gate->comp_stride != L1 * N) HIP_TRY(launch_copy_cts(c, (u32)L1, n, src, gate->ct_stride, gate->comp_stride, compact, st));
+        const u64* srcs[KS_MAX_BATCH];
+        const ckks_key* keys[KS_MAX_BATCH];
+        u32 gal[KS_MAX_BATCH];
+        u64* outs[KS_MAX_BATCH];
+        for (u32 b = 0; b < n; b++) {
+            srcs[b] = gate->comp_stride != L1 * N ? compact + b * ct : src + (size_t)b * gate->ct_stride;
+            keys[b] = rot_keys[0];
+            gal[b] = rot_keys[0]->galois_elt;
+            outs[b] = turned + (g0 + b) * ct;
+        }
+        if (int rc = run_rotate_batch(c, level, n, srcs, keys, gal, outs, ws, st)) return rc;
+    }
+    if (int rc = run_scan(c, d, false, h_k, *grad, he_ct_array{(const uint64_t*)turned, ct, L1 * N}, rot_keys, cross_keys, (u64*)d_dx, ar.rest(), st)) return rc;
+    if (!d_dgate) return CKKS_OK;
+    const size_t dct = (size_t)2 * (last + 1) * N, poly = (size_t)(last + 1) * N;
+    for (u32 g0 = 0; g0 < d->heads; g0 += ng) {
+        const u32 n = d->heads - g0 < ng ? d->heads - g0 : ng;
+        Arena sub = ar.rest();
+        u64* terms = sub.take(4 * (size_t)n * poly);
+        if (!sub.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the scan's backward pass");
+        TensorSum T = {(const u64*)d_dx + (size_t)g0 * per * dct, dct, poly, (const u64*)states->d + (size_t)g0 * per * states->ct_stride, states->ct_stride, states->comp_stride,
+                       per, n, back, 0, nullptr, 0, 0};
+        HIP_TRY(launch_tensor_sum(c, last, T, terms, st));
+        u64* outs[KS_MAX_BATCH];
+        for (u32 b = 0; b < n; b++) outs[b] = (u64*)d_dgate + (size_t)(g0 + b) * 2 * last * N;
+        if (int rc = run_turned_terms(c, last, n, terms, back_rot->d_key, back_cross->d_key, outs, sub.rest(), st)) return rc;
+    }
+    return CKKS_OK;
+}
+
+// n products a[b] b[b] + k x[b] (x: null, or an addend each) with relinearisation and rescale; scaled addends go through scratch where no kernel forms them on the way
+static size_t ws_product_add(const ckks_ctx* c, u32 level, u32 n) { return ws_ctct(c, level, n) + (ntt_has_modup(c) ? 0 : blk((size_t)n * 2 * (level + 1) * c->N)); }
+static int run_product_add(const ckks_ctx* c, u32 level, u32 n, const u64* const* a, size_t a_comp, const u64* const* b, size_t b_comp, int64_t k, const u64* const* x, size_t x_comp,
+                           const u64* d_rlk, u64* const* outs, Arena ar, hipStream_t st) {
+    if (!x) return run_ctct_merged(c, level, a, a_comp, b, b_comp, nullptr, 0, d_rlk, outs, n, ar, st);
+    const LimbScalars ks = limb_scalars(c, level, k), zero = limb_scalars(c, level, 0);
+    if (ntt_has_modup(c)) {
+        const LinAddend lin = {x, x_comp, ks.v, x, x_comp, zero.v};
+        return run_ctct_merged(c, level, a, a_comp, b, b_comp, nullptr, 0, d_rlk, outs, n, ar, st, &lin);
+    }
+    const size_t ct = (size_t)2 * (level + 1) * c->N;
+    u64* scaled = ar.take(n * ct);
+    if (!ar.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for products");
+    for (u32 i = 0; i < n; i++) HIP_TRY(launch_affine(c, level, x[i], x_comp, ks, zero, scaled + i * ct, st));
+    return run_ctct_merged(c, level, a, a_comp, b, b_comp, scaled, ct, d_rlk, outs, n, ar.rest(), st);
+}
+
+static int step_check(const ckks_ctx* c, const he_scan_desc* d) {
+    he_scan_desc one = d ? *d : he_scan_desc{};
+    one.steps = 1;
+    return scan_check(c, d ? &one : nullptr, 0);
+}
+static u32 step_batch(const ckks_ctx* c, const he_scan_desc* d, bool turned) { return even_batch(d->channels, turned ? turned_batch(c) : ks_batch(c)); }
+static size_t ws_step(const ckks_ctx* c, const he_scan_desc* d, bool turned) {
+    const u32 nb = step_batch(c, d, turned);
+    return turned ? ws_turned(c, d->level, nb) : ws_product_add(c, d->level, nb);
+}
+size_t he_scan_step_workspace_bytes(const ckks_ctx* c, const he_scan_desc* d) {
+    if (!c || step_check(c, d)) return 0;
+    const size_t a = ws_step(c, d, true), b = ws_step(c, d, false);
+    return a > b ? a : b;
+}
+int he_scan_step(const ckks_ctx* c, const he_scan_desc* d, int64_t k, const he_ct_array* gate, const he_ct_array* state, const he_ct_array* x, const ckks_key* rot_key,
+                 const ckks_key* cross_key, uint64_t* d_out, void* d_ws, size_t ws_bytes, void* stream) {
+    if (!c) return CKKS_ERR_INVALID_ARG;
+    if (int rc = step_check(c, d)) return rc;
+    if (!d_out) return set_err(c, CKKS_ERR_INVALID_ARG, "null pointer");
+    if ((uintptr_t)d_out & 15) return set_err(c, CKKS_ERR_INVALID_ARG, "output not aligned to 16 bytes");
+    if (!cross_key) return set_err(c, CKKS_ERR_NO_KEY, "no key");
+    const bool turned = rot_key != nullptr;
+    if (!turned && cross_key->galois_elt != 0) return set_err(c, CKKS_ERR_NO_KEY, "without a rotation the key has to be the relinearisation key");
+    if (turned) {
+        if (rot_key->galois_elt <= 1 || (rot_key->galois_elt & CKKS_KEY_CROSS)) return set_err(c, CKKS_ERR_NO_KEY, "not a rotation key, or one of a rotation by 0");
+        if (int rc = check_turn_keys(c, rot_key, cross_key, rot_key->galois_elt)) return rc;
+    }
+    const u32 level = d->level, per = d->channels / d->heads;
+    if (int rc = check_array(c, gate, d->heads, level + 1, 2)) return rc;
+    if (int rc = check_array(c, state, d->channels, level + 1, 2)) return rc;
+    const bool add = x && x->d;
+    if (add)
+        if (int rc = check_array(c, x, d->channels, level + 1, 2)) return rc;
+    if (!d_ws || ws_bytes < ws_step(c, d, turned)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the step");
+    const u32 nb = step_batch(c, d, turned);
+    for (u32 c0 = 0; c0 < d->channels; c0 += nb) {
+        const u32 n = d->channels - c0 < nb ? d->channels - c0 : nb;
+        const u64 *pa[KS_MAX_BATCH], *ph[KS_MAX_BATCH], *px[KS_MAX_BATCH];
+        u64* po[KS_MAX_BATCH];
+        for (u32 b = 0; b < n; b++) {
+            pa[b] = (const u64*)gate->d + (size_t)((c0 + b) / per) * gate->ct_stride;
+            ph[b] = (const u64*)state->d + (size_t)(c0 + b) * state->ct_stride;
+            px[b] = add ? (const u64*)x->d + (size_t)(c0 + b) * x->ct_stride : nullptr;
+            po[b] = (u64*)d_out + (size_t)(c0 + b) * 2 * level * c->N;
+        }
+        const size_t x_comp = add ? x->comp_stride : 0;
+        int rc;
+        if (turned)
+            rc = run_turned(c, level, n, pa, gate->comp_stride, ph, state->comp_stride, rot_key->galois_elt, k, add ? px : nullptr, x_comp, rot_key->d_key, cross_key->d_key, po,
+                            Arena(d_ws, ws_bytes), (hipStream_t)stream);
+        else
+            rc = run_product_add(c, level, n, pa, gate->comp_stride, ph, state->comp_stride, k, add ? px : nullptr, x_comp, cross_key->d_key, po, Arena(d_ws, ws_bytes),
+                                 (hipStream_t)stream);
+        if (rc) return rc;
+    }
+    return CKKS_OK;
+}
+
+// ---- layer norm ----
+static int check_rlk(const ckks_ctx* c, const ckks_key* rlk) {
+    if (!rlk) return set_err(c, CKKS_ERR_NO_KEY, "no relinearisation key");
+    if (rlk->galois_elt != 0) return set_err(c, CKKS_ERR_NO_KEY, "key is a rotation key, not the relinearisation key");
+    return CKKS_OK;
+}
+static int layer_norm_check(const ckks_ctx* c, const he_layer_norm_desc* d) {
+    if (!d) return set_err(c, CKKS_ERR_INVALID_ARG, "null descriptor");
+    if (d->channels == 0 || d->channels > 65536) return set_err(c, CKKS_ERR_INVALID_ARG, "channels out of range (1 to 65536)");
+    if (d->iterations > HE_NORM_MAX_ITERATIONS) return set_err(c, CKKS_ERR_INVALID_ARG, "too many iterations");
+    if (d->affine > 1) return set_err(c, CKKS_ERR_INVALID_ARG, "affine is 0 or 1");
+    if (!c->dnum) return set_err(c, CKKS_ERR_UNSUPPORTED_PARAMS, "context has no key-switching digits");
+    if (!level_ok(c, d->level) || d->level < 3 + d->affine + 2 * d->iterations)
+        return set_err(c, CKKS_ERR_LEVEL_MISMATCH, "layer norm needs 3 + 2 iterations <= level < num_q, with a gain one more");
+    return CKKS_OK;
+}
+static size_t ws_layer_norm(const ckks_ctx* c, const he_layer_norm_desc* d) {
+    const size_t N = c->N, L1 = d->level + 1, m = d->level - 2 - 2 * d->iterations;
+    const u32 nb = even_batch(d->channels, ks_batch(c));
+    size_t sub = ws_inverse_root(c, d->level, d->iterations), t;
+    if ((t = blk((size_t)nb * 2 * (m + 1) * N) + ws_ctct(c, (u32)m, nb)) > sub) sub = t;
+    if (d->affine && (t = ws_product_add(c, (u32)m - 1, nb)) > sub) sub = t;
+    return blk(3 * L1 * N) + 3 * blk(2 * L1 * N) + 3 * blk(2 * N * d->level) + sub;
+}
+size_t he_layer_norm_workspace_bytes(const ckks_ctx* c, const he_layer_norm_desc* d) {
+    if (!c || layer_norm_check(c, d)) return 0;
+    return ws_layer_norm(c, d);
+}
+int he_layer_norm(const ckks_ctx* c, const he_layer_norm_desc* d, const int64_t* h_k_newton, const he_ct_array* x, const he_ct_array* gain, const he_ct_array* bias,
+                  const ckks_key* rlk, uint64_t* d_norm, uint64_t* d_inv, uint64_t* d_out, void* d_ws, size_t ws_bytes, void* stream) {
+    if (!c) return CKKS_ERR_INVALID_ARG;
+    if (int rc = layer_norm_check(c, d)) return rc;
+    if (!d_norm || (d->iterations && !h_k_newton)) return set_err(c, CKKS_ERR_INVALID_ARG, "null pointer");
+    if ((d->affine != 0) != (d_out != nullptr)) return set_err(c, CKKS_ERR_INVALID_ARG, "an output with gain and bias comes with a gain, and only then");
+    if (((uintptr_t)d_norm | (uintptr_t)d_inv | (uintptr_t)d_out) & 15) return set_err(c, CKKS_ERR_INVALID_ARG, "output not aligned to 16 bytes");
+    if (int rc = check_rlk(c, rlk)) return rc;
+    const u32 level = d->level, m = level - 2 - 2 * d->iterations, C = d->channels;
+    if (int rc = check_array(c, x, C, level + 1, 2)) return rc;
+    if (d->affine)
+        if (int rc = check_array(c, gain, C, m, 2)) return rc;
+    const bool add = bias && bias->d;
+    if (add && !d->affine) return set_err(c, CKKS_ERR_INVALID_ARG, "a bias needs a gain");
+    if (add)
+        if (int rc = check_array(c, bias, C, m, 2)) return rc;
+    if (!d_ws || ws_bytes < ws_layer_norm(c, d)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the layer norm");
+    hipStream_t st = (hipStream_t)stream;
+    const size_t N = c->N, L1 = level + 1;
+    Arena ar(d_ws, ws_bytes);
+    u64* sq3 = ar.take(3 * L1 * N);
+    u64* sum = ar.take(2 * L1 * N);
+    u64* ra = ar.take(2 * L1 * N);
+    u64* rb = ar.take(2 * L1 * N);
+    u64* s = ar.take(2 * N * level);
+    u64* u = ar.take(2 * N * level);
+    u64* w = ar.take(2 * N * level);
+    if (!ar.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the layer norm");
+    HIP_TRY(launch_centred_squares(c, level, (const u64*)x->d, x->ct_stride, x->comp_stride, C, times_limb(c, d->k_eps, level), sq3, sum, st));
+    if (int rc = run_inverse_root(c, level, d->iterations, d->k_slope, d->k_start, h_k_newton, rlk->d_key, sq3, s, u, w, ra, rb, ar.rest(), st)) return rc;
+    if (d_inv) HIP_TRY(launch_copy(ra, (u64*)d_inv, (size_t)2 * (m + 1) * N, st));
+    const u32 nb = even_batch(C, ks_batch(c));
+    const size_t rs = (size_t)(m + 1) * N, norm_ct = (size_t)2 * m * N, out_ct = (size_t)2 * (m - 1) * N;
+    for (u32 c0 = 0; c0 < C; c0 += nb) {
+        const u32 n = C - c0 < nb ? C - c0 : nb;
+        Arena sub = ar.rest();
+        u64* y = sub.take(n * 2 * rs);
+        if (!sub.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the layer norm");
+        HIP_TRY(launch_centre(c, m + 1, n, (const u64*)x->d + (size_t)c0 * x->ct_stride, x->ct_stride, x->comp_stride, C, sum, L1 * N, y, st));
+        const u64 *py[KS_MAX_BATCH], *pr[KS_MAX_BATCH], *pg[KS_MAX_BATCH], *pn[KS_MAX_BATCH], *pb[KS_MAX_BATCH];
+        u64 *on[KS_MAX_BATCH], *oo[KS_MAX_BATCH];
+        for (u32 b = 0; b < n; b++) {
+            py[b] = y + b * 2 * rs;
+            pr[b] = ra;
+            on[b] = (u64*)d_norm + (size_t)(c0 + b) * norm_ct;
+            pn[b] = on[b];
+            pg[b] = d->affine ? (const u64*)gain->d + (size_t)(c0 + b) * gain->ct_stride : nullptr;
+            pb[b] = add ? (const u64*)bias->d + (size_t)(c0 + b) * bias->ct_stride : nullptr;
+            oo[b] = d->affine ? (u64*)d_out + (size_t)(c0 + b) * out_ct : nullptr;
+        }
+        if (int rc = run_ctct_merged(c, m, py, rs, pr, rs, nullptr, 0, rlk->d_key, on, n, sub.rest(), st)) return rc;
+        if (!d->affine) continue;
+        if (int rc = run_product_add(c, m - 1, n, pg, gain->comp_stride, pn, (size_t)m * N, d->k_bias, add ? pb : nullptr, add ? bias->comp_stride : 0, rlk->d_key, oo, ar.rest(), st))
+            return rc;
+    }
+    return CKKS_OK;
+}
+
+static int layer_norm_grad_check(const ckks_ctx* c, const he_layer_norm_grad_desc* d) {
+    if (!d) return set_err(c, CKKS_ERR_INVALID_ARG, "null descriptor");
+    if (d->channels == 0 || d->channels > 65536) return set_err(c, CKKS_ERR_INVALID_ARG, "channels out of range (1 to 65536)");
+    if (d->affine > 1) return set_err(c, CKKS_ERR_INVALID_ARG, "affine is 0 or 1");
+    if (d->n_stages > HE_SUM_MAX_STAGES) return set_err(c, CKKS_ERR_INVALID_ARG, "too many stages");
+    if (!c->dnum) return set_err(c, CKKS_ERR_UNSUPPORTED_PARAMS, "context has no key-switching digits");
+    if (!level_ok(c, d->level) || d->level < 3 + d->affine) return set_err(c, CKKS_ERR_LEVEL_MISMATCH, "layer norm's backward pass needs 3 <= level < num_q, with a gain one more");
+    return CKKS_OK;
+}
+static u32 slot_sum_batch(u32 n) { return even_batch(n, CT_BATCH); }
+static size_t ws_slot_sum(const ckks_ctx* c, u32 level, u32 n) { return ws_ks(c, level, n, 2 * n); }
+// z[b] <- z[b] + the sum of its rotations by the keys, n <= CT_BATCH ciphertexts [2][level + 1][N]
+static int run_slot_sum(const ckks_ctx* c, u32 level, u32 n, u64* const* z, const ckks_key* const* keys, u32 n_keys, Arena ar, hipStream_t st) {
+    KsWs ws;
+    if (!carve_ks(c, level, n, 2 * n, ar, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for sums over slots");
+    const u64 *c0s[KS_MAX_BATCH], *c1s[KS_MAX_BATCH], *kd[KS_MAX_BATCH];
+    u32 gs[KS_MAX_BATCH];
+    FinalItem items[KS_MAX_BATCH];
+    for (u32 b = 0; b < n; b++) {
+        c0s[b] = z[b];
+        c1s[b] = z[b] + (size_t)(level + 1) * c->N;
+        items[b] = FinalItem{nullptr, nullptr, nullptr, z[b], 1, 0, z[b]};
+    }
+    if (int rc = run_modup(c, level, c1s, n, ws, st)) return rc;
+    for (u32 i = 0; i < n_keys; i++) {
+        for (u32 b = 0; b < n; b++) kd[b] = keys[i]->d_key, gs[b] = keys[i]->galois_elt;
+        HIP_TRY(launch_key_inner_items(c, level, dsrc(c, ws, 0), kd, gs, c0s, ws.v + (i ? n : 0) * ws.v_b, ws.v_b, n, st));
+        if (i) HIP_TRY(launch_add_ext(c, level, ws.v, ws.v + n * ws.v_b, 2 * n, st));
+    }
+    return run_moddown(c, level, ws, n, items, st);
+}
+static size_t ws_layer_norm_grad(const ckks_ctx* c, const he_layer_norm_grad_desc* d) {
+    const size_t N = c->N, level = d->level, bg = level - d->affine;
+    const u32 nb = even_batch(d->channels, ks_batch(c)), ns = slot_sum_batch(d->channels);
+    size_t sub = ws_ctct(c, d->level, nb), t;
+    if ((t = ws_ks(c, (u32)bg, 1, 1)) > sub) sub = t;
+    if ((t = blk(3 * nb * (bg - 1) * N) + ws_ks(c, (u32)bg - 2, nb, nb)) > sub) sub = t;
+    if (d->n_stages && (t = ws_slot_sum(c, d->level - 1, ns)) > sub) sub = t;
+    return (d->affine ? blk((size_t)d->channels * 2 * level * N) : 0) + blk(3 * (bg + 1) * N) + blk(2 * (bg + 1) * N) + 2 * blk(2 * bg * N) + sub;
+}
+size_t he_layer_norm_backward_workspace_bytes(const ckks_ctx* c, const he_layer_norm_grad_desc* d) {
+    if (!c || layer_norm_grad_check(c, d)) return 0;
+    return ws_layer_norm_grad(c, d);
+}
+int he_layer_norm_backward(const ckks_ctx* c, const he_layer_norm_grad_desc* d, const he_ct_array* grad, const he_ct_array* norm, const he_ct_array* inv, const he_ct_array* gain,
+                           const ckks_key* rlk, const uint32_t* h_stage_rots, const ckks_key* const* sum_keys, uint64_t* d_dx, uint64_t* d_dgain, uint64_t* d_dbias, void* d_ws,
+                           size_t ws_bytes, void* stream) {
+    if (!c) return CKKS_ERR_INVALID_ARG;
+    if (int rc = layer_norm_grad_check(c, d)) return rc;
+    if (!d_dx) return set_err(c, CKKS_ERR_INVALID_ARG, "null pointer");
+    if (((uintptr_t)d_dx | (uintptr_t)d_dgain | (uintptr_t)d_dbias) & 15) return set_err(c, CKKS_ERR_INVALID_ARG, "output not aligned to 16 bytes");
+    if (int rc = check_rlk(c, rlk)) return rc;
+    const u32 level = d->level, C = d->channels, bg = level - d->affine;
+    const bool sums = d->n_stages && (d_dgain || d_dbias);
+    if (sums) {
+        if (!h_stage_rots || !sum_keys) return set_err(c, CKKS_ERR_INVALID_ARG, "null pointer");
+        u32 k = 0;
+        for (u32 i = 0; i < d->n_stages; i++) {
+            if (h_stage_rots[i] == 0 || h_stage_rots[i] > 65536) return set_err(c, CKKS_ERR_INVALID_ARG, "a stage of a sum over slots has 1 to 65536 rotations");
+            for (u32 r = 0; r < h_stage_rots[i]; r++, k++)
+                if (!sum_keys[k] || sum_keys[k]->galois_elt <= 1 || (sum_keys[k]->galois_elt & CKKS_KEY_CROSS))
+                    return set_err(c, CKKS_ERR_NO_KEY, "key of a sum over slots missing, or not the key of a rotation by other than 0");
+        }
+    }
+    if (int rc = check_array(c, grad, C, level + 1, 2)) return rc;
+    if (int rc = check_array(c, norm, C, level + 1, 2)) return rc;
+    if (int rc = check_array(c, inv, 1, bg, 2)) return rc;
+    if (d->affine)
+        if (int rc = check_array(c, gain, C, level + 1, 2)) return rc;
+    if (!d_ws || ws_bytes < ws_layer_norm_grad(c, d)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the layer norm's backward pass");
+    hipStream_t st = (hipStream_t)stream;
+    const size_t N = c->N;
+    const u32 nb = even_batch(C, ks_batch(c));
+    Arena ar(d_ws, ws_bytes);
+    u64* g = d->affine ? ar.take((size_t)C * 2 * level * N) : nullptr;
+    u64* dot3 = ar.take(3 * (size_t)(bg + 1) * N);
+    u64* sum = ar.take(2 * (size_t)(bg + 1) * N);
+    u64* dot = ar.take(2 * (size_t)bg * N);
+    u64* t = ar.take(2 * (size_t)bg * N);
+    if (!ar.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the layer norm's backward pass");
+    auto at = [](const he_ct_array* a, u32 i) { return (const u64*)a->d + (size_t)i * a->ct_stride; };
+    he_ct_array ga = *grad;
+    if (d->affine) {
+        for (u32 c0 = 0; c0 < C; c0 += nb) {
+            const u32 n = C - c0 < nb ? C - c0 : nb;
+            const u64 *pa[KS_MAX_BATCH], *pb[KS_MAX_BATCH];
+            u64* po[KS_MAX_BATCH];
+            for (u32 b = 0; b < n; b++) pa[b] = at(gain, c0 + b), pb[b] = at(grad, c0 + b), po[b] = g + (size_t)(c0 + b) * 2 * level * N;
+            if (int rc = run_ctct_merged(c, level, pa, gain->comp_stride, pb, grad->comp_stride, nullptr, 0, rlk->d_key, po, n, ar.rest(), st)) return rc;
+        }
+        ga = he_ct_array{(const uint64_t*)g, (size_t)2 * level * N, (size_t)level * N};
+    }
+    // T, u and t
+    const u32 m = bg - 2;  // level of the last products
+    const size_t poly = (size_t)(bg + 1) * N, sum_comp = (size_t)(m + 1) * N;
+    TensorSum T = {(const u64*)ga.d, ga.ct_stride, ga.comp_stride, (const u64*)norm->d, norm->ct_stride, norm->comp_stride, C, 1, 1, 1, sum, m + 1, 0};
+    HIP_TRY(launch_tensor_sum(c, bg, T, dot3, st));
+    auto relinearise = [&](u32 lv, const u64* terms, size_t p, u32 n, u64* const* outs, Arena sub) -> int {  // terms: n d0, n d1, n d2, p words each
+        KsWs ws;
+        if (!carve_ks(c, lv, n, n, sub, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the layer norm's backward pass");
+        const u64 *d0[KS_MAX_BATCH], *d1[KS_MAX_BATCH], *d2[KS_MAX_BATCH];
+        u64* vs[KS_MAX_BATCH];
+        FinalItem items[KS_MAX_BATCH];
+        for (u32 b = 0; b < n; b++) {
+            d0[b] = terms + b * p;
+            d1[b] = terms + (n + b) * p;
+            d2[b] = terms + (2 * n + b) * p;
+            vs[b] = ws.v + b * ws.v_b;
+            items[b] = FinalItem{nullptr, nullptr, nullptr, outs[b], 1, 0, nullptr};
+        }
+        if (int rc = run_modup(c, lv, d2, n, ws, st)) return rc;
+        HIP_TRY(launch_key_inner_ext(c, lv, dsrc(c, ws, 0), rlk->d_key, 1, d0, d1, nullptr, vs, n, st));
+        return run_moddown(c, lv, ws, n, items, st, true);
+    };
+    if (int rc = relinearise(bg, dot3, poly, 1, &dot, ar.rest())) return rc;
+    {
+        const u64 *pi = (const u64*)inv->d, *pd = dot;
+        if (int rc = run_ctct_merged(c, bg - 1, &pi, inv->comp_stride, &pd, (size_t)bg * N, nullptr, 0, rlk->d_key, &t, 1, ar.rest(), st)) return rc;
+    }
+    // dx
+    for (u32 c0 = 0; c0 < C; c0 += nb) {
+        const u32 n = C - c0 < nb ? C - c0 : nb;
+        const size_t p = (size_t)(m + 1) * N;
+        Arena sub = ar.rest();
+        u64* terms = sub.take(3 * n * p);
+        if (!sub.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the layer norm's backward pass");
+        const NormGradTerms G = {(const u64*)inv->d, inv->comp_stride, t, (size_t)(bg - 1) * N, sum, sum_comp, (const u64*)ga.d + (size_t)c0 * ga.ct_stride, ga.ct_stride, ga.comp_stride,
+                                 at(norm, c0), norm->ct_stride, norm->comp_stride, C, 0, limb_scalars(c, m, d->k_grad), limb_scalars(c, m, d->k_norm)};
+        HIP_TRY(launch_norm_grad_terms(c, m, G, terms, n, st));
+        u64* po[KS_MAX_BATCH];
+        for (u32 b = 0; b < n; b++) po[b] = (u64*)d_dx + (size_t)(c0 + b) * 2 * m * N;
+        if (int rc = relinearise(m, terms, p, n, po, sub.rest())) return rc;
+    }
+    // the gradients of gain and bias, in place
+    const size_t wct = (size_t)2 * level * N;
+    if (d_dgain) {
+        for (u32 c0 = 0; c0 < C; c0 += nb) {
+            const u32 n = C - c0 < nb ? C - c0 : nb;
+            const u64 *pa[KS_MAX_BATCH], *pb[KS_MAX_BATCH];
+            u64* po[KS_MAX_BATCH];
+            for (u32 b = 0; b < n; b++) pa[b] = at(grad, c0 + b), pb[b] = at(norm, c0 + b), po[b] = (u64*)d_dgain + (size_t)(c0 + b) * wct;
+            if (int rc = run_ctct_merged(c, level, pa, grad->comp_stride, pb, norm->comp_stride, nullptr, 0, rlk->d_key, po, n, ar.rest(), st)) return rc;
+        }
+    }
+    if (d_dbias) {
+        for (u32 c0 = 0; c0 < C; c0 += 1024) {
+            const u32 n = C - c0 < 1024 ? C - c0 : 1024;
+            HIP_TRY(launch_copy_cts(c, level, n, at(grad, c0), grad->ct_stride, grad->comp_stride, (u64*)d_dbias + (size_t)c0 * wct, st));
+        }
+    }
+    if (!sums) return CKKS_OK;
+    const u32 ns = slot_sum_batch(C);
+    for (u64* z : {(u64*)d_dgain, (u64*)d_dbias}) {
+        if (!z) continue;
+        for (u32 c0 = 0; c0 < C; c0 += ns) {
+            const u32 n = C - c0 < ns ? C - c0 : ns;
+            u64* pz[KS_MAX_BATCH];
+            for (u32 b = 0; b < n; b++) pz[b] = z + (size_t)(c0 + b) * wct;
+            for (u32 i = 0, k = 0; i < d->n_stages; k += h_stage_rots[i], i++)
+                if (int rc = run_slot_sum(c, level - 1, n, pz, sum_keys + k, h_stage_rots[i], ar.rest(), st)) return rc;
+        }
     }
     return CKKS_OK;
 }

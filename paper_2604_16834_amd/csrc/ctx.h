@@ -449,3 +449,40 @@ hipError_t launch_affine(const ckks_ctx* c, u32 level, const u64* ct, size_t ct_
 // limbs limb0 .. level: out [n][2][level + 1 - limb0][N]
 hipError_t launch_gate_mul(const ckks_ctx* c, u32 level, u32 limb0, u32 n, const u64* ct, size_t ct_stride, size_t ct_comp, const u64* gate, size_t gate_stride,
                            u64* out, hipStream_t st);
+// recurrent.hip
+// item b: out [4][n][level + 1][N] = a0 sigma_g(h0) + k x0, a1 sigma_g(h0) + k x1, a0 sigma_g(h1), a1 sigma_g(h1)   (x.p[b] may be null)
+hipError_t launch_turned_terms(const ckks_ctx* c, u32 level, const PtrList8& a, size_t a_comp, const PtrList8& h, size_t h_comp, const PtrList8& x, size_t x_comp,
+                               const LimbScalars& k, u32 g, u64* out, u32 n, hipStream_t st);
+// sums of a_c (x) sigma_g(b_c) over the `per` channels of each group: out [3 (closed, g = 1) or 4][groups][level + 1][N]
+struct TensorSum {
+    const u64* a;
+    size_t a_ct, a_comp;
+    const u64* b;
+    size_t b_ct, b_comp;
+    u32 per, groups, g, closed;
+    u64* sum;  // or null: sum_c a_c, [2][sum_limbs][N] (one group)
+    u32 sum_limbs, pad;
+};
+hipError_t launch_tensor_sum(const ckks_ctx* c, u32 level, const TensorSum& T, u64* out, hipStream_t st);
+hipError_t launch_centred_squares(const ckks_ctx* c, u32 level, const u64* in, size_t in_ct, size_t in_comp, u32 channels, const LimbScalars& add, u64* d, u64* sum,
+                                  hipStream_t st);
+hipError_t launch_centre(const ckks_ctx* c, u32 limbs, u32 n, const u64* in, size_t in_ct, size_t in_comp, u32 channels, const u64* sum, size_t sum_comp, u64* out,
+                         hipStream_t st);
+// d = inv (x) k_grad (channels g - sum) + (k_norm t) (x) norm for n channels
+struct NormGradTerms {
+    const u64* inv;
+    size_t inv_comp;
+    const u64* t;
+    size_t t_comp;
+    const u64* sum;
+    size_t sum_comp;
+    const u64* g;
+    size_t g_ct, g_comp;
+    const u64* norm;
+    size_t norm_ct, norm_comp;
+    u32 channels, pad;
+    LimbScalars k_grad, k_norm;
+};
+hipError_t launch_norm_grad_terms(const ckks_ctx* c, u32 level, const NormGradTerms& T, u64* out, u32 n, hipStream_t st);
+hipError_t launch_add_ext(const ckks_ctx* c, u32 level, u64* v, const u64* w, u32 n, hipStream_t st);
+hipError_t launch_copy_cts(const ckks_ctx* c, u32 limbs, u32 n, const u64* in, size_t in_ct, size_t in_comp, u64* out, hipStream_t st);
