@@ -137,8 +137,9 @@ size_t ws_ctct(const ckks_ctx* c, u32 level, u32 n) {
 // inside the inner product (launch_ntt_lo_mac).
 // muls (with hi_only): the polynomial to decompose is srcs[b] (.) muls[b], formed as the inverse transform loads it.
 // gals (with hi_only, ntt_has_modup): it is sigma_gals[b](srcs[b]); the own limbs stay where they are, not permuted.
+// gal_mul_only (with muls and gals): it is srcs[b] (.) sigma_gals[b](muls[b]).
 int run_modup(const ckks_ctx* c, u32 level, const u64* const* srcs, u32 n, const KsWs& ws, hipStream_t st, bool hi_only = false,
-              const u64* const* muls = nullptr, const u32* gals = nullptr) {
+              const u64* const* muls = nullptr, const u32* gals = nullptr, bool gal_mul_only = false) {
     const u32 N = c->N, L1 = level + 1, E = c->ext_limbs(level), beta = c->live_digits(level);
     for (u32 b = 0; b < KS_MAX_BATCH; b++) ws.own[b] = (b < n && !muls) ? srcs[b] : nullptr;  // a product has no stored own limbs
     if (muls && !hi_only) return set_err(c, CKKS_ERR_INVALID_ARG, "internal: product source without the fused inner product");
@@ -150,7 +151,7 @@ int run_modup(const ckks_ctx* c, u32 level, const u64* const* srcs, u32 n, const
     if (hi_only && !fused) return set_err(c, CKKS_ERR_INVALID_ARG, "internal: fused inner product without fused ModUp");
     const u32 mid = ntt_mid_modup(c, level, n);  // the inverse's second pass inside the converting one
     HIP_TRY(launch_ntt(c, true, nullptr, 0, ws.y, L1, range_list(0, L1, 0), n, st, srcs, nullptr,
-                       fused ? c->d_modup_prep_f + (size_t)level * c->num_q : nullptr, muls, nullptr, mid ? NTT_LO : NTT_BOTH, gals));  // (positions 0..level are moduli 0..level)
+                       fused ? c->d_modup_prep_f + (size_t)level * c->num_q : nullptr, muls, nullptr, mid ? NTT_LO : NTT_BOTH, gals, gal_mul_only));  // (positions 0..level are moduli 0..level)
     if (fused) {
         HIP_TRY(launch_ntt_modup(c, level, (const double*)ws.y, ws.y_b, ws.digits, n, st, hi_only, mid));
         return CKKS_OK;
@@ -276,23 +277,25 @@ int run_moddown(const ckks_ctx* c, u32 level, const KsWs& ws, u32 n, const Final
 // sixteen (6144 a batch) 993 / 981 / 840
 #define DIVIDE_INSIDE_HOISTED 900
 int run_inner_divide(const ckks_ctx* c, u32 level, const KsWs& ws, const u64* const* keys, u32 n, u64* const* outs, const u64* const* accs, hipStream_t st,
-                     bool merged, const MacProduct* prod, const MacRotate* rot, u32 keep = 0) {  // keep: see run_moddown
+                     bool merged, const MacProduct* prod, const MacRotate* rot, u32 keep = 0, const MacTurn* turn = nullptr) {  // keep: see run_moddown
     u64* vs[KS_MAX_BATCH];
     for (u32 b = 0; b < n; b++) vs[b] = ws.v + b * ws.v_b;
+    DigitSrc digits = dsrc(c, ws, 0);
+    if (turn) digits.bstride *= 2;  // two polynomials an item
     const u32 from = dropped_from(level, merged);
     const u32 slices = from * n << c->log_hi;
     if (rot && rot->hoisted ? slices < DIVIDE_INSIDE_HOISTED : c->log_hi < 2 || slices < DIVIDE_INSIDE_SLICES) {
-        HIP_TRY(launch_ntt_lo_mac(c, level, dsrc(c, ws, 0), keys, vs, n, st, from, prod, rot));
+        HIP_TRY(launch_ntt_lo_mac(c, level, digits, keys, vs, n, st, from, prod, rot, nullptr, nullptr, false, turn));
         FinalItem items[KS_MAX_BATCH];
         for (u32 b = 0; b < n; b++) items[b] = FinalItem{nullptr, nullptr, nullptr, outs[b], 1, 0, accs ? accs[b] : nullptr};
         return run_moddown(c, level, ws, n, items, st, merged, true, keep);
     }
-    HIP_TRY(launch_ntt_lo_mac(c, level, dsrc(c, ws, 0), keys, vs, n, st, from, prod, rot, nullptr, nullptr, true));
+    HIP_TRY(launch_ntt_lo_mac(c, level, digits, keys, vs, n, st, from, prod, rot, nullptr, nullptr, true, turn));
     if (int rc = run_moddown(c, level, ws, n, nullptr, st, merged, true, keep)) return rc;
     const u64* tab = merged ? c->moddown_rs_table(level) : c->d_moddown;
     const u32 kp = merged ? c->k2_pad : c->k_pad;
     const MacDivide div = {(const double*)ws.w, tab + 2 * kp + (size_t)kp * c->num_q, outs, accs};
-    HIP_TRY(launch_ntt_lo_mac(c, level, dsrc(c, ws, 0), keys, vs, n, st, keep ? keep : from, prod, rot, nullptr, &div));
+    HIP_TRY(launch_ntt_lo_mac(c, level, digits, keys, vs, n, st, keep ? keep : from, prod, rot, nullptr, &div, false, turn));
     return CKKS_OK;
 }
 
@@ -2553,40 +2556,74 @@ int he_norm_gate(const ckks_ctx* c, const he_norm_desc* d, const int64_t* h_k_ne
 }
 
 // ---- a recurrent block's operators -----------------------------------------------------------------------
-// n products with a rotated operand, outs[b] = Rescale(a[b] (.) sigma_g(h[b]) + k x[b]) (x: null, or one addend each), level -> level - 1: two key switches, of a0 sigma(h1)
-// and of a1 sigma(h1), that share one division.  n <= turned_batch.
+// n products with a rotated operand, outs[b] = Rescale(a[b] (.) sigma_g(h[b]) + k x[b]) (x: null, or addends, entries may be null), level -> level - 1: two key switches, of
+// a0 sigma(h1) and of a1 sigma(h1), that share one division.  n <= turned_batch.  With the fused passes nothing of the tensor product is stored: the decomposed polynomials are formed
+// as their inverse transforms load them, everything else where the inner product ends; elsewhere launch_turned_terms writes its four parts.
 static u32 turned_batch(const ckks_ctx* c) { return ks_batch(c) / 2; }
-static size_t ws_turned(const ckks_ctx* c, u32 level, u32 n) { return blk(4 * (size_t)n * (level + 1) * c->N) + ws_ks(c, level, 2 * n, 2 * n); }
+static size_t ws_turned_ks(const ckks_ctx* c, u32 level, u32 n) { return ws_ks(c, level, 2 * n, ntt_has_modup(c) ? n : 2 * n); }
+static size_t ws_turned(const ckks_ctx* c, u32 level, u32 n, bool terms) {
+    return (terms || !ntt_has_modup(c) ? blk(4 * (size_t)n * (level + 1) * c->N) : 0) + ws_turned_ks(c, level, n);
+}
 // terms [4][n][level + 1][N]: what launch_turned_terms gives
 static int run_turned_terms(const ckks_ctx* c, u32 level, u32 n, const u64* terms, const u64* d_rot, const u64* d_cross, u64* const* outs, Arena ar, hipStream_t st) {
     const size_t poly = (size_t)(level + 1) * c->N;
+    const bool mac = ntt_has_modup(c);
     KsWs ws;
-    if (!carve_ks(c, level, 2 * n, 2 * n, ar, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for products with rotated operands");
-    const u64 *polys[KS_MAX_BATCH], *add0[KS_MAX_BATCH], *add1[KS_MAX_BATCH];
+    if (!carve_ks(c, level, 2 * n, mac ? n : 2 * n, ar, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for products with rotated operands");
+    const u64 *polys[KS_MAX_BATCH], *e0[KS_MAX_BATCH], *e1[KS_MAX_BATCH], *u[KS_MAX_BATCH], *v[KS_MAX_BATCH], *keys[KS_MAX_BATCH];
+    for (u32 b = 0; b < n; b++) {
+        e0[b] = terms + b * poly;
+        e1[b] = terms + (n + b) * poly;
+        u[b] = terms + (2 * n + b) * poly;
+        v[b] = terms + (3 * n + b) * poly;
+        keys[b] = d_rot;
+        polys[mac ? 2 * b : b] = u[b];
+        polys[mac ? 2 * b + 1 : n + b] = v[b];
+    }
+    if (int rc = run_modup(c, level, polys, 2 * n, ws, st, mac)) return rc;
+    if (mac) {
+        const MacTurn turn = {e0, e1, u, v, d_cross, 1, true};
+        return run_inner_divide(c, level, ws, keys, n, outs, nullptr, st, true, nullptr, nullptr, 0, &turn);
+    }
     u64* vs[KS_MAX_BATCH];
     FinalItem items[KS_MAX_BATCH];
-    for (u32 b = 0; b < 2 * n; b++) {
-        polys[b] = terms + (2 * n + b) * poly;  // u of every item, then v of every item
-        vs[b] = ws.v + b * ws.v_b;
-    }
-    for (u32 b = 0; b < n; b++) {
-        add0[b] = terms + b * poly;
-        add1[b] = terms + (n + b) * poly;
-        items[b] = FinalItem{nullptr, nullptr, nullptr, outs[b], 1, 0, nullptr};
-    }
-    if (int rc = run_modup(c, level, polys, 2 * n, ws, st)) return rc;
-    HIP_TRY(launch_key_inner_ext(c, level, dsrc(c, ws, 0), d_rot, 1, add0, add1, nullptr, vs, n, st));
+    for (u32 b = 0; b < 2 * n; b++) vs[b] = ws.v + b * ws.v_b;
+    for (u32 b = 0; b < n; b++) items[b] = FinalItem{nullptr, nullptr, nullptr, outs[b], 1, 0, nullptr};
+    HIP_TRY(launch_key_inner_ext(c, level, dsrc(c, ws, 0), d_rot, 1, e0, e1, nullptr, vs, n, st));
     HIP_TRY(launch_key_inner_ext(c, level, dsrc(c, ws, n), d_cross, 1, nullptr, nullptr, nullptr, vs + n, n, st));
     HIP_TRY(launch_add_ext(c, level, ws.v, ws.v + n * ws.v_b, 2 * n, st));
     return run_moddown(c, level, ws, n, items, st, true);
 }
 static int run_turned(const ckks_ctx* c, u32 level, u32 n, const u64* const* a, size_t a_comp, const u64* const* h, size_t h_comp, u32 g, int64_t k, const u64* const* x, size_t x_comp,
                       const u64* d_rot, const u64* d_cross, u64* const* outs, Arena ar, hipStream_t st) {
-    u64* terms = ar.take(4 * (size_t)n * (level + 1) * c->N);
-    if (!ar.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for products with rotated operands");
+    const LimbScalars ks = limb_scalars(c, level, k);
     const u64* none[KS_MAX_BATCH] = {};
-    HIP_TRY(launch_turned_terms(c, level, ptr_list(a, n), a_comp, ptr_list(h, n), h_comp, ptr_list(x ? x : none, n), x_comp, limb_scalars(c, level, k), g, terms, n, st));
-    return run_turned_terms(c, level, n, terms, d_rot, d_cross, outs, ar.rest(), st);
+    if (!x) x = none;
+    if (!ntt_has_modup(c)) {
+        u64* terms = ar.take(4 * (size_t)n * (level + 1) * c->N);
+        if (!ar.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for products with rotated operands");
+        HIP_TRY(launch_turned_terms(c, level, ptr_list(a, n), a_comp, ptr_list(h, n), h_comp, ptr_list(x, n), x_comp, ks, g, terms, n, st));
+        return run_turned_terms(c, level, n, terms, d_rot, d_cross, outs, ar.rest(), st);
+    }
+    KsWs ws;
+    if (!carve_ks(c, level, 2 * n, n, ar, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for products with rotated operands");
+    const u64 *srcs[KS_MAX_BATCH], *muls[KS_MAX_BATCH], *a1[KS_MAX_BATCH], *h1[KS_MAX_BATCH], *px[KS_MAX_BATCH], *keys[KS_MAX_BATCH];
+    u32 gals[KS_MAX_BATCH];
+    bool add[KS_MAX_BATCH], any = false;
+    for (u32 b = 0; b < n; b++) any = any || x[b];
+    for (u32 b = 0; b < n; b++) {
+        a1[b] = a[b] + a_comp;
+        h1[b] = h[b] + h_comp;
+        keys[b] = d_rot;
+        add[b] = x[b] != nullptr;
+        px[b] = x[b] ? x[b] : (any ? h[b] : a[b]);  // (read with the component stride below, times zero)
+        srcs[2 * b] = a[b], srcs[2 * b + 1] = a1[b];
+        muls[2 * b] = muls[2 * b + 1] = h1[b];
+        gals[2 * b] = gals[2 * b + 1] = g;
+    }
+    if (int rc = run_modup(c, level, srcs, 2 * n, ws, st, true, muls, gals, true)) return rc;
+    const MacTurn turn = {a, a1, h, h1, d_cross, g, false, px, any ? x_comp : a_comp, add, ks.v};
+    return run_inner_divide(c, level, ws, keys, n, outs, nullptr, st, true, nullptr, nullptr, 0, &turn);
 }
 
 static int scan_check(const ckks_ctx* c, const he_scan_desc* d, u32 deeper) {
@@ -2616,7 +2653,7 @@ static u32 scan_batch(const ckks_ctx* c, const he_scan_desc* d) {
     return all > last ? all : last;
 }
 static size_t ws_scan(const ckks_ctx* c, const he_scan_desc* d) {
-    return (d->steps > 1 ? blk(scan_rows(c, d)) : 0) + (d->steps > 2 ? blk(scan_rows(c, d)) : 0) + ws_turned(c, d->level, scan_batch(c, d));
+    return (d->steps > 1 ? blk(scan_rows(c, d)) : 0) + (d->steps > 2 ? blk(scan_rows(c, d)) : 0) + ws_turned(c, d->level, scan_batch(c, d), false);
 }
 static int run_scan(const ckks_ctx* c, const he_scan_desc* d, bool forward, const int64_t* h_k, const he_ct_array& x, const he_ct_array& gate, const ckks_key* const* rot_keys,
                     const ckks_key* const* cross_keys, u64* d_out, Arena ar, hipStream_t st) {
@@ -2685,7 +2722,7 @@ static size_t ws_scan_backward(const ckks_ctx* c, const he_scan_desc* d) {
     const u32 ng = scan_gates_batch(c, d);
     size_t sub = blk((size_t)ng * 2 * L1 * N) + ws_rotate_unhoisted(c, d->level, ng), t;
     if ((t = ws_scan(c, d)) > sub) sub = t;
-    if (last && (t = ws_turned(c, (u32)last, ng)) > sub) sub = t;
+    if (last && (t = ws_turned(c, (u32)last, ng, true)) > sub) sub = t;
     return blk((size_t)d->heads * 2 * L1 * N) + sub;
 }
 size_t he_scan_backward_workspace_bytes(const ckks_ctx* c, const he_scan_desc* d) {
@@ -2775,14 +2812,13 @@ static int step_check(const ckks_ctx* c, const he_scan_desc* d) {
     return scan_check(c, d ? &one : nullptr, 0);
 }
 static u32 step_batch(const ckks_ctx* c, const he_scan_desc* d, bool turned) { return even_batch(d->channels, turned ? turned_batch(c) : ks_batch(c)); }
-static size_t ws_step(const ckks_ctx* c, const he_scan_desc* d, bool turned) {
-    const u32 nb = step_batch(c, d, turned);
-    return turned ? ws_turned(c, d->level, nb) : ws_product_add(c, d->level, nb);
+static size_t ws_step(const ckks_ctx* c, const he_scan_desc* d) {  // with or without a rotation
+    const size_t a = ws_turned(c, d->level, step_batch(c, d, true), false), b = ws_product_add(c, d->level, step_batch(c, d, false));
+    return a > b ? a : b;
 }
 size_t he_scan_step_workspace_bytes(const ckks_ctx* c, const he_scan_desc* d) {
     if (!c || step_check(c, d)) return 0;
-    const size_t a = ws_step(c, d, true), b = ws_step(c, d, false);
-    return a > b ? a : b;
+    return ws_step(c, d);
 }
 int he_scan_step(const ckks_ctx* c, const he_scan_desc* d, int64_t k, const he_ct_array* gate, const he_ct_array* state, const he_ct_array* x, const ckks_key* rot_key,
                  const ckks_key* cross_key, uint64_t* d_out, void* d_ws, size_t ws_bytes, void* stream) {
@@ -2803,7 +2839,7 @@ int he_scan_step(const ckks_ctx* c, const he_scan_desc* d, int64_t k, const he_c
     const bool add = x && x->d;
     if (add)
         if (int rc = check_array(c, x, d->channels, level + 1, 2)) return rc;
-    if (!d_ws || ws_bytes < ws_step(c, d, turned)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the step");
+    if (!d_ws || ws_bytes < ws_step(c, d)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the step");
     const u32 nb = step_batch(c, d, turned);
     for (u32 c0 = 0; c0 < d->channels; c0 += nb) {
         const u32 n = d->channels - c0 < nb ? d->channels - c0 : nb;

@@ -229,9 +229,9 @@ enum NttPasses { NTT_BOTH = 0, NTT_LO, NTT_HI };
 hipError_t launch_ntt(const ckks_ctx* c, bool inverse, const u64* src, size_t src_bstride, u64* dst,
                       size_t dst_bstride, const PolyList& pl, u32 batch, hipStream_t st, const u64* const* src_ptrs = nullptr,
                       const FwdEpilogue* epilogue = nullptr, const TwF* inv_scale = nullptr, const u64* const* mul_ptrs = nullptr,
-                      const u64* lin_k = nullptr, NttPasses passes = NTT_BOTH, const u32* gals = nullptr);
+                      const u64* lin_k = nullptr, NttPasses passes = NTT_BOTH, const u32* gals = nullptr, bool gal_mul_only = false);
 // gals (inverse, with src_ptrs, contexts with ntt_has_modup): batch item b is sigma_gals[b] of src_ptrs[b], gathered on load; with mul_ptrs
-// (without lin_k) sigma_gals[b] of the product
+// (without lin_k) sigma_gals[b] of the product, or (gal_mul_only) src_ptrs[b] (.) sigma_gals[b](mul_ptrs[b])
 // passes (inverse, two-pass rings): the first pass alone (a kernel that goes on from there follows: ntt_mid_*), or the second alone, in place
 // (the first has been done: launch_ntt_lo_mac with inv_from)
 // mul_ptrs (inverse, with src_ptrs, double-precision arithmetic): batch item b is src_ptrs[b] (.) mul_ptrs[b], formed on load;
@@ -329,9 +329,25 @@ struct MacDivide {
     u64* const* outs;
     const u64* const* adds;  // or null
 };
+// turn: two key switches an item, of polynomials 2b and 2b + 1 of the digits, the first with keys[b], the second with key2.  Of the product of (a0, a1) with the rotation by g
+// of (h0, h1), which exist nowhere (launch_ntt with gal_mul_only): a0 sigma(h1) and a1 sigma(h1), with the addends P (a0 sigma(h0) + k x0), P (a1 sigma(h0) + k x1) where add[b]
+// is set, without k x elsewhere (x[b] is then any readable ciphertext); or (stored) of h0 and h1 themselves, with P a0 and P a1.
+struct MacTurn {
+    const u64* const* a0;
+    const u64* const* a1;
+    const u64* const* h0;
+    const u64* const* h1;
+    const u64* key2;
+    u32 g;
+    bool stored;
+    const u64* const* x = nullptr;
+    size_t x_cstride = 0;
+    const bool* add = nullptr;
+    const u64* k = nullptr;  // one residue per limb
+};
 hipError_t launch_ntt_lo_mac(const ckks_ctx* c, u32 level, const DigitSrc& digits, const u64* const* keys, u64* const* outs, u32 n,
                              hipStream_t st, u32 inv_from, const MacProduct* prod = nullptr, const MacRotate* rot = nullptr, u32* n_part = nullptr,
-                             const MacDivide* div = nullptr, bool dropped_only = false);
+                             const MacDivide* div = nullptr, bool dropped_only = false, const MacTurn* turn = nullptr);
 // the division by P of the sum of n such items, one result: the item's `acc` is added, times `mask` if there is one
 hipError_t launch_ntt_moddown_sum(const ckks_ctx* c, u32 level, u64* v, size_t v_bstride, u32 n, u32 n_part, u64* w, const FinalItem& item, hipStream_t st);
 // rings whose whole transforms run as one kernel (the whole limb-poly in one workgroup); key switches and rescales take them pass by

@@ -259,7 +259,8 @@ struct NttArgs {
     PtrList8 src_list;
     PtrList8 mul_list;     // inverse, first pass, product variant: batch item b is src_list.p[b] (.) mul_list.p[b]
     u64 lin_ka, lin_kb;    // use_lin: ... is lin_ka * src_list.p[b] + lin_kb * mul_list.p[b] instead (one limb per item)
-    u32 use_lin, pad2;
+    u32 use_lin;
+    u32 gal_mul_only;      // inverse, first pass, automorphism variant with a product: mul_list.p[b] alone is under sigma_gal[b]
     // loop variant of the forward lo pass, ModUp: the items are (polynomial, digit) pairs, digits fastest, `beta` of them per
     // polynomial; limb e <= level is transformed for every digit but the one it belongs to, e / alpha (0: plain items)
     u32 beta, alpha, level, pad3;
@@ -691,6 +692,11 @@ struct MacEpilogue {
     PtrList8 lx, ly;
     size_t x_cstride, y_cstride;
     u64 ka[CKKS_MAX_MODULI], kb[CKKS_MAX_MODULI];
+    // TURN: two key switches an item, whose digits follow each other (2 beta rows), with the keys `key` and `key2`.  1: the product of (a0, a1) with the rotation
+    // by gal[b] of (b0, b1): the decomposed polynomials are a0 sigma(b1) and a1 sigma(b1), the addends a0 sigma(b0) + kx x0, a1 sigma(b0) + kx x1, kx = ka where
+    // turn_add[b] is set and zero elsewhere ((x0, x1) = lx with x_cstride); 2: they are stored, b0 and b1, and so are the addends, a0 and a1
+    PtrList8 key2;
+    u32 turn_add[KS_MAX_BATCH];
     // MASK (with SUM): the rotated ciphertext is the product of (a0, D.own) with mask [level+1][N]
     const u64* mask;
     // DIV: the division's last step instead of stores: w are the converted dropped parts behind the first pass of their forward transform
@@ -883,18 +889,19 @@ __global__ __launch_bounds__(NTT_THREADS) void ntt_fwd_lo_vec_kernel(NttArgs arg
     }
 }
 
-// PROD, LIN, ROT, SUM, MASK, DIV, HOIST (see MacEpilogue) are template arguments so that what follows the digits is straight-line code: with the
+// PROD, LIN, ROT, SUM, MASK, DIV, HOIST, TURN (see MacEpilogue) are template arguments so that what follows the digits is straight-line code: with the
 // operands behind conditions, even ones that are the same for the whole launch, the compiler keeps each request next to its
 // use, one round trip to memory per point.
-template <bool PROD, bool LIN, bool ROT, bool SUM = false, bool MASK = false, bool DIV = false, bool HOIST = false>
-__global__ __launch_bounds__(NTT_THREADS) void ntt_fwd_lo_mac_kernel(NttArgs args, PolyList pl, MacEpilogue ep) {
+template <bool PROD, bool LIN, bool ROT, bool SUM = false, bool MASK = false, bool DIV = false, bool HOIST = false, int TURN = 0>
+__global__ __launch_bounds__(NTT_THREADS, TURN ? 2 : 1) void ntt_fwd_lo_mac_kernel(NttArgs args, PolyList pl, MacEpilogue ep) {
     typedef ArithF64 A;
     typedef double E;
     __shared__ E lds0[LDS_PADDED_WORDS];
     __shared__ E lds1[LDS_PADDED_WORDS];
     const u32 tid = threadIdx.x;
     const LoTile tile = lo_tile(args.log_hi, args.lo_group);
-    static_assert((!DIV || !SUM) && (!HOIST || (ROT && !SUM)), "");
+    static_assert((!DIV || !SUM) && (!HOIST || (ROT && !SUM)) && (!TURN || (!PROD && !ROT && !LIN)), "");
+    constexpr bool LATE = LIN || TURN != 0;  // ten to twelve operands a point behind the digits leave no registers for requests ahead of them
     const u32 e_at = tile.a + ep.first, e = e_at < ep.E ? e_at : e_at - ep.E;  // the dropped limbs, the longer work, first
     const u32 blk = tile.blk, m_idx = pl_at(pl.mod, e);
     // the batch items of this workgroup: tile.b, tile.b + (the grid's extent over items), ...: a workgroup that takes several
@@ -918,7 +925,9 @@ __global__ __launch_bounds__(NTT_THREADS) void ntt_fwd_lo_mac_kernel(NttArgs arg
         load_tw_w<2>(tw, 512 * TA + 2 * tid, wd);
         load_tw_w<2>(tw, 512 * TA + 2 * tid + 1, wd + 3);
     }
-    const u32 j0 = HOIST ? ep.beta : (own == 0 ? 1 : 0);  // first digit to transform
+    const u32 rows = TURN ? 2 * ep.beta : ep.beta, own2 = TURN && own < ep.beta ? ep.beta + own : 0xffffffffu;
+    u32 j0 = HOIST ? ep.beta : (own == 0 ? 1 : 0);  // first digit to transform
+    if (TURN && j0 == own2) j0++;
     E v[8], raw[8];
     // DIV: the converted parts of item b
     auto request_w = [&](u32 b, u32 comp) {
@@ -927,11 +936,11 @@ __global__ __launch_bounds__(NTT_THREADS) void ntt_fwd_lo_mac_kernel(NttArgs arg
         for (int i = 0; i < 8; i++) raw[i] = w[tid + 256 * i];
     };
     auto request_first = [&](u32 b) {  // the first points of item b
-        if (j0 < ep.beta) {
+        if (j0 < rows) {
             const double* hi0 = (const double*)(ep.D.digits + b * ep.D.bstride) + (size_t)e * N + off;
 #pragma unroll
             for (int i = 0; i < 8; i++) raw[i] = hi0[(size_t)j0 * dstride + tid + 256 * i];
-        } else if (DIV && !LIN) {
+        } else if (DIV && !LATE) {
             request_w(b, 0);
         }
     };
@@ -941,21 +950,23 @@ __global__ __launch_bounds__(NTT_THREADS) void ntt_fwd_lo_mac_kernel(NttArgs arg
     E acc0[8], acc1[8];
     for (u32 b = tile.b; b < args.batch; b += b_step) {
     const u64* key = ep.key.p[b] + (size_t)m_idx * N + off;
+    const u64* key2 = TURN ? ep.key2.p[b] + (size_t)m_idx * N + off : nullptr;
     const double* hi = (const double*)(ep.D.digits + b * ep.D.bstride) + (size_t)e * N + off;
     if (!SUM || b == tile.b || !summed) {  // a sum over items starts from the last one's reduced sum (f64m_sum_due: so it may)
 #pragma unroll
         for (int j = 0; j < 8; j++) acc0[j] = acc1[j] = 0.0;
     }
     u32 j = j0;
-    while (j < ep.beta) {
+    while (j < rows) {
         u32 jn = j + 1;
         if (jn == own) jn++;
+        if (TURN && jn == own2) jn++;
 #pragma unroll
         for (int i = 0; i < 8; i++) v[i] = raw[i];
-        if (jn < ep.beta) {  // the next digit's points, a tile ahead
+        if (jn < rows) {  // the next digit's points, a tile ahead
 #pragma unroll
             for (int i = 0; i < 8; i++) raw[i] = hi[(size_t)jn * dstride + tid + 256 * i];
-        } else if (DIV && !LIN) {
+        } else if (DIV && !LATE) {
             request_w(b, 0);
         }
         A::fwd_begin(v, mc);
@@ -982,7 +993,7 @@ __global__ __launch_bounds__(NTT_THREADS) void ntt_fwd_lo_mac_kernel(NttArgs arg
         // the key words of this digit at the points this thread ends up with: requested now, needed after the last round
         u64 k0[8], k1[8];
         {
-            const u64* kj = key + (size_t)j * 2 * kstride;
+            const u64* kj = (TURN && j >= ep.beta ? key2 + (size_t)(j - ep.beta) * 2 * kstride : key + (size_t)j * 2 * kstride);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 k0[i] = kj[tid + 256 * i];
@@ -1013,8 +1024,46 @@ __global__ __launch_bounds__(NTT_THREADS) void ntt_fwd_lo_mac_kernel(NttArgs arg
     auto request_next = [&]() {
         if (b + b_step < args.batch) request_first(b + b_step);
     };
-    if (!LIN && !DIV) request_next();
-    if (PROD && e <= ep.level) {
+    if (!LATE && !DIV) request_next();
+    if constexpr (TURN != 0) {
+        // the two polynomials of the item at a limb of their own, each with its key; P times the addends.  Sums: at most 5.5 q from the digits (f64m_sum_due), 0.75 q for each of
+        // the two own-limb products, 0.63 q for the addend's
+        if (e <= ep.level) {
+            const size_t po = (size_t)e * N;
+            const u64 *ku = key + (size_t)own * 2 * kstride - off, *kv = key2 + (size_t)own * 2 * kstride - off;
+            const u64 *pa0 = ep.a0.p[b] + po, *pa1 = ep.a1.p[b] + po, *ph0 = ep.b0.p[b] + po, *ph1 = ep.b1.p[b] + po, *px = TURN == 1 ? ep.lx.p[b] + po : nullptr;
+            const double pres = mc.q - A::from_u64(ep.negp[e]), kx = TURN == 1 && ep.turn_add[b] ? A::from_u64(ep.ka[e]) : 0.0;
+            u32 x0 = (u32)off + tid;
+            constexpr int HP = 2;
+#pragma unroll
+            for (int h = 0; h < 8; h += HP) {
+                asm volatile("" : "+v"(x0));  // no request of these points before the ones before are used: registers
+                u64 ra0[HP], ra1[HP], rh0[HP], rh1[HP], rx0[HP], rx1[HP], ru0[HP], ru1[HP], rv0[HP], rv1[HP];
+#pragma unroll
+                for (int i = 0; i < HP; i++) {
+                    const u32 x = x0 + 256 * (h + i), xs = TURN == 1 ? galois_gather_index(x, ep.gal[b], args.log_n) : x;
+                    ra0[i] = word_at(pa0, x), ra1[i] = word_at(pa1, x);
+                    rh0[i] = word_at(ph0, xs), rh1[i] = word_at(ph1, xs);
+                    if (TURN == 1) rx0[i] = word_at(px, x), rx1[i] = word_at(px + ep.x_cstride, x);
+                    ru0[i] = word_at(ku, x), ru1[i] = word_at(ku + kstride, x), rv0[i] = word_at(kv, x), rv1[i] = word_at(kv + kstride, x);
+                }
+#pragma unroll
+                for (int i = 0; i < HP; i++) {
+                    double u = A::from_u64(rh0[i]), w = A::from_u64(rh1[i]), dd0 = A::from_u64(ra0[i]), dd1 = A::from_u64(ra1[i]);
+                    if (TURN == 1) {
+                        const double A0 = dd0, A1 = dd1, H0 = u, H1 = w;
+                        u = A::mulmod_any(A0, H1, mc.q, mc.qinv), w = A::mulmod_any(A1, H1, mc.q, mc.qinv);
+                        dd0 = A::mulmod_any(A0, H0, mc.q, mc.qinv) + A::mulmod_any(A::from_u64(rx0[i]), kx, mc.q, mc.qinv);
+                        dd1 = A::mulmod_any(A1, H0, mc.q, mc.qinv) + A::mulmod_any(A::from_u64(rx1[i]), kx, mc.q, mc.qinv);
+                    }
+                    dd0 = A::reduce(dd0, mc);
+                    dd1 = A::reduce(dd1, mc);
+                    acc0[h + i] += A::mulmod_any(u, A::from_u64(ru0[i]), mc.q, mc.qinv) + A::mulmod_any(w, A::from_u64(rv0[i]), mc.q, mc.qinv) + A::mulmod_any(dd0, pres, mc.q, mc.qinv);
+                    acc1[h + i] += A::mulmod_any(u, A::from_u64(ru1[i]), mc.q, mc.qinv) + A::mulmod_any(w, A::from_u64(rv1[i]), mc.q, mc.qinv) + A::mulmod_any(dd1, pres, mc.q, mc.qinv);
+                }
+            }
+        }
+    } else if (PROD && e <= ep.level) {
         // the tensor product of this slice, formed here: d2 feeds the digit that owns the limb, P d0 and P d1 join the sums
         const u64* kj = key + (size_t)own * 2 * kstride;
         const size_t po = (size_t)e * N + off;
@@ -1126,8 +1175,8 @@ __global__ __launch_bounds__(NTT_THREADS) void ntt_fwd_lo_mac_kernel(NttArgs arg
             }
         }
     }
-    if (LIN && DIV) request_w(b, 0);
-    if (LIN && !DIV) request_next();
+    if (LATE && DIV) request_w(b, 0);
+    if (LATE && !DIV) request_next();
     u64* o0 = ep.out.p[summed ? tile.b : b] + (size_t)e * N + off;
     u64* o1 = o0 + (size_t)ep.E * N;
 #pragma unroll
@@ -1212,8 +1261,9 @@ __device__ __forceinline__ void load_permuted(const u64* __restrict__ poly, u32 
 
 // MUL (double-precision arithmetic, first pass, source list): the transform's input is the pointwise product of two
 // polynomials (the d2 = a1 (.) b1 of a ciphertext product), formed as the points are loaded: d2 itself is never stored.
-// GAL (likewise): it is the polynomial under the item's automorphism, gathered as it is loaded (with MUL: the product under it).
-template <class A, int IT, bool MUL = false, bool GAL = false>
+// GAL = 1 (likewise): it is the polynomial under the item's automorphism, gathered as it is loaded (with MUL: the product under it).  GAL = 2 (with MUL): the
+// multiplier alone is under it.
+template <class A, int IT, bool MUL = false, int GAL = 0>
 __global__ __launch_bounds__(NTT_THREADS) __attribute__((amdgpu_waves_per_eu(3, 8))) void ntt_inv_lo_kernel(NttArgs args, PolyList pl) {
     static_assert(!MUL || IT == 1, "the variants with two operands take one item");
     typedef typename A::E E;
@@ -1236,8 +1286,15 @@ __global__ __launch_bounds__(NTT_THREADS) __attribute__((amdgpu_waves_per_eu(3, 
     load_lo_tw<A, 2>(P, 512 * TA + 2 * tid + 1, wd + 3);
     load_lo_tw<A, 3>(P, 64 * TA + 8 * d3 + d2, wc);
     const size_t moff = ((size_t)pl_at(pl.spos, tile.a) << args.log_n) + off + 8 * tid;  // MUL: the multiplier's point
+    static_assert(GAL != 2 || MUL, "a multiplier");
     if constexpr (GAL) {
-        load_permuted(P.src, (u32)off + 8 * tid, args.gal[b0], args.log_n, raw);
+        if constexpr (GAL == 2) {
+            const ulonglong2* in = reinterpret_cast<const ulonglong2*>(P.src + off + 8 * tid);
+#pragma unroll
+            for (int j = 0; j < 4; j++) raw[j] = in[j];
+        } else {
+            load_permuted(P.src, (u32)off + 8 * tid, args.gal[b0], args.log_n, raw);
+        }
         if constexpr (MUL) load_permuted(args.mul_list.p[b0] + ((size_t)pl_at(pl.spos, tile.a) << args.log_n), (u32)off + 8 * tid, args.gal[b0], args.log_n, raw2);
     } else {
         const ulonglong2* in = reinterpret_cast<const ulonglong2*>(P.src + off + 8 * tid);
@@ -2235,13 +2292,17 @@ template <class A, int IT>
 static void launch_inv_lo_it(dim3 grid, hipStream_t st, const NttArgs& args, const PolyList& pl, bool mul, bool gal) {
     if constexpr (std::is_same<A, ArithF64>::value) {
         if constexpr (IT == 1) {
+            if (gal && mul && args.gal_mul_only) {
+                hipLaunchKernelGGL((ntt_inv_lo_kernel<A, IT, true, 2>), grid, dim3(NTT_THREADS), 0, st, args, pl);
+                return;
+            }
             if (gal && mul) {
-                hipLaunchKernelGGL((ntt_inv_lo_kernel<A, IT, true, true>), grid, dim3(NTT_THREADS), 0, st, args, pl);
+                hipLaunchKernelGGL((ntt_inv_lo_kernel<A, IT, true, 1>), grid, dim3(NTT_THREADS), 0, st, args, pl);
                 return;
             }
         }
         if (gal) {
-            hipLaunchKernelGGL((ntt_inv_lo_kernel<A, IT, false, true>), grid, dim3(NTT_THREADS), 0, st, args, pl);
+            hipLaunchKernelGGL((ntt_inv_lo_kernel<A, IT, false, 1>), grid, dim3(NTT_THREADS), 0, st, args, pl);
             return;
         }
     }
@@ -2455,7 +2516,8 @@ static hipError_t launch_ntt_any(const ckks_ctx* c, bool inverse, const u64* src
                                  size_t dst_bstride, const PolyList& pl, u32 batch, hipStream_t st, const u64* const* src_ptrs,
                                  const FwdEpilogue* epilogue, const TwF* inv_scale, const ConvPrologue* conv,
                                  const u64* const* mul_ptrs = nullptr, const u64* lin_k = nullptr, NttPasses passes = NTT_BOTH,
-                                 const MidPrologue* mid = nullptr, const u32* gals = nullptr) {
+                                 const MidPrologue* mid = nullptr, const u32* gals = nullptr, bool gal_mul_only = false) {
+    if (gal_mul_only && (!gals || !mul_ptrs)) return hipErrorInvalidValue;
     if (pl.n == 0 || batch == 0) return hipSuccess;
     if (passes != NTT_BOTH && ((!inverse && (!conv || epilogue || passes != NTT_HI)) || c->log_hi < 1)) return hipErrorInvalidValue;
     if (passes == NTT_HI && (src != dst || src_ptrs || (ntt_one_pass(c) && !mid))) return hipErrorInvalidValue;
@@ -2501,7 +2563,7 @@ static hipError_t launch_ntt_any(const ckks_ctx* c, bool inverse, const u64* src
     args.use_lin = lin_k ? 1 : 0;
     args.lin_ka = lin_k ? lin_k[0] : 0;
     args.lin_kb = lin_k ? lin_k[1] : 0;
-    args.pad2 = 0;
+    args.gal_mul_only = gal_mul_only ? 1 : 0;
     args.beta = args.alpha = args.level = args.pad3 = 0;
     const u32 polys = pl.n * batch;
     const dim3 block(NTT_THREADS);
@@ -2590,8 +2652,8 @@ static hipError_t launch_ntt_any(const ckks_ctx* c, bool inverse, const u64* src
 
 hipError_t launch_ntt(const ckks_ctx* c, bool inverse, const u64* src, size_t src_bstride, u64* dst, size_t dst_bstride,
                       const PolyList& pl, u32 batch, hipStream_t st, const u64* const* src_ptrs, const FwdEpilogue* epilogue,
-                      const TwF* inv_scale, const u64* const* mul_ptrs, const u64* lin_k, NttPasses passes, const u32* gals) {
-    return launch_ntt_any(c, inverse, src, src_bstride, dst, dst_bstride, pl, batch, st, src_ptrs, epilogue, inv_scale, nullptr, mul_ptrs, lin_k, passes, nullptr, gals);
+                      const TwF* inv_scale, const u64* const* mul_ptrs, const u64* lin_k, NttPasses passes, const u32* gals, bool gal_mul_only) {
+    return launch_ntt_any(c, inverse, src, src_bstride, dst, dst_bstride, pl, batch, st, src_ptrs, epilogue, inv_scale, nullptr, mul_ptrs, lin_k, passes, nullptr, gals, gal_mul_only);
 }
 
 // Small launches take all digits at once: one converting hi pass and (unless the inner product takes it from there) one lo pass,
@@ -2828,8 +2890,9 @@ hipError_t launch_ntt_rescale_vec(const ckks_ctx* c, u32 level, VecMode mode, co
 }
 
 hipError_t launch_ntt_lo_mac(const ckks_ctx* c, u32 level, const DigitSrc& digits, const u64* const* keys, u64* const* outs, u32 n,
-                             hipStream_t st, u32 inv_from, const MacProduct* prod, const MacRotate* rot, u32* n_part, const MacDivide* div, bool dropped_only) {
-    if ((div || dropped_only) && (n_part || inv_from == 0 || inv_from >= c->ext_limbs(level) || (!prod && !rot))) return hipErrorInvalidValue;
+                             hipStream_t st, u32 inv_from, const MacProduct* prod, const MacRotate* rot, u32* n_part, const MacDivide* div, bool dropped_only, const MacTurn* turn) {
+    if ((div || dropped_only) && (n_part || inv_from == 0 || inv_from >= c->ext_limbs(level) || (!prod && !rot && !turn))) return hipErrorInvalidValue;
+    if (turn && (prod || rot || n_part || (!turn->stored && (!turn->x || !turn->k)))) return hipErrorInvalidValue;
     if (!ntt_has_modup(c) || (n_part && !rot) || (rot && rot->mask && !n_part) || (rot && rot->hoisted && n_part) || c->log_hi == 0 || n == 0 || n > KS_MAX_BATCH || (prod && rot)) return hipErrorInvalidValue;
     const u32 E = c->ext_limbs(level), beta = c->live_digits(level);
     NttArgs args = {};
@@ -2856,10 +2919,19 @@ hipError_t launch_ntt_lo_mac(const ckks_ctx* c, u32 level, const DigitSrc& digit
         if (b < n && !ep.key.p[b]) return hipErrorInvalidValue;
         ep.a0.p[b] = b < n ? (prod ? prod->a0[b] : (rot ? rot->c0[b] : nullptr)) : nullptr;
         ep.gal[b] = (rot && b < n) ? rot->gs[b] : 1;
+        ep.key2.p[b] = nullptr;
+        ep.turn_add[b] = 0;
         if (rot && b < n && !ep.a0.p[b]) return hipErrorInvalidValue;
         ep.a1.p[b] = (prod && b < n) ? prod->a1[b] : nullptr;
         ep.b0.p[b] = (prod && b < n) ? prod->b0[b] : nullptr;
         ep.b1.p[b] = (prod && b < n) ? prod->b1[b] : nullptr;
+        if (turn && b < n) {
+            ep.a0.p[b] = turn->a0[b], ep.a1.p[b] = turn->a1[b], ep.b0.p[b] = turn->h0[b], ep.b1.p[b] = turn->h1[b];
+            ep.key2.p[b] = turn->key2;
+            ep.gal[b] = turn->g;
+            ep.turn_add[b] = turn->stored || !turn->add ? 0 : (turn->add[b] ? 1 : 0);
+            if (!ep.a0.p[b] || !ep.a1.p[b] || !ep.b0.p[b] || !ep.b1.p[b] || !turn->key2) return hipErrorInvalidValue;
+        }
         if (prod && b < n && (!ep.a0.p[b] || !ep.a1.p[b] || !ep.b0.p[b] || !ep.b1.p[b])) return hipErrorInvalidValue;
         if (b < n && (b == 0 || keys[b] != keys[b - 1])) n_keys += 1.0;
         if (rot && b < n && (b == 0 || rot->c0[b] != rot->c0[b - 1])) n_src += 1.0;
@@ -2882,15 +2954,16 @@ hipError_t launch_ntt_lo_mac(const ckks_ctx* c, u32 level, const DigitSrc& digit
     ep.mask = rot ? rot->mask : nullptr;
     const bool lin = prod && prod->lin_x;
     if (lin && (!prod->lin_y || !prod->ka || !prod->kb)) return hipErrorInvalidValue;
-    ep.x_cstride = lin ? prod->x_cstride : 0;
+    ep.x_cstride = lin ? prod->x_cstride : (turn && !turn->stored ? turn->x_cstride : 0);
     ep.y_cstride = lin ? prod->y_cstride : 0;
     for (u32 b = 0; b < KS_MAX_BATCH; b++) {
-        ep.lx.p[b] = (lin && b < n) ? prod->lin_x[b] : nullptr;
+        ep.lx.p[b] = (lin && b < n) ? prod->lin_x[b] : (turn && !turn->stored && b < n ? turn->x[b] : nullptr);
+        if (turn && !turn->stored && b < n && !ep.lx.p[b]) return hipErrorInvalidValue;
         ep.ly.p[b] = (lin && b < n) ? prod->lin_y[b] : nullptr;
         if (lin && b < n && (!ep.lx.p[b] || !ep.ly.p[b])) return hipErrorInvalidValue;
     }
     for (u32 i = 0; i < CKKS_MAX_MODULI; i++) {
-        ep.ka[i] = (lin && i <= level) ? prod->ka[i] : 0;
+        ep.ka[i] = (lin && i <= level) ? prod->ka[i] : (turn && !turn->stored && i <= level ? turn->k[i] : 0);
         ep.kb[i] = (lin && i <= level) ? prod->kb[i] : 0;
     }
     // the grid's extent over the batch: two, i.e. four items per workgroup in a batch of eight (measured: 16.5 ms per step for
@@ -2907,9 +2980,9 @@ hipError_t launch_ntt_lo_mac(const ckks_ctx* c, u32 level, const DigitSrc& digit
     const bool hoisted = rot && rot->hoisted;
     const double np = div ? inv_from : (dropped_only ? E - inv_from : E), kept = dropped_only ? 0.0 : (inv_from < E ? inv_from : E), inverse = div ? 0.0 : np - kept;
     const double live = div ? inv_from : (dropped_only ? level + 1.0 - inv_from : level + 1.0);
-    const double rows = beta * np - live, n_tr = hoisted ? 0.0 : n * rows;  // n_tr: transformed
-    double words = (hoisted ? 1.0 : (double)n) * rows + n_keys * 2.0 * beta * np + (rot && rot->mask ? live : 0.0);
-    words += live * (prod ? (lin ? 8.0 : 4.0) * n : (rot ? 2.0 * n_src : 1.0 * n));  // (lin: two components of two ciphertexts)
+    const double sets = turn ? 2.0 : 1.0, rows = sets * (beta * np - live), n_tr = hoisted ? 0.0 : n * rows;  // n_tr: transformed
+    double words = (hoisted ? 1.0 : (double)n) * rows + sets * n_keys * 2.0 * beta * np + (rot && rot->mask ? live : 0.0);
+    words += live * (turn ? (turn->stored ? 4.0 : 6.0) * n : prod ? (lin ? 8.0 : 4.0) * n : (rot ? 2.0 * n_src : 1.0 * n));  // (lin: two components of two ciphertexts)
     words += 2.0 * (n * inverse + (n_part ? b_ext : n) * kept);
     if (div) words += 2.0 * kept * (n + n_add);
     ProfScope ps__(c, K_NTT_FWD_LO, st, 8.0 * c->N * words, 0.5 * c->N * c->log_lo * (n_tr + 2.0 * n * (inverse + (div ? kept : 0.0))));
@@ -2918,6 +2991,13 @@ hipError_t launch_ntt_lo_mac(const ckks_ctx* c, u32 level, const DigitSrc& digit
     if (rot && rot->hoisted) {
         if (div) LO_MAC_LAUNCH(false, false, true, false, false, true, true);
         else LO_MAC_LAUNCH(false, false, true, false, false, false, true);
+        return hipGetLastError();
+    }
+    if (turn) {
+        if (turn->stored && div) LO_MAC_LAUNCH(false, false, false, false, false, true, false, 2);
+        else if (turn->stored) LO_MAC_LAUNCH(false, false, false, false, false, false, false, 2);
+        else if (div) LO_MAC_LAUNCH(false, false, false, false, false, true, false, 1);
+        else LO_MAC_LAUNCH(false, false, false, false, false, false, false, 1);
         return hipGetLastError();
     }
     if (div) {

@@ -352,8 +352,6 @@ def test_nothing_is_written_beside_outputs_and_workspace(name, ring):
 def test_a_workspace_of_a_byte_less_is_refused(name):
     ctx, ops = calls()
     call, need, shapes = ops[name]
-    if name == "step_in_place":  # (the query covers both forms)
-        need = 256
     bufs, outs = outputs(shapes)
     with pytest.raises(hx.CkksError) as e:
         call(torch.empty(need - 1, dtype=torch.uint8, device="cuda"), outs)
