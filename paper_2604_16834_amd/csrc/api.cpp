@@ -2959,14 +2959,14 @@ static int layer_norm_grad_check(const ckks_ctx* c, const he_layer_norm_grad_des
     if (!level_ok(c, d->level) || d->level < 3 + d->affine) return set_err(c, CKKS_ERR_LEVEL_MISMATCH, "layer norm's backward pass needs 3 <= level < num_q, with a gain one more");
     return CKKS_OK;
 }
-static u32 slot_sum_batch(u32 n) { return even_batch(n, CT_BATCH); }
-static size_t ws_slot_sum(const ckks_ctx* c, u32 level, u32 n) { return ws_ks(c, level, n, 2 * n); }
-// z[b] <- z[b] + the sum of its rotations by the keys, n <= CT_BATCH ciphertexts [2][level + 1][N]
+// ciphertexts of a batch of sums over slots
+static u32 slot_sum_batch(const ckks_ctx* c, u32 n) { return even_batch(n, ks_batch(c)); }
+static size_t ws_slot_sum(const ckks_ctx* c, u32 level, u32 n) { return ws_ks(c, level, n, c->small_q ? n : 2 * n); }
+// z[b] <- z[b] + the sum of its rotations by the keys, n <= ks_batch ciphertexts [2][level + 1][N]: one decomposition, and one division for all rotations
 static int run_slot_sum(const ckks_ctx* c, u32 level, u32 n, u64* const* z, const ckks_key* const* keys, u32 n_keys, Arena ar, hipStream_t st) {
     KsWs ws;
-    if (!carve_ks(c, level, n, 2 * n, ar, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for sums over slots");
-    const u64 *c0s[KS_MAX_BATCH], *c1s[KS_MAX_BATCH], *kd[KS_MAX_BATCH];
-    u32 gs[KS_MAX_BATCH];
+    if (!carve_ks(c, level, n, c->small_q ? n : 2 * n, ar, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for sums over slots");
+    const u64 *c0s[KS_MAX_BATCH], *c1s[KS_MAX_BATCH];
     FinalItem items[KS_MAX_BATCH];
     for (u32 b = 0; b < n; b++) {
         c0s[b] = z[b];
@@ -2974,16 +2974,30 @@ static int run_slot_sum(const ckks_ctx* c, u32 level, u32 n, u64* const* z, cons
         items[b] = FinalItem{nullptr, nullptr, nullptr, z[b], 1, 0, z[b]};
     }
     if (int rc = run_modup(c, level, c1s, n, ws, st)) return rc;
-    for (u32 i = 0; i < n_keys; i++) {
-        for (u32 b = 0; b < n; b++) kd[b] = keys[i]->d_key, gs[b] = keys[i]->galois_elt;
-        HIP_TRY(launch_key_inner_items(c, level, dsrc(c, ws, 0), kd, gs, c0s, ws.v + (i ? n : 0) * ws.v_b, ws.v_b, n, st));
-        if (i) HIP_TRY(launch_add_ext(c, level, ws.v, ws.v + n * ws.v_b, 2 * n, st));
+    if (c->small_q) {
+        u64* vs[KS_MAX_BATCH];
+        for (u32 b = 0; b < n; b++) vs[b] = ws.v + b * ws.v_b;
+        for (u32 k0 = 0; k0 < n_keys; k0 += ROT_SUM_KEYS) {
+            const u32 m = n_keys - k0 < ROT_SUM_KEYS ? n_keys - k0 : ROT_SUM_KEYS;
+            const u64* kd[ROT_SUM_KEYS];
+            u32 gs[ROT_SUM_KEYS];
+            for (u32 i = 0; i < m; i++) kd[i] = keys[k0 + i]->d_key, gs[i] = keys[k0 + i]->galois_elt;
+            HIP_TRY(launch_rot_sum(c, level, dsrc(c, ws, 0), kd, gs, m, c0s, vs, n, k0 != 0, st));
+        }
+    } else {
+        const u64* kd[KS_MAX_BATCH];
+        u32 gs[KS_MAX_BATCH];
+        for (u32 i = 0; i < n_keys; i++) {
+            for (u32 b = 0; b < n; b++) kd[b] = keys[i]->d_key, gs[b] = keys[i]->galois_elt;
+            HIP_TRY(launch_key_inner_items(c, level, dsrc(c, ws, 0), kd, gs, c0s, ws.v + (i ? n : 0) * ws.v_b, ws.v_b, n, st));
+            if (i) HIP_TRY(launch_add_ext(c, level, ws.v, ws.v + n * ws.v_b, 2 * n, st));
+        }
     }
     return run_moddown(c, level, ws, n, items, st);
 }
 static size_t ws_layer_norm_grad(const ckks_ctx* c, const he_layer_norm_grad_desc* d) {
     const size_t N = c->N, level = d->level, bg = level - d->affine;
-    const u32 nb = even_batch(d->channels, ks_batch(c)), ns = slot_sum_batch(d->channels);
+    const u32 nb = even_batch(d->channels, ks_batch(c)), ns = slot_sum_batch(c, 2 * d->channels);
     size_t sub = ws_ctct(c, d->level, nb), t;
     if ((t = ws_ks(c, (u32)bg, 1, 1)) > sub) sub = t;
     if ((t = blk(3 * nb * (bg - 1) * N) + ws_ks(c, (u32)bg - 2, nb, nb)) > sub) sub = t;
@@ -3101,16 +3115,14 @@ int he_layer_norm_backward(const ckks_ctx* c, const he_layer_norm_grad_desc* d, 
         }
     }
     if (!sums) return CKKS_OK;
-    const u32 ns = slot_sum_batch(C);
-    for (u64* z : {(u64*)d_dgain, (u64*)d_dbias}) {
-        if (!z) continue;
-        for (u32 c0 = 0; c0 < C; c0 += ns) {
-            const u32 n = C - c0 < ns ? C - c0 : ns;
-            u64* pz[KS_MAX_BATCH];
-            for (u32 b = 0; b < n; b++) pz[b] = z + (size_t)(c0 + b) * wct;
-            for (u32 i = 0, k = 0; i < d->n_stages; k += h_stage_rots[i], i++)
-                if (int rc = run_slot_sum(c, level - 1, n, pz, sum_keys + k, h_stage_rots[i], ar.rest(), st)) return rc;
-        }
+    u64* halves[2] = {(u64*)(d_dgain ? d_dgain : d_dbias), (u64*)(d_dgain ? d_dbias : nullptr)};
+    const u32 total = halves[1] ? 2 * C : C, ns = slot_sum_batch(c, total);
+    for (u32 c0 = 0; c0 < total; c0 += ns) {  // both gradients' ciphertexts in the same launches
+        const u32 n = total - c0 < ns ? total - c0 : ns;
+        u64* pz[KS_MAX_BATCH];
+        for (u32 b = 0; b < n; b++) pz[b] = halves[(c0 + b) / C] + (size_t)((c0 + b) % C) * wct;
+        for (u32 i = 0, k = 0; i < d->n_stages; k += h_stage_rots[i], i++)
+            if (int rc = run_slot_sum(c, level - 1, n, pz, sum_keys + k, h_stage_rots[i], ar.rest(), st)) return rc;
     }
     return CKKS_OK;
 }

@@ -179,6 +179,130 @@ hipError_t launch_norm_grad_terms(const ckks_ctx* c, u32 level, const NormGradTe
     return hipGetLastError();
 }
 
+// ---- sums of rotations on the extended basis -------------------------------------------------------------------
+// out_b = sum_r (P sigma_r(c0_b) + <sigma_r(digits_b), key_r>_0, <sigma_r(digits_b), key_r>_1), b < n: what one stage of a sum over slots divides by P once.  Moduli below 2^50: the
+// sums as chains of eight fused multiply-adds on centred doubles (f64m_chain_add).  A thread holds both components of one destination point of NB ciphertexts, so that a
+// key word is read once for them, and gathers their digits through each automorphism in turn (a wavefront's 64 points are one aligned run of 512 bytes); the operands of the next
+// digit are requested before the present one's are used.  Workgroups are dealt to the eight dies in turn: each die takes a contiguous eighth of the (limb, points) list, so that what
+// the rotations gather again comes from its own L2 cache.
+struct RotSumKeys {
+    const u64* key[ROT_SUM_KEYS];
+    u32 g[ROT_SUM_KEYS];
+    u32 n;
+};
+template <int NB>
+__global__ __launch_bounds__(RC_THREADS) void rot_sum_kernel(DigitSrc digits, RotSumKeys K, PtrList8 c0s, OutList8 out, u32 add, const u64* __restrict__ negp,
+                                                             const ModConstF* __restrict__ mcf, u32 log_n, u32 level, u32 num_q, u32 M, u32 E, u32 beta, u32 n) {
+    const u32 N = 1u << log_n, nxb = (N + RC_THREADS - 1) / RC_THREADS;
+    const u32 list = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3), e = list / nxb, b0 = blockIdx.y * NB;
+    if (e >= E) return;  // whole workgroup
+    const u32 x = list % nxb * RC_THREADS + threadIdx.x;
+    if (x >= N) return;
+    const u32 t = e <= level ? e : num_q + (e - level - 1), own = e <= level ? e / digits.alpha : 0xffffffffu;
+    const double q = mcf[t].q, qinv = mcf[t].qinv;
+    const u32 terms = beta + (e <= level ? 1 : 0);  // the digits, then c0 (P c0 is zero on the special primes)
+    auto centred = [&](u64 v) {
+        const double d = f64m_from_u64(v);
+        return d > 0.5 * q ? d - q : d;
+    };
+    const double pres = e <= level ? centred((u64)q - negp[e]) : 0.0;
+    const u64* rows[NB];  // digit 0's row of every ciphertext
+#pragma unroll
+    for (int i = 0; i < NB; i++) rows[i] = digits.digits + (b0 + i < n ? b0 + i : n - 1) * digits.bstride + (size_t)e * N;
+    u64 dv[NB], k0 = 0, k1 = 0;
+    u32 xs = 0;
+    auto load = [&](u32 r, u32 j) {
+        if (j == 0) xs = galois_gather_index(x, K.g[r], log_n);
+        if (j < beta) {
+            const u64* kp = K.key[r] + ((size_t)2 * j * M + t) * N + x;
+            k0 = kp[0];
+            k1 = kp[(size_t)M * N];
+        }
+#pragma unroll
+        for (int i = 0; i < NB; i++) {
+            const u32 b = b0 + i < n ? b0 + i : n - 1;
+            const u64* row = j == beta ? c0s.p[b] + (size_t)e * N : (j == own ? digits.own.p[b] + (size_t)e * N : rows[i] + (size_t)j * E * N);
+            dv[i] = row[xs];
+        }
+    };
+    double sum[2][NB], ct[2][NB], cl[2][NB];
+    auto begin = [&]() {
+#pragma unroll
+        for (int c = 0; c < 2; c++)
+#pragma unroll
+            for (int i = 0; i < NB; i++) ct[c][i] = F64M_DOT_BASE, cl[c][i] = 0.0;
+    };
+    auto join = [&]() {
+#pragma unroll
+        for (int c = 0; c < 2; c++)
+#pragma unroll
+            for (int i = 0; i < NB; i++) sum[c][i] = f64m_reduce(sum[c][i] + f64m_chain_join(ct[c][i], cl[c][i], q, qinv), q, qinv);
+    };
+#pragma unroll
+    for (int c = 0; c < 2; c++)
+#pragma unroll
+        for (int i = 0; i < NB; i++) sum[c][i] = 0.0;
+    begin();
+    load(0, 0);
+    u32 r = 0, j = 0, count = 0;
+    while (r < K.n) {
+        double y[NB];
+        const bool key = j < beta;
+        const double w0 = key ? centred(k0) : pres, w1 = centred(k1);
+#pragma unroll
+        for (int i = 0; i < NB; i++) y[i] = centred(dv[i]);
+        if (++j == terms) j = 0, r++;
+        if (r < K.n) load(r, j);
+#pragma unroll
+        for (int i = 0; i < NB; i++) f64m_chain_add(ct[0][i], cl[0][i], y[i], w0);
+        if (key) {  // uniform
+#pragma unroll
+            for (int i = 0; i < NB; i++) f64m_chain_add(ct[1][i], cl[1][i], y[i], w1);
+        }
+        if (++count == 8) {  // uniform
+            join();
+            begin();
+            count = 0;
+        }
+    }
+    join();
+#pragma unroll
+    for (int i = 0; i < NB; i++) {
+        if (b0 + i >= n) break;
+        u64* o = out.p[b0 + i] + (size_t)e * N + x;
+#pragma unroll
+        for (int c = 0; c < 2; c++) {
+            u64* oc = o + (size_t)c * E * N;
+            const double v = add ? f64m_reduce(sum[c][i] + f64m_from_u64(*oc), q, qinv) : sum[c][i];
+            *oc = f64m_canonical(v, q);
+        }
+    }
+}
+
+hipError_t launch_rot_sum(const ckks_ctx* c, u32 level, const DigitSrc& digits, const u64* const* keys, const u32* gs, u32 n_keys, const u64* const* c0s, u64* const* outs, u32 n,
+                          bool add, hipStream_t st) {
+    if (!c->small_q || n == 0 || n > KS_MAX_BATCH || n_keys == 0 || n_keys > ROT_SUM_KEYS) return hipErrorInvalidValue;
+    const u32 E = c->ext_limbs(level), beta = c->live_digits(level), nxb = (c->N + RC_THREADS - 1) / RC_THREADS;
+    RotSumKeys K = {};
+    K.n = n_keys;
+    for (u32 r = 0; r < n_keys; r++) K.key[r] = keys[r], K.g[r] = gs[r];
+    PtrList8 cl;
+    OutList8 ol;
+    for (u32 b = 0; b < KS_MAX_BATCH; b++) cl.p[b] = b < n ? c0s[b] : nullptr, ol.p[b] = b < n ? outs[b] : nullptr;
+    const u64* negp = c->d_moddown + 2 * c->k_pad + (size_t)c->k_pad * c->num_q + 2 * c->num_q;
+    u32 nb = 8;
+    while (nb > 1 && (nb / 2 >= n || (u64)nxb * E * ((n + nb - 1) / nb) < 1024)) nb /= 2;
+    const dim3 grid((nxb * E + 7) / 8 * 8, (n + nb - 1) / nb);
+    ProfScope ps__(c, K_KEY_INNER, st, 8.0 * c->N * (E * (n * (beta + (add ? 4.0 : 2.0)) + n_keys * 2.0 * beta * grid.y) + n * (level + 1.0)), 2.0 * n_keys * n * c->N * E * beta);
+#define ROT_SUM(NB_) hipLaunchKernelGGL(rot_sum_kernel<NB_>, grid, dim3(RC_THREADS), 0, st, digits, K, cl, ol, add ? 1u : 0u, negp, c->d_mcf, c->log_n, level, c->num_q, c->M, E, beta, n)
+    if (nb == 8) ROT_SUM(8);
+    else if (nb == 4) ROT_SUM(4);
+    else if (nb == 2) ROT_SUM(2);
+    else ROT_SUM(1);
+#undef ROT_SUM
+    return hipGetLastError();
+}
+
 // ---- sums on the extended basis, copies ------------------------------------------------------------------------
 // v += w, n polynomials [E][N] each
 __global__ __launch_bounds__(RC_THREADS) void add_ext_kernel(u64* __restrict__ v, const u64* __restrict__ w, const ModConst* __restrict__ mc, u32 N, u32 level, u32 num_q) {
