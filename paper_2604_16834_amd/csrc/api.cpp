@@ -281,7 +281,7 @@ int run_inner_divide(const ckks_ctx* c, u32 level, const KsWs& ws, const u64* co
     u64* vs[KS_MAX_BATCH];
     for (u32 b = 0; b < n; b++) vs[b] = ws.v + b * ws.v_b;
     DigitSrc digits = dsrc(c, ws, 0);
-    if (turn) digits.bstride *= 2;  // two polynomials an item
+    if (turn && !turn->one) digits.bstride *= 2;  // two polynomials an item
     const u32 from = dropped_from(level, merged);
     const u32 slices = from * n << c->log_hi;
     if (rot && rot->hoisted ? slices < DIVIDE_INSIDE_HOISTED : c->log_hi < 2 || slices < DIVIDE_INSIDE_SLICES) {
@@ -2295,6 +2295,30 @@ int he_rope_axes(const ckks_ctx* c, const he_rope_desc* d, const he_ct_array* in
     return CKKS_OK;
 }
 
+// outs[b] = ((d0[b], d1[b]) + KeySwitch(d2[b])) / q_level for n <= ks_batch stored tensor products, level -> level - 1: one division by P q_level.  Scratch: ws_ks(level, n, n).
+static int run_relinearise(const ckks_ctx* c, u32 level, u32 n, const u64* const* d0, const u64* const* d1, const u64* const* d2, const u64* d_rlk, u64* const* outs, Arena ar,
+                           hipStream_t st) {
+    KsWs ws;
+    if (!carve_ks(c, level, n, n, ar, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for a relinearisation");
+    const bool mac = ntt_has_modup(c);
+    if (int rc = run_modup(c, level, d2, n, ws, st, mac)) return rc;
+    if (mac) {
+        const u64* keys[KS_MAX_BATCH];
+        for (u32 b = 0; b < n; b++) keys[b] = d_rlk;
+        MacTurn sum = {d0, d1, d2, nullptr, nullptr, 1, true};
+        sum.one = true;
+        return run_inner_divide(c, level, ws, keys, n, outs, nullptr, st, true, nullptr, nullptr, 0, &sum);
+    }
+    u64* vs[KS_MAX_BATCH];
+    FinalItem items[KS_MAX_BATCH];
+    for (u32 b = 0; b < n; b++) {
+        vs[b] = ws.v + b * ws.v_b;
+        items[b] = FinalItem{nullptr, nullptr, nullptr, outs[b], 1, 0, nullptr};
+    }
+    HIP_TRY(launch_key_inner_ext(c, level, dsrc(c, ws, 0), d_rlk, 1, d0, d1, nullptr, vs, n, st));
+    return run_moddown(c, level, ws, n, items, st, true);
+}
+
 // k times q_lv: a constant k joins a quotient by B exactly as B k joins the dividend (it vanishes modulo every dropped limb), and the addends of the inner product
 // are multiplied by P already
 static LimbScalars times_limb(const ckks_ctx* c, int64_t k, u32 lv) {
@@ -2317,15 +2341,8 @@ static int run_inverse_root(const ckks_ctx* c, u32 level, u32 iterations, int64_
     const size_t N = c->N, L1 = level + 1;
     int rc;
     {
-        KsWs ws;
-        Arena sub = ar;
-        if (!carve_ks(c, level, 1, 1, sub, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the norm");
         const u64 *d0 = sq3, *d1 = sq3 + L1 * N, *d2 = sq3 + 2 * L1 * N;
-        u64* v = ws.v;
-        if ((rc = run_modup(c, level, &d2, 1, ws, st))) return rc;
-        HIP_TRY(launch_key_inner_ext(c, level, dsrc(c, ws, 0), d_rlk, 1, &d0, &d1, nullptr, &v, 1, st));
-        const FinalItem item = {nullptr, nullptr, nullptr, s, 1, 0, nullptr};
-        if ((rc = run_moddown(c, level, ws, 1, &item, st, true))) return rc;
+        if ((rc = run_relinearise(c, level, 1, &d0, &d1, &d2, d_rlk, &s, ar, st))) return rc;
     }
     // the first guess
     const size_t ss = (size_t)level * N;  // component stride of s
@@ -2626,6 +2643,43 @@ static int run_turned(const ckks_ctx* c, u32 level, u32 n, const u64* const* a, 
     return run_inner_divide(c, level, ws, keys, n, outs, nullptr, st, true, nullptr, nullptr, 0, &turn);
 }
 
+// Batches that do not depend on each other, every other one on the context's second stream between a fork and a join (see ckks_ctx_set_overlap).
+struct Lanes {
+    const ckks_ctx* c;
+    hipStream_t st;
+    bool two;
+    int fork() const {
+        if (!two) return CKKS_OK;
+        HIP_TRY(hipEventRecord(c->ev_fork, st));
+        HIP_TRY(hipStreamWaitEvent(c->side, c->ev_fork, 0));
+        return CKKS_OK;
+    }
+    int join(int rc) const {  // also on the error paths: the caller's stream never runs ahead of the second one
+        if (!two) return rc;
+        hipError_t e = hipEventRecord(c->ev_join, c->side);
+        if (e == hipSuccess) e = hipStreamWaitEvent(st, c->ev_join, 0);
+        if (e != hipSuccess && rc == CKKS_OK) return set_hip_err(c, e);
+        return rc;
+    }
+    hipStream_t at(u32 batch) const { return two && (batch & 1) ? c->side : st; }
+};
+// Whether n key switches at `level`, up to `most` in a batch, are dealt to the two streams: the kernels of one batch, which leave a part of the chip idle between their phases of
+// arithmetic and of memory traffic, fill up beside another's.  Fork and join cost 45 us, and batches of half the size share less.  By coefficients of the extended basis (millions), one stream /
+// two in us.  More than a batch: steps of 10 channels of 14 + 5 limbs at N = 2^12 (0.8) 112 / 103, at 2^13 (1.6) 147 / 117, at 2^16 (12.5) 821 / 728, of 24 at 24 + 8 limbs (50) 3114 / 2966; norms of 24
+// with gain at 2^12 (1.2) 389 / 357, at 2^16 (20) 2032 / 1805; a norm's backward pass of 17 at 2^12 (1.3) 807 / 676.  One batch or less, in halves: steps of 8 at 2^12 (0.6) 65 / 95, at 2^14 (2.5)
+// 174 / 176, at 2^15 (5.0) 346 / 321; scans of 6 channels and 2 gates in six steps at 2^14 (2.5) 841 / 871, at 2^15 (5.0) 1607 / 1537; a norm's backward pass of 5 at 2^14 (3.1) 793 / 815, at 2^15 (6.2)
+// 1401 / 1350.  (Workspaces are sized for both streams, ckks_ctx_set_overlap on or off.)
+static bool lanes_pay(const ckks_ctx* c, u32 level, u32 n, u32 most) {
+    const u64 size = (u64)n * c->N * c->ext_limbs(level);
+    return c->side && ntt_has_modup(c) && n > 1 && size >= (u64)1 << (n > most ? 19 : 22);
+}
+// n in batches of nearly the same size, at most `most`; of an even number of them for two streams
+static u32 even_batch(u32 n, u32 most, bool two = false) {
+    u32 parts = (n + most - 1) / most;
+    if (two && n > 1) parts += parts & 1;
+    return (n + parts - 1) / parts;
+}
+
 static int scan_check(const ckks_ctx* c, const he_scan_desc* d, u32 deeper) {
     if (!d) return set_err(c, CKKS_ERR_INVALID_ARG, "null descriptor");
     if (d->channels == 0 || d->channels > 65536 || d->heads == 0 || d->channels % d->heads) return set_err(c, CKKS_ERR_INVALID_ARG, "need 1 to 65536 channels, a multiple of the heads");
@@ -2643,38 +2697,45 @@ static int check_turn_keys(const ckks_ctx* c, const ckks_key* rot, const ckks_ke
     if (rot->galois_elt != g || cross->galois_elt != (CKKS_KEY_CROSS | g)) return set_err(c, CKKS_ERR_NO_KEY, "a rotation's key or its cross key was made for another offset");
     return CKKS_OK;
 }
-static u32 even_batch(u32 n, u32 most) { return (n + (n + most - 1) / most - 1) / ((n + most - 1) / most); }
 
 // the rows that a scan turns, gates before channels, in two buffers in turn
 static size_t scan_rows(const ckks_ctx* c, const he_scan_desc* d) { return ((size_t)d->heads + d->channels) * 2 * d->level * c->N; }
 // most rows of a step that go together: the last step has no gates, and its batches may be larger for it
-static u32 scan_batch(const ckks_ctx* c, const he_scan_desc* d) {
-    const u32 all = even_batch(d->heads + d->channels, turned_batch(c)), last = even_batch(d->channels, turned_batch(c));
+static bool scan_two(const ckks_ctx* c, const he_scan_desc* d) { return lanes_pay(c, d->level, d->heads + d->channels, turned_batch(c)); }
+static u32 scan_batch(const ckks_ctx* c, const he_scan_desc* d, bool two) {
+    const u32 all = even_batch(d->heads + d->channels, turned_batch(c), two), last = even_batch(d->channels, turned_batch(c), two);
     return all > last ? all : last;
 }
 static size_t ws_scan(const ckks_ctx* c, const he_scan_desc* d) {
-    return (d->steps > 1 ? blk(scan_rows(c, d)) : 0) + (d->steps > 2 ? blk(scan_rows(c, d)) : 0) + ws_turned(c, d->level, scan_batch(c, d), false);
+    const bool two = scan_two(c, d);
+    return (d->steps > 1 ? blk(scan_rows(c, d)) : 0) + (d->steps > 2 ? blk(scan_rows(c, d)) : 0) + (two ? 2 : 1) * ws_turned(c, d->level, scan_batch(c, d, two), false);
 }
 static int run_scan(const ckks_ctx* c, const he_scan_desc* d, bool forward, const int64_t* h_k, const he_ct_array& x, const he_ct_array& gate, const ckks_key* const* rot_keys,
                     const ckks_key* const* cross_keys, u64* d_out, Arena ar, hipStream_t st) {
     const size_t N = c->N;
     const u32 per = d->channels / d->heads;
     u64* buf[2] = {d->steps > 1 ? ar.take(scan_rows(c, d)) : nullptr, d->steps > 2 ? ar.take(scan_rows(c, d)) : nullptr};
+    const bool two = c->side_stream() && scan_two(c, d);
+    const size_t lane = ws_turned(c, d->level, scan_batch(c, d, two), false);
+    const Lanes lanes = {c, st, two};
+    const Arena part[2] = {Arena(ar.take(lane / sizeof(u64)), lane), lanes.two ? Arena(ar.take(lane / sizeof(u64)), lane) : Arena(nullptr, 0)};
     if (!ar.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the scan");
     he_ct_array hs = x, as = gate;
     for (u32 s = 0; s < d->steps; s++) {
         const u32 level = d->level - s, first = s + 1 < d->steps ? 0 : d->heads, rows = d->heads + d->channels;  // (nothing follows that would read the last step's gates)
-        const u32 nb = even_batch(rows - first, turned_batch(c)), g = scan_element(c, d, s, forward);
+        const u32 nb = even_batch(rows - first, turned_batch(c), two), g = scan_element(c, d, s, forward);
         const size_t ct = (size_t)2 * level * N;  // of the step's results
         u64* next = s + 1 < d->steps ? buf[s & 1] : d_out;  // from row `first` on
-        for (u32 r0 = first; r0 < rows; r0 += nb) {
+        if (int rc = lanes.fork()) return rc;
+        int rc = CKKS_OK;
+        for (u32 r0 = first, no = 0; r0 < rows && rc == CKKS_OK; r0 += nb, no++) {
             const u32 n = rows - r0 < nb ? rows - r0 : nb;
             const u64 *pa[KS_MAX_BATCH], *ph[KS_MAX_BATCH], *px[KS_MAX_BATCH];
             u64* po[KS_MAX_BATCH];
             // gates and channels of one batch differ in their strides while they are the caller's: components are then a batch's own
             u32 m = n;
             if (r0 < d->heads && r0 + n > d->heads && as.comp_stride != hs.comp_stride) m = d->heads - r0;
-            for (u32 done = 0; done < n; done += m, m = n - done) {
+            for (u32 done = 0; done < n && rc == CKKS_OK; done += m, m = n - done) {
                 for (u32 b = 0; b < m; b++) {
                     const u32 row = r0 + done + b, ch = row - d->heads;
                     const bool is_gate = row < d->heads;
@@ -2684,9 +2745,10 @@ static int run_scan(const ckks_ctx* c, const he_scan_desc* d, bool forward, cons
                     po[b] = next + (size_t)(row - first) * ct;
                 }
                 const size_t h_comp = r0 + done < d->heads ? as.comp_stride : hs.comp_stride;
-                if (int rc = run_turned(c, level, m, pa, as.comp_stride, ph, h_comp, g, h_k[s], px, h_comp, rot_keys[s]->d_key, cross_keys[s]->d_key, po, ar.rest(), st)) return rc;
+                rc = run_turned(c, level, m, pa, as.comp_stride, ph, h_comp, g, h_k[s], px, h_comp, rot_keys[s]->d_key, cross_keys[s]->d_key, po, part[lanes.two ? no & 1 : 0], lanes.at(no));
             }
         }
+        if ((rc = lanes.join(rc))) return rc;
         as = he_ct_array{(const uint64_t*)next, ct, (size_t)level * N};
         hs = he_ct_array{(const uint64_t*)(next + d->heads * ct), ct, (size_t)level * N};
     }
@@ -2811,14 +2873,19 @@ static int step_check(const ckks_ctx* c, const he_scan_desc* d) {
     one.steps = 1;
     return scan_check(c, d ? &one : nullptr, 0);
 }
-static u32 step_batch(const ckks_ctx* c, const he_scan_desc* d, bool turned) { return even_batch(d->channels, turned ? turned_batch(c) : ks_batch(c)); }
-static size_t ws_step(const ckks_ctx* c, const he_scan_desc* d) {  // with or without a rotation
-    const size_t a = ws_turned(c, d->level, step_batch(c, d, true), false), b = ws_product_add(c, d->level, step_batch(c, d, false));
+static u32 step_batch(const ckks_ctx* c, const he_scan_desc* d, bool turned, bool two) { return even_batch(d->channels, turned ? turned_batch(c) : ks_batch(c), two); }
+static size_t ws_step(const ckks_ctx* c, const he_scan_desc* d, bool turned, bool two) {
+    const u32 nb = step_batch(c, d, turned, two);
+    return (two ? 2 : 1) * (turned ? ws_turned(c, d->level, nb, false) : ws_product_add(c, d->level, nb));
+}
+static bool step_two(const ckks_ctx* c, const he_scan_desc* d, bool turned) { return lanes_pay(c, d->level, d->channels, turned ? turned_batch(c) : ks_batch(c)); }
+static size_t ws_step_any(const ckks_ctx* c, const he_scan_desc* d) {  // with or without a rotation
+    const size_t a = ws_step(c, d, true, step_two(c, d, true)), b = ws_step(c, d, false, step_two(c, d, false));
     return a > b ? a : b;
 }
 size_t he_scan_step_workspace_bytes(const ckks_ctx* c, const he_scan_desc* d) {
     if (!c || step_check(c, d)) return 0;
-    return ws_step(c, d);
+    return ws_step_any(c, d);
 }
 int he_scan_step(const ckks_ctx* c, const he_scan_desc* d, int64_t k, const he_ct_array* gate, const he_ct_array* state, const he_ct_array* x, const ckks_key* rot_key,
                  const ckks_key* cross_key, uint64_t* d_out, void* d_ws, size_t ws_bytes, void* stream) {
@@ -2839,9 +2906,16 @@ int he_scan_step(const ckks_ctx* c, const he_scan_desc* d, int64_t k, const he_c
     const bool add = x && x->d;
     if (add)
         if (int rc = check_array(c, x, d->channels, level + 1, 2)) return rc;
-    if (!d_ws || ws_bytes < ws_step(c, d)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the step");
-    const u32 nb = step_batch(c, d, turned);
-    for (u32 c0 = 0; c0 < d->channels; c0 += nb) {
+    if (!d_ws || ws_bytes < ws_step_any(c, d)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the step");
+    hipStream_t st = (hipStream_t)stream;
+    const bool two = c->side_stream() && step_two(c, d, turned);
+    const u32 nb = step_batch(c, d, turned, two);
+    const size_t lane = two ? ws_step(c, d, turned, true) / 2 : ws_bytes;
+    const Lanes lanes = {c, st, two};
+    if (int rc = lanes.fork()) return rc;
+    int rc = CKKS_OK;
+    for (u32 c0 = 0, no = 0; c0 < d->channels && rc == CKKS_OK; c0 += nb, no++) {
+        const Arena part((char*)d_ws + (lanes.two && (no & 1) ? lane : 0), lane);
         const u32 n = d->channels - c0 < nb ? d->channels - c0 : nb;
         const u64 *pa[KS_MAX_BATCH], *ph[KS_MAX_BATCH], *px[KS_MAX_BATCH];
         u64* po[KS_MAX_BATCH];
@@ -2852,16 +2926,13 @@ int he_scan_step(const ckks_ctx* c, const he_scan_desc* d, int64_t k, const he_c
             po[b] = (u64*)d_out + (size_t)(c0 + b) * 2 * level * c->N;
         }
         const size_t x_comp = add ? x->comp_stride : 0;
-        int rc;
         if (turned)
-            rc = run_turned(c, level, n, pa, gate->comp_stride, ph, state->comp_stride, rot_key->galois_elt, k, add ? px : nullptr, x_comp, rot_key->d_key, cross_key->d_key, po,
-                            Arena(d_ws, ws_bytes), (hipStream_t)stream);
+            rc = run_turned(c, level, n, pa, gate->comp_stride, ph, state->comp_stride, rot_key->galois_elt, k, add ? px : nullptr, x_comp, rot_key->d_key, cross_key->d_key, po, part,
+                            lanes.at(no));
         else
-            rc = run_product_add(c, level, n, pa, gate->comp_stride, ph, state->comp_stride, k, add ? px : nullptr, x_comp, cross_key->d_key, po, Arena(d_ws, ws_bytes),
-                                 (hipStream_t)stream);
-        if (rc) return rc;
+            rc = run_product_add(c, level, n, pa, gate->comp_stride, ph, state->comp_stride, k, add ? px : nullptr, x_comp, cross_key->d_key, po, part, lanes.at(no));
     }
-    return CKKS_OK;
+    return lanes.join(rc);
 }
 
 // ---- layer norm ----
@@ -2880,13 +2951,18 @@ static int layer_norm_check(const ckks_ctx* c, const he_layer_norm_desc* d) {
         return set_err(c, CKKS_ERR_LEVEL_MISMATCH, "layer norm needs 3 + 2 iterations <= level < num_q, with a gain one more");
     return CKKS_OK;
 }
-static size_t ws_layer_norm(const ckks_ctx* c, const he_layer_norm_desc* d) {
-    const size_t N = c->N, L1 = d->level + 1, m = d->level - 2 - 2 * d->iterations;
-    const u32 nb = even_batch(d->channels, ks_batch(c));
-    size_t sub = ws_inverse_root(c, d->level, d->iterations), t;
-    if ((t = blk((size_t)nb * 2 * (m + 1) * N) + ws_ctct(c, (u32)m, nb)) > sub) sub = t;
+static bool layer_norm_two(const ckks_ctx* c, const he_layer_norm_desc* d) { return lanes_pay(c, d->level - 2 - 2 * d->iterations, d->channels, ks_batch(c)); }
+static size_t ws_layer_norm_lane(const ckks_ctx* c, const he_layer_norm_desc* d, bool two) {
+    const size_t N = c->N, m = d->level - 2 - 2 * d->iterations;
+    const u32 nb = even_batch(d->channels, ks_batch(c), two);
+    size_t sub = blk((size_t)nb * 2 * (m + 1) * N) + ws_ctct(c, (u32)m, nb), t;
     if (d->affine && (t = ws_product_add(c, (u32)m - 1, nb)) > sub) sub = t;
-    return blk(3 * L1 * N) + 3 * blk(2 * L1 * N) + 3 * blk(2 * N * d->level) + sub;
+    return sub;
+}
+static size_t ws_layer_norm(const ckks_ctx* c, const he_layer_norm_desc* d) {
+    const bool two = layer_norm_two(c, d);
+    const size_t N = c->N, L1 = d->level + 1, root = ws_inverse_root(c, d->level, d->iterations), lanes = (two ? 2 : 1) * ws_layer_norm_lane(c, d, two);
+    return blk(3 * L1 * N) + 3 * blk(2 * L1 * N) + 3 * blk(2 * N * d->level) + (root > lanes ? root : lanes);
 }
 size_t he_layer_norm_workspace_bytes(const ckks_ctx* c, const he_layer_norm_desc* d) {
     if (!c || layer_norm_check(c, d)) return 0;
@@ -2923,31 +2999,36 @@ int he_layer_norm(const ckks_ctx* c, const he_layer_norm_desc* d, const int64_t*
     HIP_TRY(launch_centred_squares(c, level, (const u64*)x->d, x->ct_stride, x->comp_stride, C, times_limb(c, d->k_eps, level), sq3, sum, st));
     if (int rc = run_inverse_root(c, level, d->iterations, d->k_slope, d->k_start, h_k_newton, rlk->d_key, sq3, s, u, w, ra, rb, ar.rest(), st)) return rc;
     if (d_inv) HIP_TRY(launch_copy(ra, (u64*)d_inv, (size_t)2 * (m + 1) * N, st));
-    const u32 nb = even_batch(C, ks_batch(c));
-    const size_t rs = (size_t)(m + 1) * N, norm_ct = (size_t)2 * m * N, out_ct = (size_t)2 * (m - 1) * N;
-    for (u32 c0 = 0; c0 < C; c0 += nb) {
-        const u32 n = C - c0 < nb ? C - c0 : nb;
-        Arena sub = ar.rest();
+    const bool two = c->side_stream() && layer_norm_two(c, d);
+    const u32 nb = even_batch(C, ks_batch(c), two);
+    const size_t rs = (size_t)(m + 1) * N, norm_ct = (size_t)2 * m * N, out_ct = (size_t)2 * (m - 1) * N, lane = ws_layer_norm_lane(c, d, two);
+    const Arena part[2] = {Arena(ar.take(lane / sizeof(u64)), lane), two ? Arena(ar.take(lane / sizeof(u64)), lane) : Arena(nullptr, 0)};
+    if (!ar.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the layer norm");
+    auto run_batch = [&](u32 c0, u32 n, Arena all, hipStream_t on) -> int {
+        Arena sub = all;
         u64* y = sub.take(n * 2 * rs);
         if (!sub.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the layer norm");
-        HIP_TRY(launch_centre(c, m + 1, n, (const u64*)x->d + (size_t)c0 * x->ct_stride, x->ct_stride, x->comp_stride, C, sum, L1 * N, y, st));
+        HIP_TRY(launch_centre(c, m + 1, n, (const u64*)x->d + (size_t)c0 * x->ct_stride, x->ct_stride, x->comp_stride, C, sum, L1 * N, y, on));
         const u64 *py[KS_MAX_BATCH], *pr[KS_MAX_BATCH], *pg[KS_MAX_BATCH], *pn[KS_MAX_BATCH], *pb[KS_MAX_BATCH];
-        u64 *on[KS_MAX_BATCH], *oo[KS_MAX_BATCH];
+        u64 *on_[KS_MAX_BATCH], *oo[KS_MAX_BATCH];
         for (u32 b = 0; b < n; b++) {
             py[b] = y + b * 2 * rs;
             pr[b] = ra;
-            on[b] = (u64*)d_norm + (size_t)(c0 + b) * norm_ct;
-            pn[b] = on[b];
+            on_[b] = (u64*)d_norm + (size_t)(c0 + b) * norm_ct;
+            pn[b] = on_[b];
             pg[b] = d->affine ? (const u64*)gain->d + (size_t)(c0 + b) * gain->ct_stride : nullptr;
             pb[b] = add ? (const u64*)bias->d + (size_t)(c0 + b) * bias->ct_stride : nullptr;
             oo[b] = d->affine ? (u64*)d_out + (size_t)(c0 + b) * out_ct : nullptr;
         }
-        if (int rc = run_ctct_merged(c, m, py, rs, pr, rs, nullptr, 0, rlk->d_key, on, n, sub.rest(), st)) return rc;
-        if (!d->affine) continue;
-        if (int rc = run_product_add(c, m - 1, n, pg, gain->comp_stride, pn, (size_t)m * N, d->k_bias, add ? pb : nullptr, add ? bias->comp_stride : 0, rlk->d_key, oo, ar.rest(), st))
-            return rc;
-    }
-    return CKKS_OK;
+        if (int e = run_ctct_merged(c, m, py, rs, pr, rs, nullptr, 0, rlk->d_key, on_, n, sub.rest(), on)) return e;
+        if (!d->affine) return CKKS_OK;
+        return run_product_add(c, m - 1, n, pg, gain->comp_stride, pn, (size_t)m * N, d->k_bias, add ? pb : nullptr, add ? bias->comp_stride : 0, rlk->d_key, oo, all, on);
+    };
+    const Lanes lanes = {c, st, two};
+    if (int rc = lanes.fork()) return rc;
+    int rc = CKKS_OK;
+    for (u32 c0 = 0, no = 0; c0 < C && rc == CKKS_OK; c0 += nb, no++) rc = run_batch(c0, C - c0 < nb ? C - c0 : nb, part[two ? no & 1 : 0], lanes.at(no));
+    return lanes.join(rc);
 }
 
 static int layer_norm_grad_check(const ckks_ctx* c, const he_layer_norm_grad_desc* d) {
@@ -2959,8 +3040,6 @@ static int layer_norm_grad_check(const ckks_ctx* c, const he_layer_norm_grad_des
     if (!level_ok(c, d->level) || d->level < 3 + d->affine) return set_err(c, CKKS_ERR_LEVEL_MISMATCH, "layer norm's backward pass needs 3 <= level < num_q, with a gain one more");
     return CKKS_OK;
 }
-// ciphertexts of a batch of sums over slots
-static u32 slot_sum_batch(const ckks_ctx* c, u32 n) { return even_batch(n, ks_batch(c)); }
 static size_t ws_slot_sum(const ckks_ctx* c, u32 level, u32 n) { return ws_ks(c, level, n, c->small_q ? n : 2 * n); }
 // z[b] <- z[b] + the sum of its rotations by the keys, n <= ks_batch ciphertexts [2][level + 1][N]: one decomposition, and one division for all rotations
 static int run_slot_sum(const ckks_ctx* c, u32 level, u32 n, u64* const* z, const ckks_key* const* keys, u32 n_keys, Arena ar, hipStream_t st) {
@@ -2995,14 +3074,21 @@ static int run_slot_sum(const ckks_ctx* c, u32 level, u32 n, u64* const* z, cons
     }
     return run_moddown(c, level, ws, n, items, st);
 }
-static size_t ws_layer_norm_grad(const ckks_ctx* c, const he_layer_norm_grad_desc* d) {
-    const size_t N = c->N, level = d->level, bg = level - d->affine;
-    const u32 nb = even_batch(d->channels, ks_batch(c)), ns = slot_sum_batch(c, 2 * d->channels);
+// the channels' batches in turn on two streams: with a gradient of gain or bias to be summed, each stream takes half of the ciphertexts through all stages
+static bool layer_norm_grad_two(const ckks_ctx* c, const he_layer_norm_grad_desc* d) { return lanes_pay(c, d->level, 2 * d->channels, ks_batch(c)); }
+static size_t ws_layer_norm_grad_lane(const ckks_ctx* c, const he_layer_norm_grad_desc* d, bool two) {
+    const size_t N = c->N, bg = d->level - d->affine;
+    const u32 nb = even_batch(d->channels, ks_batch(c), two), both = even_batch(2 * d->channels, ks_batch(c), two);
     size_t sub = ws_ctct(c, d->level, nb), t;
     if ((t = ws_ks(c, (u32)bg, 1, 1)) > sub) sub = t;
     if ((t = blk(3 * nb * (bg - 1) * N) + ws_ks(c, (u32)bg - 2, nb, nb)) > sub) sub = t;
-    if (d->n_stages && (t = ws_slot_sum(c, d->level - 1, ns)) > sub) sub = t;
-    return (d->affine ? blk((size_t)d->channels * 2 * level * N) : 0) + blk(3 * (bg + 1) * N) + blk(2 * (bg + 1) * N) + 2 * blk(2 * bg * N) + sub;
+    if (d->n_stages && (t = ws_slot_sum(c, d->level - 1, nb > both ? nb : both)) > sub) sub = t;
+    return sub;
+}
+static size_t ws_layer_norm_grad(const ckks_ctx* c, const he_layer_norm_grad_desc* d) {
+    const bool two = layer_norm_grad_two(c, d);
+    const size_t N = c->N, level = d->level, bg = level - d->affine;
+    return (d->affine ? blk((size_t)d->channels * 2 * level * N) : 0) + blk(3 * (bg + 1) * N) + blk(2 * (bg + 1) * N) + 2 * blk(2 * bg * N) + (two ? 2 : 1) * ws_layer_norm_grad_lane(c, d, two);
 }
 size_t he_layer_norm_backward_workspace_bytes(const ckks_ctx* c, const he_layer_norm_grad_desc* d) {
     if (!c || layer_norm_grad_check(c, d)) return 0;
@@ -3036,24 +3122,36 @@ int he_layer_norm_backward(const ckks_ctx* c, const he_layer_norm_grad_desc* d, 
     if (!d_ws || ws_bytes < ws_layer_norm_grad(c, d)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the layer norm's backward pass");
     hipStream_t st = (hipStream_t)stream;
     const size_t N = c->N;
-    const u32 nb = even_batch(C, ks_batch(c));
+    const bool two = c->side_stream() && layer_norm_grad_two(c, d);
+    const u32 nb = even_batch(C, ks_batch(c), two);
     Arena ar(d_ws, ws_bytes);
     u64* g = d->affine ? ar.take((size_t)C * 2 * level * N) : nullptr;
     u64* dot3 = ar.take(3 * (size_t)(bg + 1) * N);
     u64* sum = ar.take(2 * (size_t)(bg + 1) * N);
     u64* dot = ar.take(2 * (size_t)bg * N);
     u64* t = ar.take(2 * (size_t)bg * N);
+    const size_t lane = ws_layer_norm_grad_lane(c, d, two);
+    const Arena part[2] = {Arena(ar.take(lane / sizeof(u64)), lane), two ? Arena(ar.take(lane / sizeof(u64)), lane) : Arena(nullptr, 0)};
     if (!ar.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the layer norm's backward pass");
+    const Lanes lanes = {c, st, two};
     auto at = [](const he_ct_array* a, u32 i) { return (const u64*)a->d + (size_t)i * a->ct_stride; };
+    // products of two vectors of channels, a batch
+    auto products = [&](const he_ct_array* a, const he_ct_array* b, u64* out, u32 c0, u32 n, Arena sub, hipStream_t on) -> int {
+        const u64 *pa[KS_MAX_BATCH], *pb[KS_MAX_BATCH];
+        u64* po[KS_MAX_BATCH];
+        for (u32 i = 0; i < n; i++) pa[i] = at(a, c0 + i), pb[i] = at(b, c0 + i), po[i] = out + (size_t)(c0 + i) * 2 * level * N;
+        return run_ctct_merged(c, level, pa, a->comp_stride, pb, b->comp_stride, nullptr, 0, rlk->d_key, po, n, sub, on);
+    };
+    // a batch after the other, every other one on the second stream
+    auto in_turn = [&](u32 total, u32 batch, auto&& body) -> int {
+        if (int rc = lanes.fork()) return rc;
+        int rc = CKKS_OK;
+        for (u32 c0 = 0, no = 0; c0 < total && rc == CKKS_OK; c0 += batch, no++) rc = body(c0, total - c0 < batch ? total - c0 : batch, part[two ? no & 1 : 0], lanes.at(no));
+        return lanes.join(rc);
+    };
     he_ct_array ga = *grad;
     if (d->affine) {
-        for (u32 c0 = 0; c0 < C; c0 += nb) {
-            const u32 n = C - c0 < nb ? C - c0 : nb;
-            const u64 *pa[KS_MAX_BATCH], *pb[KS_MAX_BATCH];
-            u64* po[KS_MAX_BATCH];
-            for (u32 b = 0; b < n; b++) pa[b] = at(gain, c0 + b), pb[b] = at(grad, c0 + b), po[b] = g + (size_t)(c0 + b) * 2 * level * N;
-            if (int rc = run_ctct_merged(c, level, pa, gain->comp_stride, pb, grad->comp_stride, nullptr, 0, rlk->d_key, po, n, ar.rest(), st)) return rc;
-        }
+        if (int rc = in_turn(C, nb, [&](u32 c0, u32 n, Arena sub, hipStream_t on) { return products(gain, grad, g, c0, n, sub, on); })) return rc;
         ga = he_ct_array{(const uint64_t*)g, (size_t)2 * level * N, (size_t)level * N};
     }
     // T, u and t
@@ -3061,53 +3159,30 @@ int he_layer_norm_backward(const ckks_ctx* c, const he_layer_norm_grad_desc* d, 
     const size_t poly = (size_t)(bg + 1) * N, sum_comp = (size_t)(m + 1) * N;
     TensorSum T = {(const u64*)ga.d, ga.ct_stride, ga.comp_stride, (const u64*)norm->d, norm->ct_stride, norm->comp_stride, C, 1, 1, 1, sum, m + 1, 0};
     HIP_TRY(launch_tensor_sum(c, bg, T, dot3, st));
-    auto relinearise = [&](u32 lv, const u64* terms, size_t p, u32 n, u64* const* outs, Arena sub) -> int {  // terms: n d0, n d1, n d2, p words each
-        KsWs ws;
-        if (!carve_ks(c, lv, n, n, sub, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the layer norm's backward pass");
-        const u64 *d0[KS_MAX_BATCH], *d1[KS_MAX_BATCH], *d2[KS_MAX_BATCH];
-        u64* vs[KS_MAX_BATCH];
-        FinalItem items[KS_MAX_BATCH];
-        for (u32 b = 0; b < n; b++) {
-            d0[b] = terms + b * p;
-            d1[b] = terms + (n + b) * p;
-            d2[b] = terms + (2 * n + b) * p;
-            vs[b] = ws.v + b * ws.v_b;
-            items[b] = FinalItem{nullptr, nullptr, nullptr, outs[b], 1, 0, nullptr};
-        }
-        if (int rc = run_modup(c, lv, d2, n, ws, st)) return rc;
-        HIP_TRY(launch_key_inner_ext(c, lv, dsrc(c, ws, 0), rlk->d_key, 1, d0, d1, nullptr, vs, n, st));
-        return run_moddown(c, lv, ws, n, items, st, true);
-    };
-    if (int rc = relinearise(bg, dot3, poly, 1, &dot, ar.rest())) return rc;
     {
-        const u64 *pi = (const u64*)inv->d, *pd = dot;
-        if (int rc = run_ctct_merged(c, bg - 1, &pi, inv->comp_stride, &pd, (size_t)bg * N, nullptr, 0, rlk->d_key, &t, 1, ar.rest(), st)) return rc;
+        const u64 *d0 = dot3, *d1 = dot3 + poly, *d2 = dot3 + 2 * poly, *pi = (const u64*)inv->d, *pd = dot;
+        if (int rc = run_relinearise(c, bg, 1, &d0, &d1, &d2, rlk->d_key, &dot, part[0], st)) return rc;
+        if (int rc = run_ctct_merged(c, bg - 1, &pi, inv->comp_stride, &pd, (size_t)bg * N, nullptr, 0, rlk->d_key, &t, 1, part[0], st)) return rc;
     }
     // dx
-    for (u32 c0 = 0; c0 < C; c0 += nb) {
-        const u32 n = C - c0 < nb ? C - c0 : nb;
+    const LimbScalars kg = limb_scalars(c, m, d->k_grad), kn = limb_scalars(c, m, d->k_norm);
+    int rc = in_turn(C, nb, [&](u32 c0, u32 n, Arena sub, hipStream_t on) -> int {
         const size_t p = (size_t)(m + 1) * N;
-        Arena sub = ar.rest();
-        u64* terms = sub.take(3 * n * p);
+        u64* terms = sub.take(3 * n * p);  // n d0, n d1, n d2
         if (!sub.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the layer norm's backward pass");
         const NormGradTerms G = {(const u64*)inv->d, inv->comp_stride, t, (size_t)(bg - 1) * N, sum, sum_comp, (const u64*)ga.d + (size_t)c0 * ga.ct_stride, ga.ct_stride, ga.comp_stride,
-                                 at(norm, c0), norm->ct_stride, norm->comp_stride, C, 0, limb_scalars(c, m, d->k_grad), limb_scalars(c, m, d->k_norm)};
-        HIP_TRY(launch_norm_grad_terms(c, m, G, terms, n, st));
+                                 at(norm, c0), norm->ct_stride, norm->comp_stride, C, 0, kg, kn};
+        HIP_TRY(launch_norm_grad_terms(c, m, G, terms, n, on));
+        const u64 *d0[KS_MAX_BATCH], *d1[KS_MAX_BATCH], *d2[KS_MAX_BATCH];
         u64* po[KS_MAX_BATCH];
-        for (u32 b = 0; b < n; b++) po[b] = (u64*)d_dx + (size_t)(c0 + b) * 2 * m * N;
-        if (int rc = relinearise(m, terms, p, n, po, sub.rest())) return rc;
-    }
+        for (u32 b = 0; b < n; b++) d0[b] = terms + b * p, d1[b] = terms + (n + b) * p, d2[b] = terms + (2 * n + b) * p, po[b] = (u64*)d_dx + (size_t)(c0 + b) * 2 * m * N;
+        return run_relinearise(c, m, n, d0, d1, d2, rlk->d_key, po, sub.rest(), on);
+    });
+    if (rc) return rc;
     // the gradients of gain and bias, in place
     const size_t wct = (size_t)2 * level * N;
-    if (d_dgain) {
-        for (u32 c0 = 0; c0 < C; c0 += nb) {
-            const u32 n = C - c0 < nb ? C - c0 : nb;
-            const u64 *pa[KS_MAX_BATCH], *pb[KS_MAX_BATCH];
-            u64* po[KS_MAX_BATCH];
-            for (u32 b = 0; b < n; b++) pa[b] = at(grad, c0 + b), pb[b] = at(norm, c0 + b), po[b] = (u64*)d_dgain + (size_t)(c0 + b) * wct;
-            if (int rc = run_ctct_merged(c, level, pa, grad->comp_stride, pb, norm->comp_stride, nullptr, 0, rlk->d_key, po, n, ar.rest(), st)) return rc;
-        }
-    }
+    if (d_dgain)
+        if ((rc = in_turn(C, nb, [&](u32 c0, u32 n, Arena sub, hipStream_t on) { return products(grad, norm, (u64*)d_dgain, c0, n, sub, on); }))) return rc;
     if (d_dbias) {
         for (u32 c0 = 0; c0 < C; c0 += 1024) {
             const u32 n = C - c0 < 1024 ? C - c0 : 1024;
@@ -3116,15 +3191,14 @@ int he_layer_norm_backward(const ckks_ctx* c, const he_layer_norm_grad_desc* d, 
     }
     if (!sums) return CKKS_OK;
     u64* halves[2] = {(u64*)(d_dgain ? d_dgain : d_dbias), (u64*)(d_dgain ? d_dbias : nullptr)};
-    const u32 total = halves[1] ? 2 * C : C, ns = slot_sum_batch(c, total);
-    for (u32 c0 = 0; c0 < total; c0 += ns) {  // both gradients' ciphertexts in the same launches
-        const u32 n = total - c0 < ns ? total - c0 : ns;
+    const u32 total = halves[1] ? 2 * C : C;
+    return in_turn(total, even_batch(total, ks_batch(c), two), [&](u32 c0, u32 n, Arena sub, hipStream_t on) -> int {  // both gradients' ciphertexts in the same launches
         u64* pz[KS_MAX_BATCH];
         for (u32 b = 0; b < n; b++) pz[b] = halves[(c0 + b) / C] + (size_t)((c0 + b) % C) * wct;
         for (u32 i = 0, k = 0; i < d->n_stages; k += h_stage_rots[i], i++)
-            if (int rc = run_slot_sum(c, level - 1, n, pz, sum_keys + k, h_stage_rots[i], ar.rest(), st)) return rc;
-    }
-    return CKKS_OK;
+            if (int e = run_slot_sum(c, level - 1, n, pz, sum_keys + k, h_stage_rots[i], sub, on)) return e;
+        return CKKS_OK;
+    });
 }
 
 // ---- optional per-kernel timing -------------------------------------------------------------------

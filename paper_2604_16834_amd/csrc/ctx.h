@@ -331,7 +331,7 @@ struct MacDivide {
 };
 // turn: two key switches an item, of polynomials 2b and 2b + 1 of the digits, the first with keys[b], the second with key2.  Of the product of (a0, a1) with the rotation by g
 // of (h0, h1), which exist nowhere (launch_ntt with gal_mul_only): a0 sigma(h1) and a1 sigma(h1), with the addends P (a0 sigma(h0) + k x0), P (a1 sigma(h0) + k x1) where add[b]
-// is set, without k x elsewhere (x[b] is then any readable ciphertext); or (stored) of h0 and h1 themselves, with P a0 and P a1.
+// is set, without k x elsewhere (x[b] is then any readable ciphertext); or (stored) of h0 and h1 themselves, with P a0 and P a1; or (stored, one) of h0 alone, with keys[b].
 struct MacTurn {
     const u64* const* a0;
     const u64* const* a1;
@@ -344,6 +344,7 @@ struct MacTurn {
     size_t x_cstride = 0;
     const bool* add = nullptr;
     const u64* k = nullptr;  // one residue per limb
+    bool one = false;
 };
 hipError_t launch_ntt_lo_mac(const ckks_ctx* c, u32 level, const DigitSrc& digits, const u64* const* keys, u64* const* outs, u32 n,
                              hipStream_t st, u32 inv_from, const MacProduct* prod = nullptr, const MacRotate* rot = nullptr, u32* n_part = nullptr,

@@ -694,7 +694,8 @@ struct MacEpilogue {
     u64 ka[CKKS_MAX_MODULI], kb[CKKS_MAX_MODULI];
     // TURN: two key switches an item, whose digits follow each other (2 beta rows), with the keys `key` and `key2`.  1: the product of (a0, a1) with the rotation
     // by gal[b] of (b0, b1): the decomposed polynomials are a0 sigma(b1) and a1 sigma(b1), the addends a0 sigma(b0) + kx x0, a1 sigma(b0) + kx x1, kx = ka where
-    // turn_add[b] is set and zero elsewhere ((x0, x1) = lx with x_cstride); 2: they are stored, b0 and b1, and so are the addends, a0 and a1
+    // turn_add[b] is set and zero elsewhere ((x0, x1) = lx with x_cstride); 2: they are stored, b0 and b1, and so are the addends, a0 and a1; 3: likewise, but one
+    // polynomial an item, b0, and beta rows
     PtrList8 key2;
     u32 turn_add[KS_MAX_BATCH];
     // MASK (with SUM): the rotated ciphertext is the product of (a0, D.own) with mask [level+1][N]
@@ -901,7 +902,7 @@ __global__ __launch_bounds__(NTT_THREADS, TURN ? 2 : 1) void ntt_fwd_lo_mac_kern
     const u32 tid = threadIdx.x;
     const LoTile tile = lo_tile(args.log_hi, args.lo_group);
     static_assert((!DIV || !SUM) && (!HOIST || (ROT && !SUM)) && (!TURN || (!PROD && !ROT && !LIN)), "");
-    constexpr bool LATE = LIN || TURN != 0;  // ten to twelve operands a point behind the digits leave no registers for requests ahead of them
+    constexpr bool TWO = TURN == 1 || TURN == 2, LATE = LIN || TURN != 0;  // ten to twelve operands a point behind the digits leave no registers for requests ahead of them
     const u32 e_at = tile.a + ep.first, e = e_at < ep.E ? e_at : e_at - ep.E;  // the dropped limbs, the longer work, first
     const u32 blk = tile.blk, m_idx = pl_at(pl.mod, e);
     // the batch items of this workgroup: tile.b, tile.b + (the grid's extent over items), ...: a workgroup that takes several
@@ -925,9 +926,9 @@ __global__ __launch_bounds__(NTT_THREADS, TURN ? 2 : 1) void ntt_fwd_lo_mac_kern
         load_tw_w<2>(tw, 512 * TA + 2 * tid, wd);
         load_tw_w<2>(tw, 512 * TA + 2 * tid + 1, wd + 3);
     }
-    const u32 rows = TURN ? 2 * ep.beta : ep.beta, own2 = TURN && own < ep.beta ? ep.beta + own : 0xffffffffu;
+    const u32 rows = TWO ? 2 * ep.beta : ep.beta, own2 = TWO && own < ep.beta ? ep.beta + own : 0xffffffffu;
     u32 j0 = HOIST ? ep.beta : (own == 0 ? 1 : 0);  // first digit to transform
-    if (TURN && j0 == own2) j0++;
+    if (TWO && j0 == own2) j0++;
     E v[8], raw[8];
     // DIV: the converted parts of item b
     auto request_w = [&](u32 b, u32 comp) {
@@ -950,7 +951,7 @@ __global__ __launch_bounds__(NTT_THREADS, TURN ? 2 : 1) void ntt_fwd_lo_mac_kern
     E acc0[8], acc1[8];
     for (u32 b = tile.b; b < args.batch; b += b_step) {
     const u64* key = ep.key.p[b] + (size_t)m_idx * N + off;
-    const u64* key2 = TURN ? ep.key2.p[b] + (size_t)m_idx * N + off : nullptr;
+    const u64* key2 = TWO ? ep.key2.p[b] + (size_t)m_idx * N + off : nullptr;
     const double* hi = (const double*)(ep.D.digits + b * ep.D.bstride) + (size_t)e * N + off;
     if (!SUM || b == tile.b || !summed) {  // a sum over items starts from the last one's reduced sum (f64m_sum_due: so it may)
 #pragma unroll
@@ -960,7 +961,7 @@ __global__ __launch_bounds__(NTT_THREADS, TURN ? 2 : 1) void ntt_fwd_lo_mac_kern
     while (j < rows) {
         u32 jn = j + 1;
         if (jn == own) jn++;
-        if (TURN && jn == own2) jn++;
+        if (TWO && jn == own2) jn++;
 #pragma unroll
         for (int i = 0; i < 8; i++) v[i] = raw[i];
         if (jn < rows) {  // the next digit's points, a tile ahead
@@ -993,7 +994,7 @@ __global__ __launch_bounds__(NTT_THREADS, TURN ? 2 : 1) void ntt_fwd_lo_mac_kern
         // the key words of this digit at the points this thread ends up with: requested now, needed after the last round
         u64 k0[8], k1[8];
         {
-            const u64* kj = (TURN && j >= ep.beta ? key2 + (size_t)(j - ep.beta) * 2 * kstride : key + (size_t)j * 2 * kstride);
+            const u64* kj = (TWO && j >= ep.beta ? key2 + (size_t)(j - ep.beta) * 2 * kstride : key + (size_t)j * 2 * kstride);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 k0[i] = kj[tid + 256 * i];
@@ -1030,8 +1031,8 @@ __global__ __launch_bounds__(NTT_THREADS, TURN ? 2 : 1) void ntt_fwd_lo_mac_kern
         // the two own-limb products, 0.63 q for the addend's
         if (e <= ep.level) {
             const size_t po = (size_t)e * N;
-            const u64 *ku = key + (size_t)own * 2 * kstride - off, *kv = key2 + (size_t)own * 2 * kstride - off;
-            const u64 *pa0 = ep.a0.p[b] + po, *pa1 = ep.a1.p[b] + po, *ph0 = ep.b0.p[b] + po, *ph1 = ep.b1.p[b] + po, *px = TURN == 1 ? ep.lx.p[b] + po : nullptr;
+            const u64 *ku = key + (size_t)own * 2 * kstride - off, *kv = TWO ? key2 + (size_t)own * 2 * kstride - off : nullptr;
+            const u64 *pa0 = ep.a0.p[b] + po, *pa1 = ep.a1.p[b] + po, *ph0 = ep.b0.p[b] + po, *ph1 = TWO ? ep.b1.p[b] + po : nullptr, *px = TURN == 1 ? ep.lx.p[b] + po : nullptr;
             const double pres = mc.q - A::from_u64(ep.negp[e]), kx = TURN == 1 && ep.turn_add[b] ? A::from_u64(ep.ka[e]) : 0.0;
             u32 x0 = (u32)off + tid;
             constexpr int HP = 2;
@@ -1043,13 +1044,15 @@ __global__ __launch_bounds__(NTT_THREADS, TURN ? 2 : 1) void ntt_fwd_lo_mac_kern
                 for (int i = 0; i < HP; i++) {
                     const u32 x = x0 + 256 * (h + i), xs = TURN == 1 ? galois_gather_index(x, ep.gal[b], args.log_n) : x;
                     ra0[i] = word_at(pa0, x), ra1[i] = word_at(pa1, x);
-                    rh0[i] = word_at(ph0, xs), rh1[i] = word_at(ph1, xs);
+                    rh0[i] = word_at(ph0, xs);
+                    if (TWO) rh1[i] = word_at(ph1, xs);
                     if (TURN == 1) rx0[i] = word_at(px, x), rx1[i] = word_at(px + ep.x_cstride, x);
-                    ru0[i] = word_at(ku, x), ru1[i] = word_at(ku + kstride, x), rv0[i] = word_at(kv, x), rv1[i] = word_at(kv + kstride, x);
+                    ru0[i] = word_at(ku, x), ru1[i] = word_at(ku + kstride, x);
+                    if (TWO) rv0[i] = word_at(kv, x), rv1[i] = word_at(kv + kstride, x);
                 }
 #pragma unroll
                 for (int i = 0; i < HP; i++) {
-                    double u = A::from_u64(rh0[i]), w = A::from_u64(rh1[i]), dd0 = A::from_u64(ra0[i]), dd1 = A::from_u64(ra1[i]);
+                    double u = A::from_u64(rh0[i]), w = TWO ? A::from_u64(rh1[i]) : 0.0, dd0 = A::from_u64(ra0[i]), dd1 = A::from_u64(ra1[i]);
                     if (TURN == 1) {
                         const double A0 = dd0, A1 = dd1, H0 = u, H1 = w;
                         u = A::mulmod_any(A0, H1, mc.q, mc.qinv), w = A::mulmod_any(A1, H1, mc.q, mc.qinv);
@@ -1058,8 +1061,12 @@ __global__ __launch_bounds__(NTT_THREADS, TURN ? 2 : 1) void ntt_fwd_lo_mac_kern
                     }
                     dd0 = A::reduce(dd0, mc);
                     dd1 = A::reduce(dd1, mc);
-                    acc0[h + i] += A::mulmod_any(u, A::from_u64(ru0[i]), mc.q, mc.qinv) + A::mulmod_any(w, A::from_u64(rv0[i]), mc.q, mc.qinv) + A::mulmod_any(dd0, pres, mc.q, mc.qinv);
-                    acc1[h + i] += A::mulmod_any(u, A::from_u64(ru1[i]), mc.q, mc.qinv) + A::mulmod_any(w, A::from_u64(rv1[i]), mc.q, mc.qinv) + A::mulmod_any(dd1, pres, mc.q, mc.qinv);
+                    acc0[h + i] += A::mulmod_any(u, A::from_u64(ru0[i]), mc.q, mc.qinv) + A::mulmod_any(dd0, pres, mc.q, mc.qinv);
+                    acc1[h + i] += A::mulmod_any(u, A::from_u64(ru1[i]), mc.q, mc.qinv) + A::mulmod_any(dd1, pres, mc.q, mc.qinv);
+                    if (TWO) {
+                        acc0[h + i] += A::mulmod_any(w, A::from_u64(rv0[i]), mc.q, mc.qinv);
+                        acc1[h + i] += A::mulmod_any(w, A::from_u64(rv1[i]), mc.q, mc.qinv);
+                    }
                 }
             }
         }
@@ -2892,7 +2899,7 @@ hipError_t launch_ntt_rescale_vec(const ckks_ctx* c, u32 level, VecMode mode, co
 hipError_t launch_ntt_lo_mac(const ckks_ctx* c, u32 level, const DigitSrc& digits, const u64* const* keys, u64* const* outs, u32 n,
                              hipStream_t st, u32 inv_from, const MacProduct* prod, const MacRotate* rot, u32* n_part, const MacDivide* div, bool dropped_only, const MacTurn* turn) {
     if ((div || dropped_only) && (n_part || inv_from == 0 || inv_from >= c->ext_limbs(level) || (!prod && !rot && !turn))) return hipErrorInvalidValue;
-    if (turn && (prod || rot || n_part || (!turn->stored && (!turn->x || !turn->k)))) return hipErrorInvalidValue;
+    if (turn && (prod || rot || n_part || (turn->one && !turn->stored) || (!turn->stored && (!turn->x || !turn->k)))) return hipErrorInvalidValue;
     if (!ntt_has_modup(c) || (n_part && !rot) || (rot && rot->mask && !n_part) || (rot && rot->hoisted && n_part) || c->log_hi == 0 || n == 0 || n > KS_MAX_BATCH || (prod && rot)) return hipErrorInvalidValue;
     const u32 E = c->ext_limbs(level), beta = c->live_digits(level);
     NttArgs args = {};
@@ -2926,11 +2933,11 @@ hipError_t launch_ntt_lo_mac(const ckks_ctx* c, u32 level, const DigitSrc& digit
         ep.b0.p[b] = (prod && b < n) ? prod->b0[b] : nullptr;
         ep.b1.p[b] = (prod && b < n) ? prod->b1[b] : nullptr;
         if (turn && b < n) {
-            ep.a0.p[b] = turn->a0[b], ep.a1.p[b] = turn->a1[b], ep.b0.p[b] = turn->h0[b], ep.b1.p[b] = turn->h1[b];
-            ep.key2.p[b] = turn->key2;
+            ep.a0.p[b] = turn->a0[b], ep.a1.p[b] = turn->a1[b], ep.b0.p[b] = turn->h0[b], ep.b1.p[b] = turn->one ? nullptr : turn->h1[b];
+            ep.key2.p[b] = turn->one ? keys[b] : turn->key2;
             ep.gal[b] = turn->g;
             ep.turn_add[b] = turn->stored || !turn->add ? 0 : (turn->add[b] ? 1 : 0);
-            if (!ep.a0.p[b] || !ep.a1.p[b] || !ep.b0.p[b] || !ep.b1.p[b] || !turn->key2) return hipErrorInvalidValue;
+            if (!ep.a0.p[b] || !ep.a1.p[b] || !ep.b0.p[b] || (!turn->one && (!ep.b1.p[b] || !turn->key2))) return hipErrorInvalidValue;
         }
         if (prod && b < n && (!ep.a0.p[b] || !ep.a1.p[b] || !ep.b0.p[b] || !ep.b1.p[b])) return hipErrorInvalidValue;
         if (b < n && (b == 0 || keys[b] != keys[b - 1])) n_keys += 1.0;
@@ -2980,9 +2987,9 @@ hipError_t launch_ntt_lo_mac(const ckks_ctx* c, u32 level, const DigitSrc& digit
     const bool hoisted = rot && rot->hoisted;
     const double np = div ? inv_from : (dropped_only ? E - inv_from : E), kept = dropped_only ? 0.0 : (inv_from < E ? inv_from : E), inverse = div ? 0.0 : np - kept;
     const double live = div ? inv_from : (dropped_only ? level + 1.0 - inv_from : level + 1.0);
-    const double sets = turn ? 2.0 : 1.0, rows = sets * (beta * np - live), n_tr = hoisted ? 0.0 : n * rows;  // n_tr: transformed
+    const double sets = turn && !turn->one ? 2.0 : 1.0, rows = sets * (beta * np - live), n_tr = hoisted ? 0.0 : n * rows;  // n_tr: transformed
     double words = (hoisted ? 1.0 : (double)n) * rows + sets * n_keys * 2.0 * beta * np + (rot && rot->mask ? live : 0.0);
-    words += live * (turn ? (turn->stored ? 4.0 : 6.0) * n : prod ? (lin ? 8.0 : 4.0) * n : (rot ? 2.0 * n_src : 1.0 * n));  // (lin: two components of two ciphertexts)
+    words += live * (turn ? (turn->one ? 3.0 : turn->stored ? 4.0 : 6.0) * n : prod ? (lin ? 8.0 : 4.0) * n : (rot ? 2.0 * n_src : 1.0 * n));  // (lin: two components of two ciphertexts)
     words += 2.0 * (n * inverse + (n_part ? b_ext : n) * kept);
     if (div) words += 2.0 * kept * (n + n_add);
     ProfScope ps__(c, K_NTT_FWD_LO, st, 8.0 * c->N * words, 0.5 * c->N * c->log_lo * (n_tr + 2.0 * n * (inverse + (div ? kept : 0.0))));
@@ -2994,7 +3001,9 @@ hipError_t launch_ntt_lo_mac(const ckks_ctx* c, u32 level, const DigitSrc& digit
         return hipGetLastError();
     }
     if (turn) {
-        if (turn->stored && div) LO_MAC_LAUNCH(false, false, false, false, false, true, false, 2);
+        if (turn->one && div) LO_MAC_LAUNCH(false, false, false, false, false, true, false, 3);
+        else if (turn->one) LO_MAC_LAUNCH(false, false, false, false, false, false, false, 3);
+        else if (turn->stored && div) LO_MAC_LAUNCH(false, false, false, false, false, true, false, 2);
         else if (turn->stored) LO_MAC_LAUNCH(false, false, false, false, false, false, false, 2);
         else if (div) LO_MAC_LAUNCH(false, false, false, false, false, true, false, 1);
         else LO_MAC_LAUNCH(false, false, false, false, false, false, false, 1);

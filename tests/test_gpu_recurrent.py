@@ -333,7 +333,7 @@ def alone(bufs, ws=None, need=0, pad=64):
         assert bool((ws[need:] == 0x5a).all())
 
 
-@pytest.mark.parametrize("ring", [(12, 7, 3, 3, 50), (10, 7, 3, 3, 50), (12, 7, 3, 3, 56), (13, 7, 1, 7, 50)])
+@pytest.mark.parametrize("ring", [(12, 7, 3, 3, 50), (10, 7, 3, 3, 50), (12, 7, 3, 3, 56), (13, 7, 1, 7, 50), (14, 7, 3, 3, 50)])
 @pytest.mark.parametrize("name", NAMES)
 def test_nothing_is_written_beside_outputs_and_workspace(name, ring):
     ctx, ops = calls(ring)
@@ -381,10 +381,29 @@ def test_on_another_stream(name):
     assert all(torch.equal(a, b) for a, b in zip(ref, outs))
 
 
+@pytest.mark.parametrize("ring", [(13, 7, 3, 3, 50), (14, 7, 3, 3, 50), (12, 7, 3, 3, 56)])
 @pytest.mark.parametrize("name", NAMES)
-def test_captured_and_replayed(name):
+def test_one_stream_and_two_agree(name, ring):
+    """The same workspace serves both; sizes on both sides of the rule that deals batches to the context's second stream."""
+    ctx, ops = calls(ring)
+    call, need, shapes = ops[name]
+    ws = torch.full((need + 4096,), 0x5a, dtype=torch.uint8, device="cuda")
+    (b1, one), (b2, two) = outputs(shapes), outputs(shapes)
+    call(ws[:need], two)
+    try:
+        hx.ckks_ctx_set_overlap(ctx, False)
+        call(ws[:need], one)
+    finally:
+        hx.ckks_ctx_set_overlap(ctx, True)
+    alone(b1 + b2, ws, need)
+    assert all(torch.equal(a, b) for a, b in zip(one, two))
+
+
+@pytest.mark.parametrize("ring", [(12, 7, 3, 3, 50), (14, 7, 3, 3, 50)])
+@pytest.mark.parametrize("name", NAMES)
+def test_captured_and_replayed(name, ring):
     """Two graphs that share a workspace, replayed in turn with eager calls between, every replay against the eager result."""
-    ctx, ops = calls()
+    ctx, ops = calls(ring)
     call, need, shapes = ops[name]
     ws = torch.empty(need, dtype=torch.uint8, device="cuda")
     _, ref = outputs(shapes)
