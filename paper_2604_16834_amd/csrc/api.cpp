@@ -2327,7 +2327,8 @@ static LimbScalars times_limb(const ckks_ctx* c, int64_t k, u32 lv) {
     return v;
 }
 // The norms' inverse square root: s from the tensor product sq3 of `level` ([3][level + 1][N], the constant in it already), the linear first guess, Newton's iterations.
-// s, u, w [2][level][N]; ra, rb [2][level + 1][N] (swapped: the result is in ra).  Scratch: ws_inverse_root.
+// s, u, w [2][level][N]; ra, rb [2][level + 1][N] (swapped: the result is in ra); out: the result goes there instead, [2][level - 1 - 2 iterations][N], or null.  Scratch:
+// ws_inverse_root.
 static size_t ws_inverse_root(const ckks_ctx* c, u32 level, u32 iterations) {
     const size_t N = c->N, L1 = level + 1;
     size_t sub = ws_ks(c, level, 1, 1), t;
@@ -2336,7 +2337,7 @@ static size_t ws_inverse_root(const ckks_ctx* c, u32 level, u32 iterations) {
     return sub;
 }
 static int run_inverse_root(const ckks_ctx* c, u32 level, u32 iterations, int64_t k_slope, int64_t k_start, const int64_t* h_k_newton, const u64* d_rlk, const u64* sq3, u64* s,
-                            u64* u, u64* w, u64*& ra, u64*& rb, Arena ar, hipStream_t st) {
+                            u64* u, u64* w, u64*& ra, u64*& rb, u64* out, Arena ar, hipStream_t st) {
     const bool mac = ntt_has_modup(c);
     const size_t N = c->N, L1 = level + 1;
     int rc;
@@ -2348,10 +2349,12 @@ static int run_inverse_root(const ckks_ctx* c, u32 level, u32 iterations, int64_
     const size_t ss = (size_t)level * N;  // component stride of s
     HIP_TRY(launch_affine(c, level - 1, s, ss, limb_scalars(c, level - 1, k_slope), times_limb(c, k_start, level - 1), rb, st));
     const u64* prb = rb;
+    if (out && iterations == 0) ra = out;
     if ((rc = run_rescale(c, level - 1, &prb, ss, &ra, 1, ar, st))) return rc;
     // r at level m
     u32 m = level - 2;
     for (u32 it = 0; it < iterations; it++, m -= 2) {
+        if (out && it + 1 == iterations) rb = out;
         const size_t rs = (size_t)(m + 1) * N, us = (size_t)m * N;
         const u64 *pr = ra, *ps = s, *pu = u, *pw = w;
         Arena sub = ar;
@@ -2507,7 +2510,7 @@ int he_norm_gate(const ckks_ctx* c, const he_norm_desc* d, const int64_t* h_k_ne
     // s and Newton's iterations
     auto run_chain = [&]() -> int {
         HIP_TRY(launch_square_sum(c, level, (const u64*)x->d, x->ct_stride, x->comp_stride, d->channels, times_limb(c, d->k_eps, level), sq3, st));
-        return run_inverse_root(c, level, d->iterations, d->k_slope, d->k_start, h_k_newton, rlk->d_key, sq3, s, u, w, ra, rb, ar.rest(), st);
+        return run_inverse_root(c, level, d->iterations, d->k_slope, d->k_start, h_k_newton, rlk->d_key, sq3, s, u, w, ra, rb, nullptr, ar.rest(), st);
     };
     // the last products
     const size_t rs = (size_t)(last + 1) * N, out_ct = (size_t)2 * last * N;
@@ -2997,8 +3000,7 @@ int he_layer_norm(const ckks_ctx* c, const he_layer_norm_desc* d, const int64_t*
     u64* w = ar.take(2 * N * level);
     if (!ar.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for the layer norm");
     HIP_TRY(launch_centred_squares(c, level, (const u64*)x->d, x->ct_stride, x->comp_stride, C, times_limb(c, d->k_eps, level), sq3, sum, st));
-    if (int rc = run_inverse_root(c, level, d->iterations, d->k_slope, d->k_start, h_k_newton, rlk->d_key, sq3, s, u, w, ra, rb, ar.rest(), st)) return rc;
-    if (d_inv) HIP_TRY(launch_copy(ra, (u64*)d_inv, (size_t)2 * (m + 1) * N, st));
+    if (int rc = run_inverse_root(c, level, d->iterations, d->k_slope, d->k_start, h_k_newton, rlk->d_key, sq3, s, u, w, ra, rb, (u64*)d_inv, ar.rest(), st)) return rc;
     const bool two = c->side_stream() && layer_norm_two(c, d);
     const u32 nb = even_batch(C, ks_batch(c), two);
     const size_t rs = (size_t)(m + 1) * N, norm_ct = (size_t)2 * m * N, out_ct = (size_t)2 * (m - 1) * N, lane = ws_layer_norm_lane(c, d, two);
@@ -3040,7 +3042,7 @@ static int layer_norm_grad_check(const ckks_ctx* c, const he_layer_norm_grad_des
     if (!level_ok(c, d->level) || d->level < 3 + d->affine) return set_err(c, CKKS_ERR_LEVEL_MISMATCH, "layer norm's backward pass needs 3 <= level < num_q, with a gain one more");
     return CKKS_OK;
 }
-static size_t ws_slot_sum(const ckks_ctx* c, u32 level, u32 n) { return ws_ks(c, level, n, c->small_q ? n : 2 * n); }
+static size_t ws_slot_sum(const ckks_ctx* c, u32 level, u32 n) { return blk((size_t)n * 2 * (level + 1) * c->N) + ws_ks(c, level, n, c->small_q ? n : 2 * n); }
 // z[b] <- z[b] + the sum of its rotations by the keys, n <= ks_batch ciphertexts [2][level + 1][N]: one decomposition, and one division for all rotations
 static int run_slot_sum(const ckks_ctx* c, u32 level, u32 n, u64* const* z, const ckks_key* const* keys, u32 n_keys, Arena ar, hipStream_t st) {
     KsWs ws;
@@ -3074,6 +3076,41 @@ static int run_slot_sum(const ckks_ctx* c, u32 level, u32 n, u64* const* z, cons
     }
     return run_moddown(c, level, ws, n, items, st);
 }
+// All stages, stage i of rots[i] keys.  A stage of one rotation is a batch of rotations with an addend in the fused passes, whose workgroups gather while others store: from z into a
+// copy and back in turn.  A stage as any other, in place / so, in us: two ciphertexts of 5 + 3 limbs at N = 2^12 32.0 / 30.5, 16 of them 44.6 / 40.1, of 9 + 5 at 2^14 152 / 131, at 2^16 515 / 419, 32
+// of 12 + 8 at 2^16 1470 / 1166.
+static int run_slot_sums(const ckks_ctx* c, u32 level, u32 n, u64* const* z, const ckks_key* const* keys, const u32* rots, u32 n_stages, Arena ar, hipStream_t st) {
+    const size_t ct = (size_t)2 * (level + 1) * c->N;
+    u64* other = ar.take(n * ct);
+    if (!ar.ok()) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for sums over slots");
+    u32 singles = 0;
+    if (ntt_has_modup(c))
+        for (u32 i = 0; i < n_stages; i++) singles += rots[i] == 1;
+    bool stay = singles & 1;  // the first of an odd number of them in place, so that the last one ends in z
+    u64 *from[KS_MAX_BATCH], *to[KS_MAX_BATCH];
+    for (u32 b = 0; b < n; b++) from[b] = z[b], to[b] = other + b * ct;
+    for (u32 i = 0, k = 0; i < n_stages; k += rots[i], i++) {
+        if (rots[i] != 1 || !ntt_has_modup(c) || stay) {
+            if (rots[i] == 1) stay = false;
+            if (int rc = run_slot_sum(c, level, n, from, keys + k, rots[i], ar.rest(), st)) return rc;
+            continue;
+        }
+        KsWs ws;
+        Arena sub = ar.rest();
+        if (!carve_ks(c, level, n, n, sub, ws)) return set_err(c, CKKS_ERR_WORKSPACE_TOO_SMALL, "workspace too small for sums over slots");
+        const ckks_key* ks[KS_MAX_BATCH];
+        u32 gal[KS_MAX_BATCH];
+        for (u32 b = 0; b < n; b++) ks[b] = keys[k], gal[b] = keys[k]->galois_elt;
+        if (int rc = run_rotate_batch(c, level, n, from, ks, gal, to, ws, st, from)) return rc;
+        for (u32 b = 0; b < n; b++) {
+            u64* swap = from[b];
+            from[b] = to[b];
+            to[b] = swap;
+        }
+    }
+    return CKKS_OK;
+}
+
 // the channels' batches in turn on two streams: with a gradient of gain or bias to be summed, each stream takes half of the ciphertexts through all stages
 static bool layer_norm_grad_two(const ckks_ctx* c, const he_layer_norm_grad_desc* d) { return lanes_pay(c, d->level, 2 * d->channels, ks_batch(c)); }
 static size_t ws_layer_norm_grad_lane(const ckks_ctx* c, const he_layer_norm_grad_desc* d, bool two) {
@@ -3195,9 +3232,7 @@ int he_layer_norm_backward(const ckks_ctx* c, const he_layer_norm_grad_desc* d, 
     return in_turn(total, even_batch(total, ks_batch(c), two), [&](u32 c0, u32 n, Arena sub, hipStream_t on) -> int {  // both gradients' ciphertexts in the same launches
         u64* pz[KS_MAX_BATCH];
         for (u32 b = 0; b < n; b++) pz[b] = halves[(c0 + b) / C] + (size_t)((c0 + b) % C) * wct;
-        for (u32 i = 0, k = 0; i < d->n_stages; k += h_stage_rots[i], i++)
-            if (int e = run_slot_sum(c, level - 1, n, pz, sum_keys + k, h_stage_rots[i], sub, on)) return e;
-        return CKKS_OK;
+        return run_slot_sums(c, level - 1, n, pz, sum_keys, h_stage_rots, d->n_stages, sub, on);
     });
 }
 

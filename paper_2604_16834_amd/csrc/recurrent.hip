@@ -225,24 +225,18 @@ __global__ __launch_bounds__(RC_THREADS) void rot_sum_kernel(DigitSrc digits, Ro
             dv[i] = row[xs];
         }
     };
-    double sum[2][NB], ct[2][NB], cl[2][NB];
-    auto begin = [&]() {
-#pragma unroll
-        for (int c = 0; c < 2; c++)
-#pragma unroll
-            for (int i = 0; i < NB; i++) ct[c][i] = F64M_DOT_BASE, cl[c][i] = 0.0;
-    };
+    double ct[2][NB], cl[2][NB];  // a chain's running sum and remainders; a chain goes on from the last one's reduced sum as one more remainder, below 2^49 + 1: with the eight of a
+                                  // chain below 9 2^49 + 1, and with the chain's high part (f64m_chain_join) below 2^53
     auto join = [&]() {
 #pragma unroll
         for (int c = 0; c < 2; c++)
 #pragma unroll
-            for (int i = 0; i < NB; i++) sum[c][i] = f64m_reduce(sum[c][i] + f64m_chain_join(ct[c][i], cl[c][i], q, qinv), q, qinv);
+            for (int i = 0; i < NB; i++) cl[c][i] = f64m_chain_join(ct[c][i], cl[c][i], q, qinv), ct[c][i] = F64M_DOT_BASE;
     };
 #pragma unroll
     for (int c = 0; c < 2; c++)
 #pragma unroll
-        for (int i = 0; i < NB; i++) sum[c][i] = 0.0;
-    begin();
+        for (int i = 0; i < NB; i++) ct[c][i] = F64M_DOT_BASE, cl[c][i] = 0.0;
     load(0, 0);
     u32 r = 0, j = 0, count = 0;
     while (r < K.n) {
@@ -261,7 +255,6 @@ __global__ __launch_bounds__(RC_THREADS) void rot_sum_kernel(DigitSrc digits, Ro
         }
         if (++count == 8) {  // uniform
             join();
-            begin();
             count = 0;
         }
     }
@@ -273,7 +266,7 @@ __global__ __launch_bounds__(RC_THREADS) void rot_sum_kernel(DigitSrc digits, Ro
 #pragma unroll
         for (int c = 0; c < 2; c++) {
             u64* oc = o + (size_t)c * E * N;
-            const double v = add ? f64m_reduce(sum[c][i] + f64m_from_u64(*oc), q, qinv) : sum[c][i];
+            const double v = add ? f64m_reduce(cl[c][i] + f64m_from_u64(*oc), q, qinv) : cl[c][i];
             *oc = f64m_canonical(v, q);
         }
     }

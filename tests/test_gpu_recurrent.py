@@ -250,9 +250,9 @@ def test_layer_norm_gradients_in_batches(channels):
     grad_case((10, 5, 2, 3, 56), 3, channels, False, [(1,)], channels + 1, want_gain=channels % 2 == 0)
 
 
-@pytest.mark.parametrize("stages", [[], [(1,)] * 3, [(5, 5)], [tuple(range(1, 20))], [(1, 2, 3), (4, 8, 12), (16, 32)]])
+@pytest.mark.parametrize("stages", [[], [(1,)], [(1,), (2,)], [(1,)] * 3, [(5, 5)], [tuple(range(1, 70))], [(1, 2, 3), (4, 8, 12), (16, 32)], [(1, 2), (3,), (1, 4), (5,), (-1,)], [(2,), (1, 2, 3), (7,)]])
 def test_sums_over_slots(stages):
-    """None, the same rotation again, one twice in a stage, more rotations than any batch holds."""
+    """None, one rotation a stage an odd and an even number of times, the same again, one twice in a stage, more rotations than a launch holds, mixed."""
     grad_case((12, 4, 2, 2, 50), 3, 2, False, stages, len(stages))
     grad_case((11, 4, 2, 2, 56), 3, 2, False, stages, len(stages) + 1)
 
