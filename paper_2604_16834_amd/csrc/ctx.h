@@ -501,9 +501,12 @@ struct NormGradTerms {
     LimbScalars k_grad, k_norm;
 };
 hipError_t launch_norm_grad_terms(const ckks_ctx* c, u32 level, const NormGradTerms& T, u64* out, u32 n, hipStream_t st);
-// outs[b] (+)= the sum over the keys of (P sigma(c0s[b]) + <sigma(digits), key>_0, <sigma(digits), key>_1) on the extended basis, n <= KS_MAX_BATCH, moduli below 2^50
+// outs[b] (+)= the sum over the keys of (P sigma(c0) + <sigma(digits), key>_0, <sigma(digits), key>_1) on the extended basis, n <= KS_MAX_BATCH ciphertexts cts[b] = (c0, c1)
+// [2][level + 1][N], whose c1 has its digits, but for the digits' own limbs, at digits + b * bstride (rot_sum_applies: moduli below 2^50, at
+// most four digits)
 #define ROT_SUM_KEYS 32
-hipError_t launch_rot_sum(const ckks_ctx* c, u32 level, const DigitSrc& digits, const u64* const* keys, const u32* gs, u32 n_keys, const u64* const* c0s, u64* const* outs, u32 n,
+bool rot_sum_applies(const ckks_ctx* c, u32 level);
+hipError_t launch_rot_sum(const ckks_ctx* c, u32 level, const u64* digits, size_t bstride, const u64* const* keys, const u32* gs, u32 n_keys, const u64* const* cts, u64* const* outs, u32 n,
                           bool add, hipStream_t st);
 hipError_t launch_add_ext(const ckks_ctx* c, u32 level, u64* v, const u64* w, u32 n, hipStream_t st);
 hipError_t launch_copy_cts(const ckks_ctx* c, u32 limbs, u32 n, const u64* in, size_t in_ct, size_t in_comp, u64* out, hipStream_t st);

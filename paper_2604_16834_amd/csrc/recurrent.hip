@@ -180,85 +180,114 @@ hipError_t launch_norm_grad_terms(const ckks_ctx* c, u32 level, const NormGradTe
 }
 
 // ---- sums of rotations on the extended basis -------------------------------------------------------------------
-// out_b = sum_r (P sigma_r(c0_b) + <sigma_r(digits_b), key_r>_0, <sigma_r(digits_b), key_r>_1), b < n: what one stage of a sum over slots divides by P once.  Moduli below 2^50: the
-// sums as chains of eight fused multiply-adds on centred doubles (f64m_chain_add).  A thread holds both components of one destination point of NB ciphertexts, so that a
-// key word is read once for them, and gathers their digits through each automorphism in turn (a wavefront's 64 points are one aligned run of 512 bytes); the operands of the next
-// digit are requested before the present one's are used.  Workgroups are dealt to the eight dies in turn: each die takes a contiguous eighth of the (limb, points) list, so that what
-// the rotations gather again comes from its own L2 cache.
+// out_b = sum_r (P sigma_r(c0_b) + <sigma_r(digits_b), key_r>_0, <sigma_r(digits_b), key_r>_1), b < n: what one stage of a sum over slots divides by P once.  Moduli below 2^50,
+// BETA digits: the sums as chains of fused multiply-adds on centred doubles (f64m_chain_add).  A thread holds both components of one destination point of NB ciphertexts, so that a
+// key word is read once for them, and gathers their digits through each automorphism in turn (a wavefront's 64 points are one aligned run of 512 bytes).  Workgroups are dealt to the eight
+// dies in turn: each die takes a contiguous eighth of the (limb, points, ciphertexts) list, so that what the rotations gather again, and the keys for the next ciphertexts, come from its own L2
+// cache.  16 ciphertexts of 12 + 8 limbs at N = 2^16, seven rotations: 480 us; 1.0 GB have to be moved (196 us), the arithmetic alone takes 220.  An inner product and an addition for every
+// rotation took 1160 us; with one term after the other behind branches 530; four ciphertexts a thread 517, two 570; four points of two ciphertexts 575.
 struct RotSumKeys {
     const u64* key[ROT_SUM_KEYS];
     u32 g[ROT_SUM_KEYS];
     u32 n;
 };
-template <int NB>
-__global__ __launch_bounds__(RC_THREADS) void rot_sum_kernel(DigitSrc digits, RotSumKeys K, PtrList8 c0s, OutList8 out, u32 add, const u64* __restrict__ negp,
-                                                             const ModConstF* __restrict__ mcf, u32 log_n, u32 level, u32 num_q, u32 M, u32 E, u32 beta, u32 n) {
-    const u32 N = 1u << log_n, nxb = (N + RC_THREADS - 1) / RC_THREADS;
-    const u32 list = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3), e = list / nxb, b0 = blockIdx.y * NB;
-    if (e >= E) return;  // whole workgroup
-    const u32 x = list % nxb * RC_THREADS + threadIdx.x;
-    if (x >= N) return;
-    const u32 t = e <= level ? e : num_q + (e - level - 1), own = e <= level ? e / digits.alpha : 0xffffffffu;
-    const double q = mcf[t].q, qinv = mcf[t].qinv;
-    const u32 terms = beta + (e <= level ? 1 : 0);  // the digits, then c0 (P c0 is zero on the special primes)
+__device__ __forceinline__ u64 word_at_byte(const u64* poly, u32 byte) { return *reinterpret_cast<const u64*>(reinterpret_cast<const char*>(poly) + byte); }
+
+// LIVE: limb e is one of the ciphertexts' (nothing of c0 is added on the special primes)
+template <int BETA, int NB, bool LIVE>
+__device__ __forceinline__ void rot_sum_chains(const u64* const (&row)[BETA][NB], const u64* const (&c0)[NB], const RotSumKeys& K, u32 x, u32 log_n, size_t to_limb, size_t kstride,
+                                               double q, double qinv, double pres, double (&sum)[2][NB]) {
+    // A chain's running sum and remainders; a chain of at most eight terms goes on from the last one's reduced sum as one more remainder, below 2^49 + 1: with the eight of a
+    // chain below 9 2^49 + 1, and with what is left of the chain's high part (f64m_chain_join) below 2^53.
+    constexpr u32 PER = 8 / (BETA + 1);  // rotations a chain
+    double ct[2][NB];
+#pragma unroll
+    for (int c = 0; c < 2; c++)
+#pragma unroll
+        for (int i = 0; i < NB; i++) ct[c][i] = F64M_DOT_BASE, sum[c][i] = 0.0;
     auto centred = [&](u64 v) {
         const double d = f64m_from_u64(v);
         return d > 0.5 * q ? d - q : d;
     };
-    const double pres = e <= level ? centred((u64)q - negp[e]) : 0.0;
-    const u64* rows[NB];  // digit 0's row of every ciphertext
+    // The next rotation's operands are requested as the present one's are used, with no branch around a request: a wait is then for the operands that are needed alone.  Behind
+    // the last rotation it is requested once more.
+    u64 dv[BETA][NB], k0[BETA], k1[BETA], cv[NB];
+    const u64* key = K.key[0] + to_limb;
+    u32 xs = 8 * galois_gather_index(x, K.g[0], log_n);
+    auto request = [&](int j) {
+        k0[j] = word_at_byte(key + (size_t)(2 * j) * kstride, 8 * x);
+        k1[j] = word_at_byte(key + (size_t)(2 * j + 1) * kstride, 8 * x);
 #pragma unroll
-    for (int i = 0; i < NB; i++) rows[i] = digits.digits + (b0 + i < n ? b0 + i : n - 1) * digits.bstride + (size_t)e * N;
-    u64 dv[NB], k0 = 0, k1 = 0;
-    u32 xs = 0;
-    auto load = [&](u32 r, u32 j) {
-        if (j == 0) xs = galois_gather_index(x, K.g[r], log_n);
-        if (j < beta) {
-            const u64* kp = K.key[r] + ((size_t)2 * j * M + t) * N + x;
-            k0 = kp[0];
-            k1 = kp[(size_t)M * N];
-        }
-#pragma unroll
-        for (int i = 0; i < NB; i++) {
-            const u32 b = b0 + i < n ? b0 + i : n - 1;
-            const u64* row = j == beta ? c0s.p[b] + (size_t)e * N : (j == own ? digits.own.p[b] + (size_t)e * N : rows[i] + (size_t)j * E * N);
-            dv[i] = row[xs];
-        }
+        for (int i = 0; i < NB; i++) dv[j][i] = word_at_byte(row[j][i], xs);
     };
-    double ct[2][NB], cl[2][NB];  // a chain's running sum and remainders; a chain goes on from the last one's reduced sum as one more remainder, below 2^49 + 1: with the eight of a
-                                  // chain below 9 2^49 + 1, and with the chain's high part (f64m_chain_join) below 2^53
-    auto join = [&]() {
+    auto request_c0 = [&]() {
 #pragma unroll
-        for (int c = 0; c < 2; c++)
-#pragma unroll
-            for (int i = 0; i < NB; i++) cl[c][i] = f64m_chain_join(ct[c][i], cl[c][i], q, qinv), ct[c][i] = F64M_DOT_BASE;
+        for (int i = 0; i < NB; i++) cv[i] = word_at_byte(c0[i], xs);
     };
 #pragma unroll
-    for (int c = 0; c < 2; c++)
+    for (int j = 0; j < BETA; j++) request(j);
+    if (LIVE) request_c0();
+    for (u32 r = 0, count = 0; r < K.n; r++) {
+        const u32 rn = r + 1 < K.n ? r + 1 : r;
+        key = K.key[rn] + to_limb;
+        xs = 8 * galois_gather_index(x, K.g[rn], log_n);
 #pragma unroll
-        for (int i = 0; i < NB; i++) ct[c][i] = F64M_DOT_BASE, cl[c][i] = 0.0;
-    load(0, 0);
-    u32 r = 0, j = 0, count = 0;
-    while (r < K.n) {
-        double y[NB];
-        const bool key = j < beta;
-        const double w0 = key ? centred(k0) : pres, w1 = centred(k1);
+        for (int j = 0; j < BETA; j++) {
+            const double w0 = centred(k0[j]), w1 = centred(k1[j]);
+            double y[NB];
 #pragma unroll
-        for (int i = 0; i < NB; i++) y[i] = centred(dv[i]);
-        if (++j == terms) j = 0, r++;
-        if (r < K.n) load(r, j);
+            for (int i = 0; i < NB; i++) y[i] = centred(dv[j][i]);
+            request(j);
 #pragma unroll
-        for (int i = 0; i < NB; i++) f64m_chain_add(ct[0][i], cl[0][i], y[i], w0);
-        if (key) {  // uniform
-#pragma unroll
-            for (int i = 0; i < NB; i++) f64m_chain_add(ct[1][i], cl[1][i], y[i], w1);
+            for (int i = 0; i < NB; i++) {
+                f64m_chain_add(ct[0][i], sum[0][i], y[i], w0);
+                f64m_chain_add(ct[1][i], sum[1][i], y[i], w1);
+            }
         }
-        if (++count == 8) {  // uniform
-            join();
+        if (LIVE) {
+            double y[NB];
+#pragma unroll
+            for (int i = 0; i < NB; i++) y[i] = centred(cv[i]);
+            request_c0();
+#pragma unroll
+            for (int i = 0; i < NB; i++) f64m_chain_add(ct[0][i], sum[0][i], y[i], pres);
+        }
+        if (++count == PER || r + 1 == K.n) {  // uniform
             count = 0;
+#pragma unroll
+            for (int c = 0; c < 2; c++)
+#pragma unroll
+                for (int i = 0; i < NB; i++) sum[c][i] = f64m_chain_join(ct[c][i], sum[c][i], q, qinv), ct[c][i] = F64M_DOT_BASE;
         }
     }
-    join();
+}
+
+template <int BETA, int NB>
+__global__ __launch_bounds__(RC_THREADS) void rot_sum_kernel(const u64* __restrict__ digits, size_t bstride, u32 alpha, RotSumKeys K, PtrList8 cts, OutList8 out, u32 add,
+                                                             const u64* __restrict__ negp, const ModConstF* __restrict__ mcf, u32 log_n, u32 level, u32 num_q, u32 M, u32 E, u32 n) {
+    const u32 N = 1u << log_n, nxb = (N + RC_THREADS - 1) / RC_THREADS, groups = (n + NB - 1) / NB;
+    const u32 list = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3), e = list / (nxb * groups), b0 = list % groups * NB;
+    if (e >= E) return;  // whole workgroup
+    const u32 x = list / groups % nxb * RC_THREADS + threadIdx.x;
+    if (x >= N) return;
+    const bool live = e <= level;
+    const u32 t = live ? e : num_q + (e - level - 1), own = live ? e / alpha : 0xffffffffu;
+    const double q = mcf[t].q, qinv = mcf[t].qinv;
+    const u64 *row[BETA][NB], *c0[NB];
+#pragma unroll
+    for (int i = 0; i < NB; i++) {
+        const u32 b = b0 + i < n ? b0 + i : n - 1;
+        c0[i] = cts.p[b] + (size_t)(live ? e : 0) * N;
+#pragma unroll
+        for (int j = 0; j < BETA; j++) row[j][i] = own == (u32)j ? c0[i] + (size_t)(level + 1) * N : digits + b * bstride + ((size_t)j * E + e) * N;
+    }
+    double sum[2][NB];
+    if (live) {
+        const double p = q - f64m_from_u64(negp[e]);  // P mod q_e
+        rot_sum_chains<BETA, NB, true>(row, c0, K, x, log_n, (size_t)t * N, (size_t)M * N, q, qinv, p > 0.5 * q ? p - q : p, sum);
+    } else {
+        rot_sum_chains<BETA, NB, false>(row, c0, K, x, log_n, (size_t)t * N, (size_t)M * N, q, qinv, 0.0, sum);
+    }
 #pragma unroll
     for (int i = 0; i < NB; i++) {
         if (b0 + i >= n) break;
@@ -266,32 +295,44 @@ __global__ __launch_bounds__(RC_THREADS) void rot_sum_kernel(DigitSrc digits, Ro
 #pragma unroll
         for (int c = 0; c < 2; c++) {
             u64* oc = o + (size_t)c * E * N;
-            const double v = add ? f64m_reduce(cl[c][i] + f64m_from_u64(*oc), q, qinv) : cl[c][i];
+            const double v = add ? f64m_reduce(sum[c][i] + f64m_from_u64(*oc), q, qinv) : sum[c][i];
             *oc = f64m_canonical(v, q);
         }
     }
 }
 
-hipError_t launch_rot_sum(const ckks_ctx* c, u32 level, const DigitSrc& digits, const u64* const* keys, const u32* gs, u32 n_keys, const u64* const* c0s, u64* const* outs, u32 n,
+bool rot_sum_applies(const ckks_ctx* c, u32 level) { return c->small_q && c->live_digits(level) <= 4; }
+hipError_t launch_rot_sum(const ckks_ctx* c, u32 level, const u64* digits, size_t bstride, const u64* const* keys, const u32* gs, u32 n_keys, const u64* const* cts, u64* const* outs, u32 n,
                           bool add, hipStream_t st) {
-    if (!c->small_q || n == 0 || n > KS_MAX_BATCH || n_keys == 0 || n_keys > ROT_SUM_KEYS) return hipErrorInvalidValue;
+    if (!rot_sum_applies(c, level) || n == 0 || n > KS_MAX_BATCH || n_keys == 0 || n_keys > ROT_SUM_KEYS) return hipErrorInvalidValue;
     const u32 E = c->ext_limbs(level), beta = c->live_digits(level), nxb = (c->N + RC_THREADS - 1) / RC_THREADS;
     RotSumKeys K = {};
     K.n = n_keys;
     for (u32 r = 0; r < n_keys; r++) K.key[r] = keys[r], K.g[r] = gs[r];
     PtrList8 cl;
     OutList8 ol;
-    for (u32 b = 0; b < KS_MAX_BATCH; b++) cl.p[b] = b < n ? c0s[b] : nullptr, ol.p[b] = b < n ? outs[b] : nullptr;
+    for (u32 b = 0; b < KS_MAX_BATCH; b++) cl.p[b] = b < n ? cts[b] : nullptr, ol.p[b] = b < n ? outs[b] : nullptr;
     const u64* negp = c->d_moddown + 2 * c->k_pad + (size_t)c->k_pad * c->num_q + 2 * c->num_q;
-    u32 nb = 8;
+    // ciphertexts a thread: as many as its registers hold, fewer where a launch would not give every CU four workgroups
+    u32 nb = beta <= 2 ? 8 : 4;
     while (nb > 1 && (nb / 2 >= n || (u64)nxb * E * ((n + nb - 1) / nb) < 1024)) nb /= 2;
-    const dim3 grid((nxb * E + 7) / 8 * 8, (n + nb - 1) / nb);
-    ProfScope ps__(c, K_KEY_INNER, st, 8.0 * c->N * (E * (n * (beta + (add ? 4.0 : 2.0)) + n_keys * 2.0 * beta * grid.y) + n * (level + 1.0)), 2.0 * n_keys * n * c->N * E * beta);
-#define ROT_SUM(NB_) hipLaunchKernelGGL(rot_sum_kernel<NB_>, grid, dim3(RC_THREADS), 0, st, digits, K, cl, ol, add ? 1u : 0u, negp, c->d_mcf, c->log_n, level, c->num_q, c->M, E, beta, n)
-    if (nb == 8) ROT_SUM(8);
-    else if (nb == 4) ROT_SUM(4);
-    else if (nb == 2) ROT_SUM(2);
-    else ROT_SUM(1);
+    const u32 groups = (n + nb - 1) / nb;
+    const dim3 grid((nxb * E * groups + 7) / 8 * 8);
+    ProfScope ps__(c, K_KEY_INNER, st, 8.0 * c->N * (E * (n * (beta + (add ? 4.0 : 2.0)) + n_keys * 2.0 * beta) + n * (level + 1.0)), 2.0 * n_keys * n * c->N * E * beta);
+#define ROT_SUM(B_, NB_) hipLaunchKernelGGL((rot_sum_kernel<B_, NB_>), grid, dim3(RC_THREADS), 0, st, digits, bstride, c->alpha, K, cl, ol, add ? 1u : 0u, negp, c->d_mcf, c->log_n, level, c->num_q, c->M, E, n)
+#define ROT_SUM_B(B_)                     \
+    {                                     \
+        if (nb == 4) ROT_SUM(B_, 4);      \
+        else if (nb == 2) ROT_SUM(B_, 2); \
+        else ROT_SUM(B_, 1);              \
+    }
+    if (nb == 8 && beta == 1) ROT_SUM(1, 8);
+    else if (nb == 8) ROT_SUM(2, 8);
+    else if (beta == 1) ROT_SUM_B(1)
+    else if (beta == 2) ROT_SUM_B(2)
+    else if (beta == 3) ROT_SUM_B(3)
+    else ROT_SUM_B(4)
+#undef ROT_SUM_B
 #undef ROT_SUM
     return hipGetLastError();
 }

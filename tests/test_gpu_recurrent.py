@@ -1,6 +1,7 @@
 """A recurrent block's operators on the GPU, through the C boundary, against the CPU oracle on the same seeded inputs: every residue equal (results are integers: there is
 no tolerance)."""
 import ctypes as C
+import gc
 
 import numpy as np
 import pytest
@@ -35,6 +36,14 @@ def world(log_n, num_q, num_p, dnum, bits=50):
             p = make_params(log_n, num_q, num_p, dnum, bits=bits)
         _worlds[key] = (p, Oracle(p), hx.Context(p))
     return _worlds[key]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def leave_nothing():
+    """Contexts, and tensors that refusals' tracebacks hold on to, go when this file is done: others watch the allocator."""
+    yield
+    _worlds.clear()
+    gc.collect()
 
 
 def ciphertexts(rng, p, level, n):
@@ -255,6 +264,15 @@ def test_sums_over_slots(stages):
     """None, one rotation a stage an odd and an even number of times, the same again, one twice in a stage, more rotations than a launch holds, mixed."""
     grad_case((12, 4, 2, 2, 50), 3, 2, False, stages, len(stages))
     grad_case((11, 4, 2, 2, 56), 3, 2, False, stages, len(stages) + 1)
+
+
+@pytest.mark.parametrize("dnum", [1, 2, 3, 4, 5, 8])
+@pytest.mark.parametrize("channels", [1, 2, 3, 5, 9])
+def test_sums_over_slots_by_digits_and_ciphertexts(dnum, channels):
+    """Every number of digits that has a kernel of its own and more, with both counts of ciphertexts a thread takes."""
+    ring = (12, 8, -(-8 // dnum), dnum, 50)
+    grad_case(ring, 7, channels, False, [(1, 2, 3, 4, 5, 6, 7), (-1, 5)], dnum + channels)
+    grad_case((11, 8, -(-8 // dnum), dnum, 50), 3, channels, False, [(3,), (1, 2, 3)], dnum + channels, want_gain=False)
 
 
 def test_layer_norm_gradients_of_a_large_ring():
