@@ -185,7 +185,9 @@ hipError_t launch_norm_grad_terms(const ckks_ctx* c, u32 level, const NormGradTe
 // key word is read once for them, and gathers their digits through each automorphism in turn (a wavefront's 64 points are one aligned run of 512 bytes).  Workgroups are dealt to the eight
 // dies in turn: each die takes a contiguous eighth of the (limb, points, ciphertexts) list, so that what the rotations gather again, and the keys for the next ciphertexts, come from its own L2
 // cache.  16 ciphertexts of 12 + 8 limbs at N = 2^16, seven rotations: 480 us; 1.0 GB have to be moved (196 us), the arithmetic alone takes 220.  An inner product and an addition for every
-// rotation took 1160 us; with one term after the other behind branches 530; four ciphertexts a thread 517, two 570; four points of two ciphertexts 575.
+// rotation took 1160 us; with one term after the other behind branches 530; four ciphertexts a thread 517, two 570; four points of two ciphertexts 575.  It fetches 1.3 GB where the stage's rotations share runs of
+// points and 2.5 where they do not; an order of the runs along the first rotation's orbits brought the latter to 1.1 and the kernel from 490 us to 482 on average, too little for its code: the
+// waits for gathered words and the arithmetic bound it, not the traffic.
 struct RotSumKeys {
     const u64* key[ROT_SUM_KEYS];
     u32 g[ROT_SUM_KEYS];

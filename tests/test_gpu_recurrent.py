@@ -314,24 +314,24 @@ def calls(ring=(12, 7, 3, 3, 50), seed=3):
     p, ctx, N = turns.p, turns.ctx, turns.orc.N
     level = ring[1] - 1
     ct = lambda n, limbs=level + 1: hx.from_host(ciphertexts(rng, p, limbs - 1, n))  # noqa: E731
-    x, gate, states, rlk = ct(10), ct(2), ct(10, level - 1), hx.ckks_key_load(ctx, hx.from_host(random_key(rng, p)), 0)
+    x, gate, states, rlk = ct(18), ct(2), ct(18, level - 1), hx.ckks_key_load(ctx, hx.from_host(random_key(rng, p)), 0)
     fwd, bwd, back = turns.lists((-1, -2))[2:], turns.lists((1, 2))[2:], turns(-1)[1]
     k, m = [1 << 50, 3 << 49], level - 4
-    gain, bias, inv = ct(10), ct(10), ct(1)[0]
+    gain, bias, inv = ct(18), ct(18), ct(1)[0]
     sums = [[turns(o)[1][0] for o in (1, 2, 3)], [turns(4)[1][0]]]
     return ctx, {
         "scan": (lambda ws, o, st=None: hx.he_scan_gated(ctx, level, x, gate, k, *fwd, out=o[0], ws=ws, stream=st),
-                 hx.he_scan_workspace_bytes(ctx, level, 10, 2, 2), [(10, 2, level - 1, N)]),
+                 hx.he_scan_workspace_bytes(ctx, level, 18, 2, 2), [(18, 2, level - 1, N)]),
         "scan_backward": (lambda ws, o, st=None: hx.he_scan_gated_backward(ctx, level, x, gate, states, k, *bwd, *back, dx=o[0], dgate=o[1], ws=ws, stream=st),
-                          hx.he_scan_backward_workspace_bytes(ctx, level, 10, 2, 2), [(10, 2, level - 1, N), (2, 2, level - 2, N)]),
+                          hx.he_scan_backward_workspace_bytes(ctx, level, 18, 2, 2), [(18, 2, level - 1, N), (2, 2, level - 2, N)]),
         "step": (lambda ws, o, st=None: hx.he_scan_step(ctx, level, gate, x, back[1], back[0], bias, 1 << 50, out=o[0], ws=ws, stream=st),
-                 hx.he_scan_step_workspace_bytes(ctx, level, 10, 2), [(10, 2, level, N)]),
+                 hx.he_scan_step_workspace_bytes(ctx, level, 18, 2), [(18, 2, level, N)]),
         "step_in_place": (lambda ws, o, st=None: hx.he_scan_step(ctx, level, gate, x, rlk, None, bias, 1 << 50, out=o[0], ws=ws, stream=st),
-                          hx.he_scan_step_workspace_bytes(ctx, level, 10, 2), [(10, 2, level, N)]),
+                          hx.he_scan_step_workspace_bytes(ctx, level, 18, 2), [(18, 2, level, N)]),
         "norm": (lambda ws, o, st=None: hx.he_layer_norm(ctx, level, x, 1 << 40, -(3 << 47), 5 << 48, (3 << 49,), rlk, gain, bias, 1 << 49, norm=o[0], inv=o[1], out=o[2], ws=ws, stream=st),
-                 hx.he_layer_norm_workspace_bytes(ctx, level, 10, 1, True), [(10, 2, m, N), (2, m + 1, N), (10, 2, m - 1, N)]),
+                 hx.he_layer_norm_workspace_bytes(ctx, level, 18, 1, True), [(18, 2, m, N), (2, m + 1, N), (18, 2, m - 1, N)]),
         "norm_backward": (lambda ws, o, st=None: hx.he_layer_norm_backward(ctx, level, x, bias, inv, 1 << 20, -(1 << 20), rlk, gain, sums, dx=o[0], dgain=o[1], dbias=o[2], ws=ws, stream=st),
-                          hx.he_layer_norm_backward_workspace_bytes(ctx, level, 10, True, 2), [(10, 2, level - 3, N), (10, 2, level, N), (10, 2, level, N)]),
+                          hx.he_layer_norm_backward_workspace_bytes(ctx, level, 18, True, 2), [(18, 2, level - 3, N), (18, 2, level, N), (18, 2, level, N)]),
     }
 
 
@@ -528,3 +528,18 @@ def test_contexts_without_key_switching_refuse():
     ctx = hx.Context(p)
     for need in (hx.he_scan_workspace_bytes(ctx, 3, 1, 1, 1), hx.he_layer_norm_workspace_bytes(ctx, 3, 1, 0), hx.he_layer_norm_backward_workspace_bytes(ctx, 3, 1)):
         assert need == 0
+
+
+# ------------------------------------------------------------------------------------------ together
+@pytest.mark.parametrize("log_n", [12, 13])
+def test_the_example_agrees_with_float64(log_n):
+    """examples/encrypted_recurrence.py: norm, recurrence, step and both backward passes one after the other, decrypted, within what the Newton iterations and the constants' rounding
+    leave.  (That the float64 gradients are the differences of its loss is tested without a GPU.)"""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "encrypted_recurrence.py")
+    spec = importlib.util.spec_from_file_location("encrypted_recurrence", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    for name, (diff, bound) in module.run(log_n, seed=log_n, verbose=False).items():
+        assert diff <= bound, name

@@ -219,3 +219,37 @@ def test_constants_refuse_what_they_cannot_serve():
     with pytest.raises(ValueError):
         scan_steps(0)
     assert scan_gate_mask([1, 3, 0, 2], 8).tolist() == [0, 0, 1, 1, 0, 1, 0, 0] and scan_gate_mask([1, 3, 0, 2], 8, True).tolist() == [0, 1, 1, 0, 1, 0, 0, 0]
+
+
+def test_the_examples_gradients_are_differences():
+    """examples/encrypted_recurrence.py: its float64 gradients against central differences of its loss sum(upstream * states).  The loss is linear in gain and bias and in each gate alone
+    (exact but for rounding); along the inputs a step of 1e-4 leaves its square times a third derivative, below 1e3 here (inv^3 up to 30, states' sums up to 30)."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "encrypted_recurrence.py")
+    spec = importlib.util.spec_from_file_location("encrypted_recurrence", path)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    rng, n = np.random.default_rng(0), 24
+    mask = scan_gate_mask([3, 8, 1, 5, 7], n)
+    x = rng.uniform(0.4, 1.0, (ex.CHANNELS, n)) * np.array([1.0, -1.0, 1.0, -1.0])[:, None]
+    gain, bias, up, gate = rng.uniform(0.5, 1.5, ex.CHANNELS), rng.uniform(-1, 1, ex.CHANNELS), rng.uniform(-1, 1, (ex.CHANNELS, n)), rng.uniform(0.3, 1.0, (ex.HEADS, n)) * mask
+    _, dx, dgate, dgain, dbias = ex.reference(x, gain, bias, gate, up)
+    loss = lambda x, gain, bias, gate: float((up * ex.recurrence(ex.layer_norm(x, gain, bias)[2], gate)).sum())  # noqa: E731
+
+    def slope(which, at, step):
+        args = [x, gain, bias, gate]
+        ends = []
+        for sign in (1, -1):
+            moved = args[which].copy()
+            moved[at] += sign * step
+            ends.append(loss(*args[:which], moved, *args[which + 1:]))
+        return (ends[0] - ends[1]) / (2 * step)
+
+    for _ in range(20):
+        c, t, h = int(rng.integers(ex.CHANNELS)), int(rng.integers(n)), int(rng.integers(ex.HEADS))
+        assert abs(slope(0, (c, t), 1e-4) - dx[c, t]) < 1e-5
+        assert abs(slope(1, c, 0.5) - dgain[c].sum()) < 1e-9
+        assert abs(slope(2, c, 0.5) - dbias[c].sum()) < 1e-9
+        if mask[t]:
+            assert abs(slope(3, (h, t), 0.5) - dgate[h, t]) < 1e-9
