@@ -16,7 +16,7 @@
  *     ckks_last_error_string() gives the reason of the last failure on that context.
  *   - Pointers named d_* are DEVICE pointers owned by the caller; pointers named h_* and all
  *     structs are HOST memory.  Hot calls never allocate, free or synchronise: work is enqueued on
- *     the caller's stream (a hipStream_t passed as void*, NULL = default stream; three calls may put
+ *     the caller's stream (a hipStream_t passed as void*, NULL = default stream; some calls may put
  *     part of it on a second stream of the context's, joined before they return: see
  *     ckks_ctx_set_overlap) and scratch space comes from the caller's workspace (d_ws, ws_bytes; size
  *     from the *_workspace_bytes() queries).  The caller keeps every buffer alive until the stream
@@ -78,7 +78,8 @@ void ckks_ctx_destroy(ckks_ctx* ctx);
 const char* ckks_last_error_string(const ckks_ctx* ctx);
 
 /* Scheduling (not from the paper).  Operations made of independent channel batches (he_conv_batched in the deferred
- * schedules, he_poly_act_deg7, he_norm_gate, whose gates also run there beside its Newton chain) run every other batch on a second
+ * schedules, he_poly_act_deg7, he_norm_gate, whose gates also run there beside its Newton chain, he_scan_gated, he_scan_step,
+ * he_layer_norm and the backward passes he_scan_gated_backward and he_layer_norm_backward) run every other batch on a second
  * stream owned by the context, between a fork after the caller's earlier work and a join before the call's last enqueue on the
  * caller's stream: arithmetic-bound and traffic-bound kernels of different batches overlap.  The caller still sees one ordered stream.  on = 0 keeps all work
  * on the caller's stream (per-kernel timings are then not blurred by overlap); default on.  Results are identical.
