@@ -399,6 +399,46 @@ def test_on_another_stream(name):
     assert all(torch.equal(a, b) for a, b in zip(ref, outs))
 
 
+@pytest.mark.parametrize("ring", [(12, 7, 3, 3, 50), (14, 7, 3, 3, 50), (12, 7, 3, 3, 56)])
+@pytest.mark.parametrize("name", NAMES)
+def test_two_calls_at_once(name, ring):
+    """One context, two streams, a workspace each: nothing waits on the host between the calls, and the context's second stream serves both."""
+    ctx, ops = calls(ring)
+    call, need, shapes = ops[name]
+    first, second = ([torch.empty(need, dtype=torch.uint8, device="cuda"), torch.cuda.Stream(), outputs(shapes)[1]] for _ in range(2))
+    _, ref = outputs(shapes)
+    call(first[0], ref)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for ws, stream, outs in (first, second):
+            call(ws, outs, stream.cuda_stream)
+    torch.cuda.synchronize()
+    for _, _, outs in (first, second):
+        assert all(torch.equal(a, b) for a, b in zip(ref, outs))
+
+
+@pytest.mark.parametrize("bits", [50, 56])
+def test_operands_far_apart(bits):
+    """Ciphertexts 2^30 words (8 GiB) and their components more than 2^29 words from each other: offsets pass 32 bits in bytes and, at the fifth, in words."""
+    ring, level, channels, far, comp = (12, 6, 2, 3, bits), 5, 5, 1 << 30, (1 << 29) + 4096
+    rng = np.random.default_rng(5)
+    turns = Turns(ring, rng)
+    p, ctx, N = turns.p, turns.ctx, turns.orc.N
+    pool = torch.empty((channels - 1) * far + comp + (level + 1) * N, dtype=torch.int64, device="cuda")
+    apart = pool.as_strided((channels, 2, level + 1, N), (far, comp, N, 1))
+    near, gate, rlk = hx.from_host(ciphertexts(rng, p, level, channels)), hx.from_host(ciphertexts(rng, p, level, 1)), hx.ckks_key_load(ctx, hx.from_host(random_key(rng, p)), 0)
+    apart.copy_(near)
+    fwd, bwd, back = turns.lists((-1, -2))[2:], turns.lists((1, 2))[2:], turns(-1)[1]
+    k = [1 << 50, 3 << 49]
+    for f in (lambda x: [hx.he_scan_gated(ctx, level, x, gate, k, *fwd)],
+              lambda x: hx.he_scan_gated_backward(ctx, level, x, gate, x, k, *bwd, *back),
+              lambda x: [hx.he_scan_step(ctx, level, x, x, back[1], back[0], x, 1 << 50)],
+              lambda x: [hx.he_scan_step(ctx, level, x, x, rlk, None, x, 1 << 50)],
+              lambda x: hx.he_layer_norm(ctx, level, x, 1 << 40, -(3 << 47), 5 << 48, (), rlk, x, x, 1 << 49),
+              lambda x: hx.he_layer_norm_backward(ctx, level, x, x, gate[0], 1 << 20, -(1 << 20), rlk, x, [[back[0], fwd[0][1]]])):
+        assert all(torch.equal(a, b) for a, b in zip(f(near), f(apart)))
+
+
 @pytest.mark.parametrize("ring", [(13, 7, 3, 3, 50), (14, 7, 3, 3, 50), (12, 7, 3, 3, 56)])
 @pytest.mark.parametrize("name", NAMES)
 def test_one_stream_and_two_agree(name, ring):
