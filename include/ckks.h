@@ -468,6 +468,8 @@ int he_layer_norm(const ckks_ctx* ctx, const he_layer_norm_desc* desc, const int
  * k_norm has the sign that makes it C inv (g - mean g - norm mean(g norm)) (layer_norm_grad_constants).  Sum adds up slots in n_stages stages: z <- z + the sum of its rotations
  * by the h_stage_rots[i] keys of stage i, with one decomposition and one division by P for all of them; sum_keys holds the stages' keys one after the other.  One rotation a stage
  * (1, 2, 4, ..) doubles what is summed, three (1, 2, 3; 4, 8, 12; ..) give four times; n_stages = 0: the gradients slot by slot.
+ * At the lowest level dx has the limb of q_0 alone: |dx| times its scale, which holds C k_grad and the scales of inv and g, has to stay below q_0 / 2 there, so k_grad small and grad's scale
+ * well below the primes (layer_norm_grad_constants takes the former where it can, and refuses).
  * Limbs read: grad, gain, norm 0 .. level, inv 0 .. b-1; level >= 3, 4 with a gain.  d_dx uint64[C][2][b-2][N]; d_dgain, d_dbias uint64[C][2][level][N], or NULL: not wanted. */
 #define HE_SUM_MAX_STAGES 64
 typedef struct he_layer_norm_grad_desc {

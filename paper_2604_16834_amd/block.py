@@ -4,6 +4,7 @@ scales it has to track.  Nothing here touches ciphertexts or the GPU."""
 from __future__ import annotations
 
 import math
+from fractions import Fraction
 from typing import NamedTuple, Optional, Sequence, Tuple
 
 import numpy as np
@@ -129,6 +130,11 @@ def _check_int64(*values: int) -> None:
         raise ValueError("a constant passes 63 bits: the inputs' scale is too far from the moduli")
 
 
+def _room(q: Sequence[float], level: int) -> float:
+    """What a value times its scale may be at ``level``: coefficients are at most that, below half the product q_0 .. q_level with a part left for noise."""
+    return math.prod(q[:level + 1]) * (0.5 - 2.0 ** -7)
+
+
 def norm_constants(moduli: Sequence[int], level: int, channels: int, scale: float, interval: Tuple[float, float], iterations: int, eps: float = 0.0,
                    gate_scale: Optional[float] = None, residual: Optional[Tuple[float, float]] = None) -> NormConstants:
     """The integers of ``he_norm_gate`` for inputs at ``scale`` (close to the moduli: the mean square has the scale channels * scale^2 /
@@ -184,9 +190,11 @@ class LayerNormGradConstants(NamedTuple):
 
 
 def layer_norm_grad_constants(moduli: Sequence[int], level: int, channels: int, grad_scale: float, norm_scale: float, inv_scale: float, gain_scale: Optional[float] = None,
-                              bits: int = 16) -> LayerNormGradConstants:
+                              bits: int = 16, largest: float = 1.0) -> LayerNormGradConstants:
     """The integers of ``he_layer_norm_backward`` for a gradient at ``grad_scale``: k_norm / k_grad is minus the ratio of the scales of the two terms of
-    channels * dx, to within 2^-(bits + 1), as both are at least 2^bits; dx's scale holds the factors channels and k_grad."""
+    channels * dx, to within 2^-(bits + 1); dx's scale holds the factors channels and k_grad.  Both integers are at least 2^bits, or, where dx's modulus has no room for that
+    (at level 3, with a gain 4, a single prime is left), the smallest found that meet the ratio as closely: small ones do where it is close to a simple fraction, as it is for a norm of
+    ``layer_norm_constants``.  largest: a bound on |dx|.  Raises ValueError where dx does not fit: a smaller grad_scale, fewer bits or a level more are needed then."""
     q = [float(int(m)) for m in moduli]
     if level < (3 if gain_scale is None else 4):
         raise ValueError("need level >= 3, 4 with a gain")
@@ -194,10 +202,21 @@ def layer_norm_grad_constants(moduli: Sequence[int], level: int, channels: int, 
     g_scale = grad_scale if gain_scale is None else gain_scale * grad_scale / q[level]
     t_scale = inv_scale * (g_scale * norm_scale / q[b]) / q[b - 1]
     ratio = inv_scale * g_scale / (t_scale * norm_scale)
+    unit = channels * inv_scale * g_scale / q[b - 2]  # dx's scale for k_grad = 1
+    most = _room(q, b - 3) / (unit * largest)
     k_grad = max(1, math.ceil(2.0 ** bits * max(1.0, 1.0 / ratio)))
+    if k_grad > most:
+        span, exact = 1, Fraction(ratio)
+        while span < k_grad:
+            near = exact.limit_denominator(span)
+            if abs(near / exact - 1) <= Fraction(2.0 ** -(bits + 1)):
+                k_grad = near.denominator
+            span *= 2
+        if k_grad > most:
+            raise ValueError("no room for dx at its level: its scale times its largest value passes half of the modulus that is left")
     k_norm = -round(k_grad * ratio)
     _check_int64(k_grad, k_norm)
-    return LayerNormGradConstants(k_grad, k_norm, b - 3, channels * k_grad * inv_scale * g_scale / q[b - 2], grad_scale * norm_scale / q[level], grad_scale)
+    return LayerNormGradConstants(k_grad, k_norm, b - 3, k_grad * unit, grad_scale * norm_scale / q[level], grad_scale)
 
 
 # ------------------------------------------------------------------------------------------ gated recurrence

@@ -1,0 +1,64 @@
+"""Layer norm and its gradients at the lowest levels that their constants accept, where results have few primes left, decrypted from the CPU oracle: slots that differ and slots that are all alike
+(whose polynomial has the value times the scale as one coefficient, the most that a modulus has to hold).
+
+Tolerances as in test_oracle_recurrent.py, with gradients at the scale 2^40: an operation there is off by less than 2^20 / 2^40 = 1e-6, which 1 / sqrt below 2, gains up to 1.5 and the three terms of
+dx, each at most (1 + the largest |norm|^2) times the gradient's, multiply by at most 30; the constants' ratio adds 2^-17 of a term below 8.  Both together are below 1e-4."""
+import numpy as np
+import pytest
+
+from test_oracle_recurrent import BOUND, EPS, SCALE, World, layer_norm
+from paper_2604_16834_amd.block import layer_norm_constants, layer_norm_grad_constants
+
+GRAD_SCALE = 2.0 ** 40
+
+
+@pytest.fixture(scope="module")
+def world():
+    return World()
+
+
+def channels_of(rng, channels, n, alike):
+    x = rng.uniform(0.4, 1.0, (channels, n)) * np.where(np.arange(channels) % 2, -1, 1)[:, None]
+    return np.repeat(x[:, :1], n, 1) if alike else x
+
+
+@pytest.mark.parametrize("alike", [False, True])
+@pytest.mark.parametrize("affine", [False, True])
+@pytest.mark.parametrize("above", [0, 1])
+def test_layer_norm_gradients_at_the_lowest_levels(world, affine, alike, above):
+    w, rng, channels, level = world, np.random.default_rng(5), 4, 3 + affine + above
+    n = w.orc.n
+    x, up, gain = channels_of(rng, channels, n, alike), channels_of(rng, channels, n, alike), rng.uniform(0.5, 1.5, channels)
+    norm, inv, _ = layer_norm(x)
+    assert inv.max() < 2
+    k = layer_norm_constants(w.p.moduli, 15, channels, 2.0 ** 47, (0.3, 1.1), 3, EPS)  # the scales that a forward call leaves
+    g = layer_norm_grad_constants(w.p.moduli, level, channels, GRAD_SCALE, k.norm_scale, k.inv_scale, SCALE if affine else None)
+    ct_gain = w.encrypt(np.repeat(gain[:, None], n, 1), level, SCALE, 40) if affine else None
+    ct_up, ct_norm = w.encrypt(up, level, GRAD_SCALE, 90), w.encrypt(norm, level, k.norm_scale, 20)
+    dx, dgain, dbias = w.orc.layer_norm_backward(ct_up, ct_norm, w.encrypt(inv[None], level, k.inv_scale, 30)[0], level, g.k_grad, g.k_norm, w.rlk, ct_gain)
+    gy = up * gain[:, None] if affine else up
+    want = inv * (gy - gy.mean(0) - norm * (gy * norm).mean(0))
+    assert g.dx_level == above
+    assert np.abs(w.decrypt(dx, g.dx_level, g.dx_scale) - want).max() < BOUND
+    assert np.abs(w.decrypt(dgain, level - 1, g.dgain_scale) - up * norm).max() < BOUND
+    assert np.abs(w.decrypt(dbias, level - 1, g.dbias_scale) - up).max() < BOUND
+
+
+def test_gradient_constants_where_there_is_room_and_where_not(world):
+    q = world.p.moduli
+    norm_scale, inv_scale = q[3] / 2.0 ** 0.5, 2.0 ** 50
+    # far from the end: both constants at least 2^bits
+    g = layer_norm_grad_constants(q, 6, 4, SCALE, norm_scale, inv_scale)
+    assert min(g.k_grad, -g.k_norm) >= 1 << 16
+    # the last prime holds values below 2^49 alone: smaller constants of the same ratio, and a refusal where these do not fit either
+    ratio = -g.k_norm / g.k_grad
+    small = layer_norm_grad_constants(q, 3, 4, GRAD_SCALE, norm_scale, inv_scale)
+    assert small.dx_level == 0 and 2.0 * small.dx_scale < q[0]
+    assert abs(-small.k_norm / small.k_grad / ratio - 1) < 2.0 ** -16
+    for kw in (dict(grad_scale=SCALE), dict(grad_scale=GRAD_SCALE, largest=2.0 ** 8), dict(grad_scale=GRAD_SCALE, norm_scale=norm_scale * 1.2345678)):
+        with pytest.raises(ValueError, match="room"):
+            layer_norm_grad_constants(**{**dict(moduli=q, level=3, channels=4, norm_scale=norm_scale, inv_scale=inv_scale), **kw})
+    # a ratio that no small constants meet, with fewer bits asked for
+    g = layer_norm_grad_constants(q, 3, 4, 2.0 ** 36, norm_scale * 1.2345678, inv_scale, bits=6)
+    ratio = float(q[3]) * q[2] / (norm_scale * 1.2345678) ** 2
+    assert abs(-g.k_norm / g.k_grad / ratio - 1) <= 2.0 ** -7 and 2.0 * g.dx_scale < q[0]
