@@ -99,8 +99,8 @@ class _InverseRoot(NamedTuple):
     relative_error: float
 
 
-def _inverse_root(q: Sequence[float], level: int, s_scale: float, interval: Tuple[float, float], iterations: int, eps: float) -> _InverseRoot:
-    """The guess and the Newton steps of 1 / sqrt(v) for v at ``s_scale``, level - 1 (see ``norm_constants``)."""
+def _inverse_root(q: Sequence[float], level: int, s_scale: float, interval: Tuple[float, float], iterations: int, eps: float, most: float = math.inf) -> _InverseRoot:
+    """The guess and the Newton steps of 1 / sqrt(v) for v at ``s_scale``, level - 1 (see ``norm_constants``); most: a bound on the scale of the result."""
     lo, hi = interval
     if not 0 < lo < hi:
         raise ValueError("need 0 < lo < hi")
@@ -113,6 +113,11 @@ def _inverse_root(q: Sequence[float], level: int, s_scale: float, interval: Tupl
     a, error = 2.0 / (top + end), (top - end) / (top + end)
     m = level - 2
     r_scale = math.sqrt(q[m] * q[m] * q[max(m - 1, 0)] / (2.0 * s_scale))
+    last = r_scale  # behind the steps
+    for n in range(m, m - 2 * iterations, -2):
+        last = 2.0 * (last * last / q[n]) * (s_scale * last / q[n]) / q[n - 1]
+    if most < last < math.inf:  # every step cubes what the scale is below the one that stays
+        r_scale *= (most / last) ** (3.0 ** -iterations)
     k_eps = round(eps * s_scale)
     k_slope, k_start = round(-sign * a * b * r_scale * q[level - 1] / s_scale), round(sign * a * r_scale)
     newton = []
@@ -168,11 +173,15 @@ class LayerNormConstants(NamedTuple):
 def layer_norm_constants(moduli: Sequence[int], level: int, channels: int, scale: float, interval: Tuple[float, float], iterations: int, eps: float = 0.0,
                          gain_scale: Optional[float] = None, bias_scale: Optional[float] = None) -> LayerNormConstants:
     """The integers of ``he_layer_norm`` for inputs at ``scale`` whose variances over the channels plus eps lie in ``interval``: what the Newton chain works on is channels^2
-    times the variance, at the scale channels^2 scale^2 / q_level; the centred channels have channels times the inputs' scale."""
+    times the variance, at the scale channels^2 scale^2 / q_level; the centred channels have channels times the inputs' scale.  norm, at most sqrt(channels - 1) in magnitude, has
+    the scale that a Newton step leaves as it is, or one at which it fits where it ends at level 0; with a gain out_scale times the largest |out| is the caller's to keep below half
+    of q_0 .. q_(norm_level - 1), by gain_scale."""
     q = [float(int(m)) for m in moduli]
     if gain_scale is not None and level < 4 + 2 * iterations:
         raise ValueError("a gain needs one more level")
-    r = _inverse_root(q, level, channels * channels * scale * scale / q[level], interval, iterations, eps)
+    last = max(level - 2 - 2 * iterations, 1)
+    most = _room(q, last - 1) / math.sqrt(max(channels - 1, 1)) * q[last] / (channels * scale)
+    r = _inverse_root(q, level, channels * channels * scale * scale / q[level], interval, iterations, eps, most)
     norm_scale, m = channels * scale * r.scale / q[r.level], r.level - 1
     k_bias = round(gain_scale * norm_scale / bias_scale) if gain_scale is not None and bias_scale is not None else 0
     _check_int64(r.k_eps, r.k_slope, r.k_start, k_bias, *r.k_newton)

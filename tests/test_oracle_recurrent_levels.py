@@ -62,3 +62,19 @@ def test_gradient_constants_where_there_is_room_and_where_not(world):
     g = layer_norm_grad_constants(q, 3, 4, 2.0 ** 36, norm_scale * 1.2345678, inv_scale, bits=6)
     ratio = float(q[3]) * q[2] / (norm_scale * 1.2345678) ** 2
     assert abs(-g.k_norm / g.k_grad / ratio - 1) <= 2.0 ** -7 and 2.0 * g.dx_scale < q[0]
+
+
+@pytest.mark.parametrize("alike", [False, True])
+@pytest.mark.parametrize("channels,iterations", [(2, 1), (4, 0), (9, 2), (17, 1)])
+def test_layer_norm_that_ends_at_the_last_prime(world, channels, iterations, alike):
+    """Without a gain, from the lowest level: norm at level 0, up to sqrt(channels - 1) in magnitude.  The error of 1 / sqrt is relative to the result; the rest as in test_oracle_recurrent.py."""
+    w, rng, level = world, np.random.default_rng(channels), 3 + 2 * iterations
+    x = channels_of(rng, channels, w.orc.n, alike)
+    x[0] *= 1 if channels < 9 else 8  # one channel that holds nearly all of the variance
+    var = x.var(0) + EPS
+    k = layer_norm_constants(w.p.moduli, level, channels, 2.0 ** 46, (0.99 * var.min(), 1.01 * var.max()), iterations, EPS)
+    norm, inv, _ = w.orc.layer_norm(w.encrypt(x, level, 2.0 ** 46), level, k.k_eps, k.k_slope, k.k_start, k.k_newton, w.rlk)
+    want, want_inv, _ = layer_norm(x)
+    assert k.norm_level == 0
+    assert np.abs(w.decrypt(norm, 0, k.norm_scale) - want).max() < BOUND + k.relative_error * np.abs(want).max()
+    assert np.abs(w.decrypt([inv], 1, k.inv_scale) - want_inv).max() < BOUND + k.relative_error * want_inv.max()
