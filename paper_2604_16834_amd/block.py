@@ -147,9 +147,13 @@ def norm_constants(moduli: Sequence[int], level: int, channels: int, scale: floa
 
     The first guess is the line a (1 - b v) whose error against 1 / sqrt(v) is the same at both ends and in the middle; a Newton step turns
     r sqrt(v) = 1 + e into 1 - (3 + e) e^2 / 2, so the first step's worst error is at e > 0 and all later ones come from below.  The scale of r is the one that a step leaves as it is: twice the scale of
-    u * w, r^2 and s r each divided by one modulus, the product by another."""
+    u * w, r^2 and s r each divided by one modulus, the product by another.  Outputs without gate and residual, at most sqrt(channels) in magnitude, get a scale at which they fit where
+    they end at level 0; with either, out_scale times the largest output is the caller's to keep below half of q_0 .. q_out_level."""
     q = [float(int(m)) for m in moduli]
-    r = _inverse_root(q, level, channels * scale * scale / q[level], interval, iterations, eps)
+    last = max(level - 2 - 2 * iterations, 1)
+    plain = gate_scale is None and residual is None
+    most = _room(q, last - 1) / math.sqrt(channels) * q[last] / scale if plain else math.inf
+    r = _inverse_root(q, level, channels * scale * scale / q[level], interval, iterations, eps, most)
     t_scale = scale if gate_scale is None else scale * gate_scale / q[level]
     k_residual = round(residual[0] * t_scale * r.scale / residual[1]) if residual else 0
     _check_int64(r.k_eps, r.k_slope, r.k_start, k_residual, *r.k_newton)

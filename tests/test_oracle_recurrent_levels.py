@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 
 from test_oracle_recurrent import BOUND, EPS, SCALE, World, layer_norm
-from paper_2604_16834_amd.block import layer_norm_constants, layer_norm_grad_constants
+from paper_2604_16834_amd.block import layer_norm_constants, layer_norm_grad_constants, norm_constants
 
 GRAD_SCALE = 2.0 ** 40
 
@@ -78,3 +78,18 @@ def test_layer_norm_that_ends_at_the_last_prime(world, channels, iterations, ali
     assert k.norm_level == 0
     assert np.abs(w.decrypt(norm, 0, k.norm_scale) - want).max() < BOUND + k.relative_error * np.abs(want).max()
     assert np.abs(w.decrypt([inv], 1, k.inv_scale) - want_inv).max() < BOUND + k.relative_error * want_inv.max()
+
+
+@pytest.mark.parametrize("alike", [False, True])
+@pytest.mark.parametrize("channels,iterations", [(1, 1), (2, 1), (4, 0), (9, 2)])
+def test_root_mean_square_norm_that_ends_at_the_last_prime(world, channels, iterations, alike):
+    """The norm without a mean, which shares the chain: outputs at level 0, up to sqrt(channels) where one channel holds nearly everything.  Tolerance as above."""
+    w, rng, level = world, np.random.default_rng(channels), 3 + 2 * iterations
+    x = channels_of(rng, channels, w.orc.n, alike)
+    x[1:] *= 0.05
+    square = (x * x).mean(0) + EPS
+    k = norm_constants(w.p.moduli, level, channels, 2.0 ** 47, (0.99 * square.min(), 1.01 * square.max()), iterations, EPS)
+    out = w.orc.norm_gate(w.encrypt(x, level, 2.0 ** 47), level, k.k_eps, k.k_slope, k.k_start, k.k_newton, w.rlk)
+    want = x / np.sqrt(square)
+    assert k.out_level == 0
+    assert np.abs(w.decrypt(out, 0, k.out_scale) - want).max() < BOUND + k.relative_error * np.abs(want).max()
