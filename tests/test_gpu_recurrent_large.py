@@ -80,3 +80,54 @@ def test_a_single_relinearised_sum_of_many_slices(level):
 def test_layer_norm_and_its_gradients_of_the_largest_ring():
     norm_case((17, 5, 2, 3, 50), 4, 3, 0, True, True, 17)
     grad_case((17, 5, 2, 3, 50), 4, 2, True, [(1, 2, 3), (4,)], 18)
+
+
+# ------------------------------------------------------------------------------------------ sums over slots
+# A thread of the sums' kernel takes 8 (up to two digits) or 4 ciphertexts, halved while a half holds all or the launch has fewer than 1024 workgroups: N / 256 x limbs of the extended basis x groups
+# of ciphertexts.  Every (digits, ciphertexts a thread) there is, by (ring, level, channels, both gradients or one): the sums run a level below, on channels or twice as many ciphertexts.
+SUMS = {
+    (1, 8): ((14, 5, 5, 1, 50), 4, 5, True),      # ten ciphertexts: eight and two
+    (1, 4): ((14, 5, 5, 1, 50), 4, 3, True),      # four and two
+    (1, 2): ((14, 5, 5, 1, 50), 4, 3, False),     # two and one
+    (1, 1): ((14, 5, 5, 1, 50), 4, 1, False),
+    (2, 8): ((14, 6, 3, 2, 50), 5, 5, True),
+    (2, 4): ((14, 6, 3, 2, 50), 5, 3, True),
+    (2, 2): ((14, 6, 3, 2, 50), 5, 3, False),
+    (2, 1): ((14, 6, 3, 2, 50), 5, 1, False),
+    (3, 4): ((14, 8, 3, 3, 50), 7, 3, True),
+    (3, 2): ((14, 8, 3, 3, 50), 7, 3, False),
+    (3, 1): ((14, 8, 3, 3, 50), 7, 1, False),
+    (4, 4): ((14, 8, 2, 4, 50), 7, 3, True),
+    (4, 2): ((14, 8, 2, 4, 50), 7, 3, False),
+    (4, 1): ((14, 8, 2, 4, 50), 7, 1, False),
+}
+
+
+def ciphertexts_a_thread(log_n, limbs, digits, n):
+    per = 8 if digits <= 2 else 4
+    while per > 1 and (per // 2 >= n or (1 << log_n) // 256 * limbs * -(-n // per) < 1024):
+        per //= 2
+    return per
+
+
+@pytest.mark.parametrize("form", list(SUMS))
+def test_sums_over_slots_in_every_form(form):
+    """A stage of seven rotations (several chains of additions), and one of two, the first of which reads what the stage before has written."""
+    ring, level, channels, both = SUMS[form]
+    log_n, num_q, num_p, dnum, _ = ring
+    digits = -(-level // -(-num_q // dnum))  # level limbs a level below
+    assert (digits, ciphertexts_a_thread(log_n, level + num_p, digits, channels * (1 + both))) == form
+    grad_case(ring, level, channels, False, [(1, 2, 3, 4, 5, 6, 7), (8, -3)], 10 * digits + channels, want_gain=both)
+
+
+@pytest.mark.parametrize("form", [(1, 8), (2, 8), (3, 4), (4, 2)])
+def test_sums_over_slots_of_more_rotations_than_a_launch_holds(form):
+    """35 rotations: a second launch adds to the first one's sums."""
+    ring, level, channels, both = SUMS[form]
+    grad_case(ring, level, channels, False, [tuple(range(1, 36))], channels, want_gain=both)
+
+
+@pytest.mark.parametrize("channels", [8, 7])
+def test_sums_over_slots_of_a_full_batch(channels):
+    """Sixteen ciphertexts, eight a thread; fourteen, eight and six."""
+    grad_case((14, 6, 3, 2, 50), 5, channels, False, [(1, 2, 3)], channels)
