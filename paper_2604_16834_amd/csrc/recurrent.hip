@@ -8,9 +8,9 @@
 #define RC_THREADS 256
 
 // ---- a sigma_g(h) --------------------------------------------------------------------------------------------
-// Item b: the four products of components, by what they are to be multiplied by to decrypt, with k x added where no key switch follows:
-// For moduli of 2^50 and more and for small rings; elsewhere the transforms form the four where they use them.  Four items of 24 limbs: 83 us, 0.5 GB.
+// Item b: the four products of components, with k x added where no key switch follows; in brackets what each is to be multiplied by to decrypt:
 //   e0 = a0 sigma(h0) + k x0 (1),  e1 = a1 sigma(h0) + k x1 (s),  u = a0 sigma(h1) (sigma(s)),  v = a1 sigma(h1) (s sigma(s));   each [n][level + 1][N]
+// For moduli of 2^50 and more and for small rings; elsewhere the transforms form the four where they use them.  Four items of 24 limbs: 89 us, 0.5 GB.
 __global__ __launch_bounds__(RC_THREADS) void turned_terms_kernel(PtrList8 a, size_t a_comp, PtrList8 h, size_t h_comp, PtrList8 x, size_t x_comp, LimbScalars k, u32 g,
                                                                   u64* __restrict__ out, const ModConst* __restrict__ mc, u32 log_n, u32 limbs, u32 n) {
     const u32 N = 1u << log_n, i = blockIdx.x * RC_THREADS + threadIdx.x;
@@ -157,7 +157,8 @@ hipError_t launch_centre(const ckks_ctx* c, u32 limbs, u32 n, const u64* in, siz
 }
 
 // d_z = r (x) k_grad (C g_z - S) + (k_norm t) (x) xh_z on limbs 0 .. level: d0, d1, d2, each [n][level + 1][N].  Both products
-// are summed before they are decomposed, so that they share one key switch.  Four channels of 10 limbs: 53 us, 0.27 GB, 5.1 TB/s.
+// are summed before they are decomposed, so that they share one key switch.  Eight channels of 10 limbs: 97 us; operands and results once are 0.33 GB (3.3 TB/s), but the L2 caches fetch 0.42
+// and write 0.13 (5.6 TB/s), as the six words that all channels share come again for each, from the last-level cache.
 __global__ __launch_bounds__(RC_THREADS) void norm_grad_terms_kernel(NormGradTerms T, u64* __restrict__ out, const ModConst* __restrict__ mc, u32 N, u32 limbs, u32 n) {
     const u32 i = blockIdx.x * RC_THREADS + threadIdx.x;
     if (i >= N) return;
@@ -345,7 +346,7 @@ hipError_t launch_rot_sum(const ckks_ctx* c, u32 level, const u64* digits, size_
 }
 
 // ---- sums on the extended basis, copies ------------------------------------------------------------------------
-// v += w, n polynomials [E][N] each: sums of rotations for moduli of 2^50 and more.  16 polynomials of 21 limbs: 84 us, 0.53 GB.
+// v += w, n polynomials [E][N] each: sums of rotations, and of the two key switches of a rotated product, outside the fused passes.  16 polynomials of 21 limbs: 84 us, 0.53 GB.
 __global__ __launch_bounds__(RC_THREADS) void add_ext_kernel(u64* __restrict__ v, const u64* __restrict__ w, const ModConst* __restrict__ mc, u32 N, u32 level, u32 num_q) {
     const u32 i = blockIdx.x * RC_THREADS + threadIdx.x;
     if (i >= N) return;
