@@ -99,13 +99,16 @@ class _InverseRoot(NamedTuple):
     relative_error: float
 
 
+def _check_chain(level: int, iterations: int) -> None:
+    if iterations < 0 or level < 3 + 2 * iterations:
+        raise ValueError("need level >= 3 + 2 * iterations")
+
+
 def _inverse_root(q: Sequence[float], level: int, s_scale: float, interval: Tuple[float, float], iterations: int, eps: float, most: float = math.inf) -> _InverseRoot:
     """The guess and the Newton steps of 1 / sqrt(v) for v at ``s_scale``, level - 1 (see ``norm_constants``); most: a bound on the scale of the result."""
     lo, hi = interval
     if not 0 < lo < hi:
         raise ValueError("need 0 < lo < hi")
-    if iterations < 0 or level < 3 + 2 * iterations:
-        raise ValueError("need level >= 3 + 2 * iterations")
     sign = -1 if iterations % 2 else 1
     # the line
     b = (math.sqrt(hi) - math.sqrt(lo)) / (hi ** 1.5 - lo ** 1.5)
@@ -150,7 +153,8 @@ def norm_constants(moduli: Sequence[int], level: int, channels: int, scale: floa
     u * w, r^2 and s r each divided by one modulus, the product by another.  Outputs without gate and residual, at most sqrt(channels) in magnitude, get a scale at which they fit where
     they end at level 0; with either, out_scale times the largest output is the caller's to keep below half of q_0 .. q_out_level."""
     q = [float(int(m)) for m in moduli]
-    last = max(level - 2 - 2 * iterations, 1)
+    _check_chain(level, iterations)
+    last = level - 2 - 2 * iterations
     plain = gate_scale is None and residual is None
     most = _room(q, last - 1) / math.sqrt(channels) * q[last] / scale if plain else math.inf
     r = _inverse_root(q, level, channels * scale * scale / q[level], interval, iterations, eps, most)
@@ -175,17 +179,20 @@ class LayerNormConstants(NamedTuple):
 
 
 def layer_norm_constants(moduli: Sequence[int], level: int, channels: int, scale: float, interval: Tuple[float, float], iterations: int, eps: float = 0.0,
-                         gain_scale: Optional[float] = None, bias_scale: Optional[float] = None) -> LayerNormConstants:
+                         gain_scale: Optional[float] = None, bias_scale: Optional[float] = None, largest: Optional[float] = None) -> LayerNormConstants:
     """The integers of ``he_layer_norm`` for inputs at ``scale`` whose variances over the channels plus eps lie in ``interval``: what the Newton chain works on is channels^2
     times the variance, at the scale channels^2 scale^2 / q_level; the centred channels have channels times the inputs' scale.  norm, at most sqrt(channels - 1) in magnitude, has
-    the scale that a Newton step leaves as it is, or one at which it fits where it ends at level 0; with a gain out_scale times the largest |out| is the caller's to keep below half
-    of q_0 .. q_(norm_level - 1), by gain_scale."""
+    the scale that a Newton step leaves as it is, or one at which it, and with a gain out, fits where that ends at level 0; largest: a bound on |out| with a gain, sixteen times
+    norm's if not given."""
     q = [float(int(m)) for m in moduli]
+    _check_chain(level, iterations)
     if gain_scale is not None and level < 4 + 2 * iterations:
         raise ValueError("a gain needs one more level")
-    last = max(level - 2 - 2 * iterations, 1)
-    most = _room(q, last - 1) / math.sqrt(max(channels - 1, 1)) * q[last] / (channels * scale)
-    r = _inverse_root(q, level, channels * channels * scale * scale / q[level], interval, iterations, eps, most)
+    last, bound = level - 2 - 2 * iterations, math.sqrt(max(channels - 1, 1))
+    most = _room(q, last - 1) / bound  # norm's scale
+    if gain_scale is not None:
+        most = min(most, _room(q, last - 2) / (16.0 * bound if largest is None else largest) * q[last - 1] / gain_scale)
+    r = _inverse_root(q, level, channels * channels * scale * scale / q[level], interval, iterations, eps, most * q[last] / (channels * scale))
     norm_scale, m = channels * scale * r.scale / q[r.level], r.level - 1
     k_bias = round(gain_scale * norm_scale / bias_scale) if gain_scale is not None and bias_scale is not None else 0
     _check_int64(r.k_eps, r.k_slope, r.k_start, k_bias, *r.k_newton)

@@ -93,3 +93,20 @@ def test_root_mean_square_norm_that_ends_at_the_last_prime(world, channels, iter
     want = x / np.sqrt(square)
     assert k.out_level == 0
     assert np.abs(w.decrypt(out, 0, k.out_scale) - want).max() < BOUND + k.relative_error * np.abs(want).max()
+
+
+@pytest.mark.parametrize("alike", [False, True])
+@pytest.mark.parametrize("channels,iterations", [(2, 1), (4, 0), (9, 2)])
+def test_layer_norm_with_gain_and_bias_that_ends_at_the_last_prime(world, channels, iterations, alike):
+    """From the lowest level: out at level 0.  Its error is the norm's times gains up to 2."""
+    w, rng, level = world, np.random.default_rng(channels), 4 + 2 * iterations
+    n = w.orc.n
+    x, gain, bias = channels_of(rng, channels, n, alike), rng.uniform(1, 2, channels), rng.uniform(-2, 2, channels)
+    var = x.var(0) + EPS
+    k = layer_norm_constants(w.p.moduli, level, channels, 2.0 ** 46, (0.99 * var.min(), 1.01 * var.max()), iterations, EPS, SCALE, SCALE)
+    ct_gain, ct_bias = (w.encrypt(np.repeat(v[:, None], n, 1), 1, SCALE, s) for v, s in ((gain, 40), (bias, 50)))
+    norm, inv, out = w.orc.layer_norm(w.encrypt(x, level, 2.0 ** 46), level, k.k_eps, k.k_slope, k.k_start, k.k_newton, w.rlk, ct_gain, ct_bias, k.k_bias)
+    want, _, want_out = layer_norm(x, gain, bias)
+    assert k.norm_level == 1
+    assert np.abs(w.decrypt(norm, 1, k.norm_scale) - want).max() < BOUND + k.relative_error * np.abs(want).max()
+    assert np.abs(w.decrypt(out, 0, k.out_scale) - want_out).max() < 2 * (BOUND + k.relative_error * np.abs(want).max())
