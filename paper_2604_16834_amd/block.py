@@ -144,21 +144,22 @@ def _room(q: Sequence[float], level: int) -> float:
 
 
 def norm_constants(moduli: Sequence[int], level: int, channels: int, scale: float, interval: Tuple[float, float], iterations: int, eps: float = 0.0,
-                   gate_scale: Optional[float] = None, residual: Optional[Tuple[float, float]] = None) -> NormConstants:
+                   gate_scale: Optional[float] = None, residual: Optional[Tuple[float, float]] = None, largest: Optional[float] = None) -> NormConstants:
     """The integers of ``he_norm_gate`` for inputs at ``scale`` (close to the moduli: the mean square has the scale channels * scale^2 /
     q_level) whose mean squares plus eps lie in ``interval``; gate_scale: the gate's scale; residual: (factor, scale) of the residual.
 
     The first guess is the line a (1 - b v) whose error against 1 / sqrt(v) is the same at both ends and in the middle; a Newton step turns
     r sqrt(v) = 1 + e into 1 - (3 + e) e^2 / 2, so the first step's worst error is at e > 0 and all later ones come from below.  The scale of r is the one that a step leaves as it is: twice the scale of
-    u * w, r^2 and s r each divided by one modulus, the product by another.  Outputs without gate and residual, at most sqrt(channels) in magnitude, get a scale at which they fit where
-    they end at level 0; with either, out_scale times the largest output is the caller's to keep below half of q_0 .. q_out_level."""
+    u * w, r^2 and s r each divided by one modulus, the product by another.  Where outputs end at level 0 it is one at which they fit: without gate and residual they are at most
+    sqrt(channels) in magnitude; largest: a bound on them with either, sixteen times that if not given."""
     q = [float(int(m)) for m in moduli]
     _check_chain(level, iterations)
     last = level - 2 - 2 * iterations
-    plain = gate_scale is None and residual is None
-    most = _room(q, last - 1) / math.sqrt(channels) * q[last] / scale if plain else math.inf
-    r = _inverse_root(q, level, channels * scale * scale / q[level], interval, iterations, eps, most)
     t_scale = scale if gate_scale is None else scale * gate_scale / q[level]
+    bound = math.sqrt(channels)
+    if gate_scale is not None or residual is not None:
+        bound = 16.0 * bound if largest is None else largest
+    r = _inverse_root(q, level, channels * scale * scale / q[level], interval, iterations, eps, _room(q, last - 1) / bound * q[last] / t_scale)
     k_residual = round(residual[0] * t_scale * r.scale / residual[1]) if residual else 0
     _check_int64(r.k_eps, r.k_slope, r.k_start, k_residual, *r.k_newton)
     return NormConstants(r.k_eps, r.k_slope, r.k_start, r.k_newton, k_residual, r.level - 1, t_scale * r.scale / q[r.level], r.relative_error)

@@ -110,3 +110,29 @@ def test_layer_norm_with_gain_and_bias_that_ends_at_the_last_prime(world, channe
     assert k.norm_level == 1
     assert np.abs(w.decrypt(norm, 1, k.norm_scale) - want).max() < BOUND + k.relative_error * np.abs(want).max()
     assert np.abs(w.decrypt(out, 0, k.out_scale) - want_out).max() < 2 * (BOUND + k.relative_error * np.abs(want).max())
+
+
+@pytest.mark.parametrize("alike", [False, True])
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("channels,iterations", [(1, 1), (4, 0), (9, 2)])
+def test_root_mean_square_norm_with_gate_or_residual_that_ends_at_the_last_prime(world, channels, iterations, gated, alike):
+    """Plaintext gates up to 2, residuals up to 3 with the factor -1.5: outputs at level 0.  A gate multiplies the error of 1 / sqrt, a residual leaves it."""
+    w, rng, level = world, np.random.default_rng(channels), 3 + 2 * iterations
+    n, gate, residual = w.orc.n, None, None
+    x = channels_of(rng, channels, n, alike)
+    square = (x * x).mean(0) + EPS
+    args = (w.p.moduli, level, channels, 2.0 ** 47, (0.99 * square.min(), 1.01 * square.max()), iterations, EPS)
+    want = x / np.sqrt(square)
+    if gated:
+        values = channels_of(rng, channels, n, alike) * 2
+        gate = [w.orc.encode_ntt(row, 2.0 ** 49, level) for row in values]
+        want = want * values
+        k = norm_constants(*args, gate_scale=2.0 ** 49)
+    else:
+        values = channels_of(rng, channels, n, alike) * 3
+        residual = w.encrypt(values, level, 2.0 ** 46, 70)
+        want = want - 1.5 * values
+        k = norm_constants(*args, residual=(-1.5, 2.0 ** 46))
+    out = w.orc.norm_gate(w.encrypt(x, level, 2.0 ** 47), level, k.k_eps, k.k_slope, k.k_start, k.k_newton, w.rlk, gate, residual, k.k_residual)
+    assert k.out_level == 0
+    assert np.abs(w.decrypt(out, 0, k.out_scale) - want).max() < 2 * (BOUND + k.relative_error * channels ** 0.5)
