@@ -271,7 +271,8 @@ def scan_gate_mask(lengths: Sequence[int], slots: int, reverse: bool = False) ->
 
 def scan_constants(moduli: Sequence[int], level: int, scale: float, gate_scale: float, steps: int) -> ScanConstants:
     """The integers of ``he_scan_gated`` (and of its backward pass) for inputs at ``scale`` and gates at ``gate_scale``: at every step the gates' scale, rounded, as what is
-    carried on has to join a product with them.  Scales stay where gate_scale is close to the moduli."""
+    carried on has to join a product with them.  Scales stay where gate_scale is close to the moduli: out_scale times the largest state or
+    gradient has to stay below half of q_0 .. q_out_level, which at level 0 is the caller's to see to, by ``scale``."""
     if not 1 <= steps <= level:
         raise ValueError("need 1 <= steps <= level")
     q, k = [float(int(m)) for m in moduli], []
